@@ -385,6 +385,168 @@ mq_status mq_linear_noalloc(int M, int N, int K, const void* X, int ldx,
                             void* Y, int ldy, hipStream_t stream);
 
 /* ======================================================================== */
+/* Around the layers: norm, 8-bit product, 4-bit cache and its attention     */
+/* ======================================================================== */
+
+/* Types of values that are not codes. */
+typedef enum mq_dtype { MQ_FP16 = 0, MQ_BF16 = 1, MQ_FP32 = 2 } mq_dtype;
+
+/* Where INT8 activation codes go: plain rows (int8 [M, ldq], ldq >= K rounded up
+ * to 16, ldq % 16 == 0; codes between K and that are 0; scales fp32 [M]), or the
+ * A8 layout of mq_quantize_act8 (K % 128 == 0, ldq is not used; scales fp16 [M]). */
+typedef enum mq_act8_layout { MQ_ACT8_ROWS = 0, MQ_ACT8_A8 = 1 } mq_act8_layout;
+
+#define MQ_NORM_MAX_K 65536
+
+/*
+ * Residual addition, RMS norm and per-token INT8 quantisation:
+ *     h = rn(X + R)  (added in fp32, rounded once to `type`; h = X without R),
+ *     y = h gamma / sqrt(mean_k(h^2) + eps),
+ *     s_x[m] = max_k |y| / 127   (fp32; in the A8 layout rounded to fp16),
+ *     q = clamp(round_half_even(y / s_x), -127, 127)          (0 if s_x == 0).
+ * Everything between h and the codes is fp32.  A row that is not finite (a value
+ * of h or of h gamma, or the sum of squares, in fp32) has the scale NaN and codes 0.
+ *   type     : of X, R, gamma and H: MQ_FP16 or MQ_BF16.
+ *   X, R, H  : [M, ldx], [M, ldr], [M, ldh], leading dimensions >= K and
+ *              multiples of 8, 16-byte aligned.  R may be NULL (H is NULL then);
+ *              H may be X or R itself, and overlaps them in no other way.
+ *   gamma    : [K], 16-byte aligned.
+ *   K        : a multiple of 8 (A8 layout: of 128), at most MQ_NORM_MAX_K.
+ *   Xq8, s_x : out, by `layout`; Xq8 16-byte aligned.
+ */
+mq_status mq_rms_norm_quantize8(int M, int K, mq_dtype type, const void* X, int ldx,
+                                const void* R, int ldr, const void* gamma, float eps,
+                                void* H, int ldh, mq_act8_layout layout,
+                                void* Xq8, int ldq, void* s_x, hipStream_t stream);
+
+/* The same quantisation of X itself, into rows (inputs that no norm precedes):
+ * s_x[m] = max_k |X| / 127 in fp32. */
+mq_status mq_quantize_rows8(int M, int K, mq_dtype type, const void* X, int ldx,
+                            void* Xq8, int ldq, void* s_x, hipStream_t stream);
+
+/* The values that INT8 codes stand for: Y[m,k] = rn(s_x[m] q[m,k]), `type`
+ * MQ_FP16 or MQ_BF16, Y [M, ldy] with ldy >= K, ldy % 8 == 0, 16-byte aligned. */
+mq_status mq_dequantize_act8(int M, int K, mq_act8_layout layout, const void* Xq8, int ldq,
+                             const void* s_x, mq_dtype type, void* Y, int ldy,
+                             hipStream_t stream);
+
+#define MQ_W8A8_MAX_K 131056
+
+/*
+ * INT8 weights, one fp32 scale for each of N output channels.  Library layout:
+ * pieces of 16 channels x 64 codes of 1 KB, piece (n / 16, k / 64) at
+ * ((n / 16) ceil(K / 64) + k / 64) 1024, in it code (n, k) at byte
+ * 16 (n % 16 + 16 ((k % 64) / 16)) + k % 16; channels past N and codes past K
+ * are 0.  Any N in [1, 2^24] and K in [1, MQ_W8A8_MAX_K].
+ */
+size_t mq_weight8_bytes(int N, int K);
+/* s_w[n] = max_k |W[n,k]| / 127, q = clamp(round_half_even(W / s_w), -127, 127)
+ * (0 if s_w == 0 or is not finite) from fp32 W [N, ldw], ldw >= K.  Wq8: out,
+ * mq_weight8_bytes(N, K) bytes, 16-byte aligned; s_w: out, fp32 [N]. */
+mq_status mq_quantize_weight8(const float* W, int N, int K, int ldw, uint8_t* Wq8, float* s_w,
+                              hipStream_t stream);
+/* Canonical int8 rows Wc [N, ldw] (ldw >= K, any alignment) <-> that layout. */
+mq_status mq_repack_weight8(int N, int K, const int8_t* Wc, int ldw, uint8_t* Wq8,
+                            hipStream_t stream);
+mq_status mq_unpack_weight8(int N, int K, const uint8_t* Wq8, int8_t* Wc, int ldw,
+                            hipStream_t stream);
+
+/*
+ * W8A8 product:
+ *     Y[m,n] = rn( s_x[m] s_w[n] sum_k Xq[m,k] Wq[n,k] + bias[n] )
+ * The sums are exact in int32 (K <= MQ_W8A8_MAX_K); they are rounded once to
+ * fp32, multiplied by s_x s_w there, and the result once to `type`.
+ *   Xq8, s_x  : int8 [M, ldx], ldx >= K rounded up to 16, ldx % 16 == 0, 16-byte
+ *               aligned; a row's bytes between K and that are read and count for
+ *               nothing.  s_x fp32 [M].
+ *   Wq8, s_w  : library layout, fp32 [N].
+ *   type      : of bias (may be NULL) and Y: MQ_FP16, MQ_BF16 or MQ_FP32.
+ *   Y         : out, [M, ldy], ldy >= N, aligned to its type.
+ *   workspace : >= mq_gemm_w8a8_workspace_size(M, N, K) bytes, 16-byte aligned
+ *               (may be NULL when that is 0).
+ */
+size_t mq_gemm_w8a8_workspace_size(int M, int N, int K);
+mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ldx, const float* s_x,
+                       const uint8_t* Wq8, const float* s_w, mq_dtype type, const void* bias,
+                       void* Y, int ldy, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Paged cache of keys and values in 4 bits.  A page holds page_size tokens (a
+ * power of two, 16 .. 65536) of every key head; head_dim is 64 or 128.  A slot
+ * is page * page_size + the place in the page.  Each row of a token and head has
+ * a scale s and a minimum z, both fp16, and codes n in [0, 15]:
+ *     z = fp16_rn(min x), s = fp16_rn((max x - z) / 15),
+ *     n = clamp(round_half_even((x - z) / s), 0, 15)     (0 if s == 0),
+ * in fp32; the value is z + s n.  A row that holds infinity or NaN, or whose z or
+ * s passes fp16's range, has the parameters NaN.
+ *   k, v               : mq_kv4_code_bytes() bytes each, [pages][heads][page_size head_dim / 2]:
+ *     keys, token by token head_dim / 2 bytes: little-endian dword c holds channels
+ *     8c .. 8c + 7, channel 8c + 2j at bit 4j and 8c + 2j + 1 at bit 16 + 4j;
+ *     values, blocks of four tokens of 2 head_dim bytes: channels 4f .. 4f + 3 of
+ *     the block's token t are the 16-bit word at byte 8f + 2t, the first lowest.
+ *   k_params, v_params : [pages][heads][page_size] dwords, s in the low half, z in
+ *     the high half.
+ * All four 16-byte aligned.  The caller clears them once (zeros are valid rows).
+ */
+typedef struct mq_kv4_cache {
+    void *k, *v, *k_params, *v_params;
+    int pages, page_size, heads, head_dim;
+} mq_kv4_cache;
+
+size_t mq_kv4_code_bytes(int pages, int page_size, int heads, int head_dim);
+
+/*
+ * Quantises T tokens into the cache.
+ *   K, V  : `type` (MQ_FP16 or MQ_BF16), token t's head h at t k_token + h k_head
+ *           (elements, multiples of 8), head_dim contiguous values, 16-byte aligned.
+ *   slots : int64 [T]; the slots inside the cache are distinct, the others (-1 for
+ *           one) are skipped.
+ */
+mq_status mq_kv4_append(const mq_kv4_cache* cache, int T, mq_dtype type,
+                        const void* K, int64_t k_token, int64_t k_head,
+                        const void* V, int64_t v_token, int64_t v_head,
+                        const int64_t* slots, hipStream_t stream);
+
+/* The values of T slots, rounded to `type`; 0 for slots outside the cache. */
+mq_status mq_kv4_read(const mq_kv4_cache* cache, int T, mq_dtype type, const int64_t* slots,
+                      void* K, int64_t k_token, int64_t k_head,
+                      void* V, int64_t v_token, int64_t v_head, hipStream_t stream);
+
+/*
+ * Attention over the cache.  Sequence b has kv_lens[b] tokens, token t in place
+ * t % page_size of page page_table[b][t / page_size], and the queries
+ * cu_q[b] .. cu_q[b + 1] - 1 of the `tokens` rows of Q (cu_q NULL: query b).  Of
+ * its nq queries, query i sees the tokens 0 .. kv_lens[b] - nq + i (causal: the
+ * last query sees all), or all of them.  Query head h reads key head h / group.
+ *     O = sum_t p_t v_t / sum_t p_t,   p_t = exp(scale q.k_t)
+ * Queries and weights enter the products in fp16 (queries scaled by a power of
+ * two each); sums, maxima and the running results are fp32.
+ * A query that sees nothing gives 0.  A row of the cache that is not finite makes
+ * the queries that see it NaN, and no others.  Tokens of a page outside [0, pages)
+ * are seen by none.
+ *   Q, O       : `type`, [tokens, heads group, head_dim] by strides as above.
+ *   page_table : int32 [sequences, table_pages].
+ *   kv_lens    : int32 [sequences];  cu_q : int32 [sequences + 1], ascending.
+ *   max_q, max_kv : at least the largest number of queries and of tokens of a
+ *                sequence (host bounds that choose the launch; queries past max_q
+ *                are left out and lengths past max_kv cut);
+ *                max_kv <= table_pages page_size.
+ *   scale      : positive.
+ *   workspace  : >= mq_attention_kv4_workspace_size() bytes, 16-byte aligned (may
+ *                be NULL when that is 0).
+ * The result does not depend on the order in which anything runs.
+ */
+size_t mq_attention_kv4_workspace_size(int sequences, int tokens, int heads, int group,
+                                       int head_dim, int max_q, int64_t max_kv);
+mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, int tokens, int group,
+                           int max_q, int64_t max_kv, mq_dtype type,
+                           const void* Q, int64_t q_token, int64_t q_head,
+                           const int32_t* page_table, int table_pages, const int32_t* kv_lens,
+                           const int32_t* cu_q, float scale, int causal,
+                           void* O, int64_t o_token, int64_t o_head,
+                           void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ======================================================================== */
 /* Offline weight preparation (not on the timed path)                        */
 /* ======================================================================== */
 

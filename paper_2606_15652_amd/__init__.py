@@ -24,6 +24,8 @@ BLOCK = 128
 
 _P = C.c_void_p
 _I = C.c_int
+_L = C.c_int64
+_F = C.c_float
 _SIG = {
     "mq_status_string": (C.c_char_p, [_I]),
     "mq_version": (_I, []),
@@ -59,6 +61,21 @@ _SIG = {
     "mq_unpack_weights": (_I, [_I, _I, _P, _P, _I, _P, _P, _P, _P, _P]),
     "mq_repack_act": (_I, [_I, _I, _P, _I, _P, _P, _P]),
     "mq_unpack_act": (_I, [_I, _I, _P, _P, _I, _P]),
+    "mq_rms_norm_quantize8": (_I, [_I, _I, _I, _P, _I, _P, _I, _P, _F, _P, _I, _I, _P, _I, _P, _P]),
+    "mq_quantize_rows8": (_I, [_I, _I, _I, _P, _I, _P, _I, _P, _P]),
+    "mq_dequantize_act8": (_I, [_I, _I, _I, _P, _I, _P, _I, _P, _I, _P]),
+    "mq_weight8_bytes": (C.c_size_t, [_I, _I]),
+    "mq_quantize_weight8": (_I, [_P, _I, _I, _I, _P, _P, _P]),
+    "mq_repack_weight8": (_I, [_I, _I, _P, _I, _P, _P]),
+    "mq_unpack_weight8": (_I, [_I, _I, _P, _P, _I, _P]),
+    "mq_gemm_w8a8_workspace_size": (C.c_size_t, [_I, _I, _I]),
+    "mq_gemm_w8a8": (_I, [_I, _I, _I, _P, _I, _P, _P, _P, _I, _P, _P, _I, _P, C.c_size_t, _P]),
+    "mq_kv4_code_bytes": (C.c_size_t, [_I, _I, _I, _I]),
+    "mq_kv4_append": (_I, [_P, _I, _I, _P, _L, _L, _P, _L, _L, _P, _P]),
+    "mq_kv4_read": (_I, [_P, _I, _I, _P, _P, _L, _L, _P, _L, _L, _P]),
+    "mq_attention_kv4_workspace_size": (C.c_size_t, [_I, _I, _I, _I, _I, _I, _L]),
+    "mq_attention_kv4": (_I, [_P, _I, _I, _I, _I, _L, _I, _P, _L, _L, _P, _I, _P, _P, _F, _I, _P, _L, _L, _P,
+                              C.c_size_t, _P]),
 }
 
 _lib: Optional[C.CDLL] = None
@@ -529,3 +546,9 @@ def prepare_weight(W, nnzb: int, criterion: str = "frob", X_calib=None, stream=N
     Rq, s_r = quantize_residual(W, Wq, s_w, rowptr, kb, stream)
     N, K = W.shape
     return PackedWeight(N, K, Wq, s_w, rowptr, kb, Rq, s_r, score)
+
+
+from .serving import (  # noqa: E402  (needs the names above)
+    KVCache4, PackedWeight8, attention_kv4, attention_kv4_workspace_bytes, dequantize_act8, gemm_w8a8,
+    gemm_w8a8_workspace_bytes, kv4_append, kv4_cache, kv4_read, quantize_rows8, quantize_weight8, repack_weight8,
+    rms_norm_quantize8, unpack_weight8)

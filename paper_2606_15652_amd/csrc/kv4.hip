@@ -1,0 +1,193 @@
+// Keys and values of new tokens into the paged 4-bit cache, and back.
+//
+//   z = fp16(min x),  s = fp16((max x - z) / 15),  n = clamp(round_half_even((x - z) / s), 0, 15)
+//
+// for each row of a token and head; the value that a code stands for is z + s n.
+#include "kv4.h"
+
+namespace mq {
+
+struct Rows4 {
+    const void *k, *v;
+    void *ko, *vo;
+    int64_t k_token, k_head, v_token, v_head;   // strides, in elements
+    const int64_t* slots;
+    int tokens;
+};
+
+// Smallest and largest of a row's lanes (8 or 16 neighbouring lanes).
+template <int LANES>
+__device__ __forceinline__ float row_min(float v) {
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) v = fminf(v, __shfl_xor(v, m));
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float row_max(float v) {
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) v = fmaxf(v, __shfl_xor(v, m));
+    return v;
+}
+
+// The codes and parameters of a row, eight values of which this lane holds.
+template <int LANES>
+__device__ __forceinline__ uint32_t quantise4(const f32x8 x, uint32_t (&n)[8]) {
+    float lo = x[0], hi = x[0];
+    bool finite = true;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        lo = fminf(lo, x[j]);
+        hi = fmaxf(hi, x[j]);
+        finite = finite && (__float_as_uint(x[j]) & 0x7FFFFFFFu) < kFloatInf;
+    }
+    lo = row_min<LANES>(lo);
+    hi = row_max<LANES>(hi);
+    const uint64_t bad = __ballot(!finite);
+    const int lane = threadIdx.x & 63;
+    const bool row_finite = ((bad >> (lane & ~(LANES - 1))) & ((1u << LANES) - 1)) == 0;
+    const uint16_t zb = float_to_half_bits(lo);
+    const float z = half_bits_to_float(zb);
+    const uint16_t sb = float_to_half_bits((hi - z) / 15.0f);
+    const float s = half_bits_to_float(sb);
+    const bool ok = row_finite && (zb & 0x7FFFu) < kHalfInf && sb < kHalfInf;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float c = __builtin_amdgcn_fmed3f(rintf((x[j] - z) / s), 0.0f, 15.0f);
+        n[j] = ok && s > 0.0f ? (uint32_t)(int)c : 0u;
+    }
+    return ok ? (uint32_t)sb | (uint32_t)zb << 16 : 0x7E007E00u;
+}
+
+// A row of a token and head takes D / 8 lanes; a wave takes 512 / D neighbouring tokens of one head.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Rows4 r, Cache4 c) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int head = (int)(unit % c.heads), ch = lane % LANES;
+    const int64_t token = unit / c.heads * ROWS + lane / LANES;
+    const int64_t slot = token < r.tokens ? r.slots[token] : -1;
+    const bool there = slot >= 0 && slot < (int64_t)c.pages << c.page_bits;
+    f32x8 kx{}, vx{};
+    if (there) {
+        kx = load8(static_cast<const T*>(r.k) + token * r.k_token + head * r.k_head + 8 * ch);
+        vx = load8(static_cast<const T*>(r.v) + token * r.v_token + head * r.v_head + 8 * ch);
+    }
+    uint32_t kn[8], vn[8];
+    const uint32_t kp = quantise4<LANES>(kx, kn), vp = quantise4<LANES>(vx, vn);
+    if (!there) return;
+    const int64_t row = row_index(c, slot, head), first = row & ~(int64_t)((1 << c.page_bits) - 1);
+    const int in_page = (int)(row - first);
+    if (ch == 0) {
+        c.kp[row] = kp;
+        c.vp[row] = vp;
+    }
+    *reinterpret_cast<uint32_t*>(c.k + row * (D / 2) + 4 * ch) = key_word(kn);
+    uint8_t* values = c.v + first * (D / 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<uint16_t*>(values + value_offset<D>(in_page, 2 * ch + h)) =
+            (uint16_t)(vn[4 * h] | vn[4 * h + 1] << 4 | vn[4 * h + 2] << 8 | vn[4 * h + 3] << 12);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv4_read_kernel(Rows4 r, Cache4 c) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int head = (int)(unit % c.heads), ch = lane % LANES;
+    const int64_t token = unit / c.heads * ROWS + lane / LANES;
+    if (token >= r.tokens) return;
+    const int64_t slot = r.slots[token];
+    f32x8 kx{}, vx{};
+    if (slot >= 0 && slot < (int64_t)c.pages << c.page_bits) {
+        const int64_t row = row_index(c, slot, head), first = row & ~(int64_t)((1 << c.page_bits) - 1);
+        const uint32_t kp = c.kp[row], vp = c.vp[row];
+        const uint32_t kw = *reinterpret_cast<const uint32_t*>(c.k + row * (D / 2) + 4 * ch);
+        const uint8_t* values = c.v + first * (D / 2);
+        uint32_t vw = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            vw |= (uint32_t)*reinterpret_cast<const uint16_t*>(values + value_offset<D>((int)(row - first), 2 * ch + h)) << (16 * h);
+        const float ks = half_bits_to_float((uint16_t)kp), kz = half_bits_to_float((uint16_t)(kp >> 16));
+        const float vs = half_bits_to_float((uint16_t)vp), vz = half_bits_to_float((uint16_t)(vp >> 16));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            kx[j] = __builtin_fmaf(ks, (float)key_code(kw, j), kz);
+            vx[j] = __builtin_fmaf(vs, (float)((vw >> (4 * j)) & 15u), vz);
+        }
+    }
+    store8(static_cast<T*>(r.ko) + token * r.k_token + head * r.k_head + 8 * ch, kx);
+    store8(static_cast<T*>(r.vo) + token * r.v_token + head * r.v_head + 8 * ch, vx);
+}
+
+// What a cache has to be, for every call that takes one.
+mq_status check_cache4(const mq_kv4_cache* c) {
+    if (!c || c->pages < 0 || c->heads < 0 || c->page_size < 0 || c->head_dim < 0) return MQ_ERR_INVALID_ARG;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->page_size < 16 || c->page_size > 65536 ||
+        (c->page_size & (c->page_size - 1)) != 0 || c->heads < 1 || c->heads > 65535 || c->pages < 1)
+        return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (!c->k || !c->v || !c->k_params || !c->v_params) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(c->k, 16) || !mq_host::aligned(c->v, 16) || !mq_host::aligned(c->k_params, 16) ||
+        !mq_host::aligned(c->v_params, 16))
+        return MQ_ERR_MISALIGNED;
+    return MQ_OK;
+}
+Cache4 device_cache4(const mq_kv4_cache* c) {
+    return Cache4{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), static_cast<uint32_t*>(c->k_params),
+                  static_cast<uint32_t*>(c->v_params), c->pages, c->heads, __builtin_ctz((unsigned)c->page_size)};
+}
+
+static mq_status check_rows(const mq_kv4_cache* c, int T, const void* K, int64_t kt, int64_t kh, const void* V, int64_t vt,
+                            int64_t vh, const int64_t* slots, mq_dtype type) {
+    if (T < 0 || !mq_host::is_half_type(type)) return MQ_ERR_INVALID_ARG;
+    if (mq_status st = check_cache4(c); st != MQ_OK) return st;
+    for (int64_t s : {kt, kh, vt, vh})
+        if (s < 0 || s % 8 != 0) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MQ_OK;
+    if (!K || !V || !slots) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(K, 16) || !mq_host::aligned(V, 16) || !mq_host::aligned(slots, 8)) return MQ_ERR_MISALIGNED;
+    return MQ_OK;
+}
+
+template <typename F>
+static mq_status launch_rows(const mq_kv4_cache* c, int T, mq_dtype type, F&& run) {
+    if (T == 0) return MQ_OK;
+    const int rows = 512 / c->head_dim;
+    const int64_t units = ((int64_t)T + rows - 1) / rows * c->heads, blocks = (units + 3) / 4;
+    if (blocks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    return mq_host::with_half_type(type, [&](auto z) {
+        using T = decltype(z);
+        if (c->head_dim == 64) run(T{}, std::integral_constant<int, 64>{}, dim3((unsigned)blocks));
+        else run(T{}, std::integral_constant<int, 128>{}, dim3((unsigned)blocks));
+        return mq_host::launch_status();
+    });
+}
+
+}  // namespace mq
+
+using namespace mq;
+
+extern "C" size_t mq_kv4_code_bytes(int pages, int page_size, int heads, int head_dim) {
+    if (pages < 1 || page_size < 1 || heads < 1 || head_dim < 1) return 0;
+    return (size_t)pages * page_size * heads * head_dim / 2;
+}
+
+extern "C" mq_status mq_kv4_append(const mq_kv4_cache* cache, int T, mq_dtype type, const void* K, int64_t k_token,
+                                   int64_t k_head, const void* V, int64_t v_token, int64_t v_head, const int64_t* slots,
+                                   hipStream_t stream) {
+    if (mq_status st = check_rows(cache, T, K, k_token, k_head, V, v_token, v_head, slots, type); st != MQ_OK) return st;
+    const Rows4 r{K, V, nullptr, nullptr, k_token, k_head, v_token, v_head, slots, T};
+    return launch_rows(cache, T, type, [&](auto z, auto d, dim3 grid) {
+        hipLaunchKernelGGL((kv4_append_kernel<decltype(z), decltype(d)::value>), grid, dim3(256), 0, stream, r, device_cache4(cache));
+    });
+}
+
+extern "C" mq_status mq_kv4_read(const mq_kv4_cache* cache, int T, mq_dtype type, const int64_t* slots, void* K, int64_t k_token,
+                                 int64_t k_head, void* V, int64_t v_token, int64_t v_head, hipStream_t stream) {
+    if (mq_status st = check_rows(cache, T, K, k_token, k_head, V, v_token, v_head, slots, type); st != MQ_OK) return st;
+    const Rows4 r{nullptr, nullptr, K, V, k_token, k_head, v_token, v_head, slots, T};
+    return launch_rows(cache, T, type, [&](auto z, auto d, dim3 grid) {
+        hipLaunchKernelGGL((kv4_read_kernel<decltype(z), decltype(d)::value>), grid, dim3(256), 0, stream, r, device_cache4(cache));
+    });
+}

@@ -1,0 +1,277 @@
+"""Attention over the paged 4-bit cache, against the definition in 64 bits on the values that the
+cache holds; the tolerance is that of the kernel's roundings (serving_oracle.attention_error)."""
+import math
+
+import pytest
+import torch
+
+import serving_oracle as so
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.float16, torch.bfloat16]
+
+
+def mq():
+    import paper_2606_15652_amd as m
+    return m
+
+
+def filled(seqs, heads, dim):
+    m = mq()
+    cache = m.kv4_cache(seqs.pages, seqs.page, heads, dim)
+    if sum(seqs.lens):
+        m.kv4_append(cache, torch.cat(seqs.k).cuda(), torch.cat(seqs.v).cuda(), torch.cat(seqs.slots).cuda())
+    return cache
+
+
+def check(lens, nqs, heads, group, dim, page, dtype, seed=0, scale=None, causal=True, spread=1.0, q_spread=1.0, prepare=None, **how):
+    """lens, nqs: tokens and queries of each sequence (nqs None: one query each)."""
+    m = mq()
+    seqs = so.Sequences(lens, heads, dim, page, dtype, seed, spread)
+    if prepare:
+        prepare(seqs)
+    cache = filled(seqs, heads, dim)
+    counts = nqs or [1] * len(lens)
+    q = (torch.randn(sum(counts), heads * group, dim, generator=so.generator(seed, 5)) * q_spread).to(dtype)
+    cu = torch.tensor([0] + list(torch.tensor(counts).cumsum(0)), dtype=torch.int32)
+    o = m.attention_kv4(q.cuda(), cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu.cuda() if nqs else None, scale=scale,
+                        causal=causal, **how).cpu()
+    assert o.dtype == dtype and o.shape == q.shape
+    scale = scale or 1 / math.sqrt(dim)
+    for b, n in enumerate(lens):
+        k, v = so.values4(seqs.k[b]), so.values4(seqs.v[b])
+        part = slice(int(cu[b]), int(cu[b + 1]))
+        if counts[b] == 0:
+            continue
+        want = so.attention(q[part], k, v, scale, causal)
+        tol = so.attention_error(q[part], k, v, scale, dtype, want) if n else torch.zeros_like(want)
+        off = (o[part].double() - want).abs()
+        assert torch.equal(torch.isnan(o[part]), torch.isnan(want))
+        assert (off <= tol).logical_or(torch.isnan(want)).all(), (b, n, (off / tol).nan_to_num().max())
+    return q, cache, seqs, cu, o
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,group", [(1, 1), (2, 4), (1, 8), (3, 5), (1, 16), (1, 17), (2, 1)])
+def test_single_tokens(heads, group, dim, dtype):
+    check([1, 2, 15, 16, 17, 31, 32, 33, 100, 257, 700], None, heads, group, dim, 16, dtype)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 1024])
+def test_pages(page):
+    check([1, page - 1, page, page + 1, 3 * page + 5], None, 2, 4, 128, page, torch.float16, seed=page)
+    check([page + 1, 2 * page + 7], [9, 5], 2, 2, 64, page, torch.float16, seed=page)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,group", [(1, 1), (2, 4), (1, 8), (1, 3)])
+def test_prompts(heads, group, dim, dtype):
+    check([40, 1, 130, 64, 300], [40, 1, 33, 64, 7], heads, group, dim, 16, dtype)
+
+
+@pytest.mark.parametrize("nq", [2, 3, 4, 5, 16, 31, 33, 127, 129])
+def test_few_queries_at_the_end_of_a_context(nq):
+    check([nq, nq + 1, 200 + nq], [nq] * 3, 2, 4, 64, 32, torch.float16, seed=nq)
+
+
+@pytest.mark.parametrize("heads,group", [(2, 4), (1, 1)])
+def test_not_causal(heads, group):
+    check([50, 33, 200], [20, 33, 64], heads, group, 128, 16, torch.float16, causal=False)
+    check([50, 1], None, heads, group, 128, 16, torch.float16, causal=False)
+
+
+def test_rows_that_see_nothing():
+    # no tokens; more queries than tokens (the first ones stand before the first token); no queries
+    _, _, _, cu, o = check([0, 3, 40, 0, 20], [2, 8, 40, 1, 0], 2, 2, 64, 16, torch.float16)
+    assert not o[int(cu[0]):int(cu[1])].any() and not o[int(cu[1]):int(cu[1]) + 5].any()
+    _, _, _, _, o = check([0, 7, 0], None, 2, 4, 128, 16, torch.float16)
+    assert not o[0].any() and not o[2].any()
+
+
+@pytest.mark.parametrize("lens", [[5000], [4096, 3], [2049, 4999, 130, 0]])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_long_contexts_split_over_the_chip(lens, dim):
+    check(lens, None, 1, 4, dim, 64, torch.float16)
+
+
+def test_long_prompts():
+    check([700], [600], 1, 2, 128, 64, torch.bfloat16)
+
+
+def test_bounds_given_by_the_host():
+    q, cache, seqs, cu, o = check([30, 500, 77], [3, 7, 1], 2, 4, 128, 16, torch.float16, max_q=7, max_kv=500)
+    m = mq()
+    again = m.attention_kv4(q.cuda(), cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu.cuda())
+    assert (again.cpu().double() - o.double()).abs().max() <= 2e-3 * o.abs().max()
+
+
+def test_one_token_shares_and_sharp_rows():
+    # scores far apart: one token takes all the weight
+    check([300, 33], None, 2, 4, 128, 16, torch.float16, scale=8.0, q_spread=4.0)
+    # equal scores: q = 0
+    check([300, 33], None, 2, 4, 128, 16, torch.float16, q_spread=0.0)
+
+
+@pytest.mark.parametrize("spread", [1e-4, 300.0])
+def test_sizes_of_values(spread):
+    check([300, 33], None, 2, 4, 64, 16, torch.float16, spread=spread)
+    check([100], [90], 2, 4, 64, 16, torch.bfloat16, spread=spread)
+
+
+@pytest.mark.parametrize("dtype,q_spread", [(torch.float16, 2000.0), (torch.float16, 1e-6), (torch.bfloat16, 1e6), (torch.bfloat16, 1e-20)])
+def test_sizes_of_queries(dtype, q_spread):
+    check([200, 33], None, 2, 4, 64, 16, dtype, q_spread=q_spread, scale=1.0 / (8 * q_spread))
+
+
+def test_values_whose_scales_differ_by_much():
+    def prepare(seqs):
+        for v in seqs.v:
+            v *= torch.logspace(-3, 2, v.shape[0])[:, None, None].to(v.dtype)
+    check([400, 64], None, 2, 2, 128, 16, torch.float16, prepare=prepare)
+
+    def back(seqs):
+        for v in seqs.v:
+            v *= torch.logspace(2, -3, v.shape[0])[:, None, None].to(v.dtype)
+    check([400, 64], [64, 64], 2, 2, 128, 16, torch.float16, prepare=back)
+
+
+def test_rows_that_are_not_finite_reach_only_those_that_see_them():
+    def prepare(seqs):
+        seqs.k[0][20, 0, 3] = math.inf                      # key head 0, token 20
+        seqs.v[1][5, 1, 0] = math.nan                       # key head 1, token 5
+    _, _, _, cu, o = check([32, 16, 50], [32, 16, 50], 2, 2, 64, 16, torch.float16, prepare=prepare)
+    assert torch.isfinite(o[:20]).all() and torch.isnan(o[20:32, :2]).all() and torch.isfinite(o[20:32, 2:]).all()
+    assert torch.isfinite(o[32:37]).all() and torch.isnan(o[37:48, 2:]).all() and torch.isfinite(o[48:]).all()
+
+
+def test_what_lies_past_the_end_is_never_seen():
+    """Tokens of the last page past a sequence's length, and other pages, hold what is not finite."""
+    m = mq()
+    lens = [1, 13, 16, 35]
+    seqs = so.Sequences(lens, 2, 64, 16, torch.float16, 3)
+    cache = m.kv4_cache(seqs.pages, 16, 2, 64)
+    for t in (cache.k, cache.v):
+        t.fill_(0xFF)
+    for t in (cache.k_params, cache.v_params):
+        t.fill_(math.nan)
+    m.kv4_append(cache, torch.cat(seqs.k).cuda(), torch.cat(seqs.v).cuda(), torch.cat(seqs.slots).cuda())
+    for nqs in (None, [1, 13, 5, 35]):
+        counts = nqs or [1] * 4
+        q = torch.randn(sum(counts), 8, 64, generator=so.generator(4)).half()
+        cu = torch.tensor([0] + list(torch.tensor(counts).cumsum(0)), dtype=torch.int32)
+        o = m.attention_kv4(q.cuda(), cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu.cuda() if nqs else None).cpu()
+        for b in range(4):
+            part = slice(int(cu[b]), int(cu[b + 1]))
+            k, v = so.values4(seqs.k[b]), so.values4(seqs.v[b])
+            want = so.attention(q[part], k, v, 0.125, True)
+            assert ((o[part].double() - want).abs() <= so.attention_error(q[part], k, v, 0.125, torch.float16, want)).all()
+
+
+def test_pages_outside_the_cache_hold_nothing():
+    m = mq()
+    seqs = so.Sequences([48, 40], 1, 64, 16, torch.float16, 6)
+    cache = filled(seqs, 1, 64)
+    table = seqs.table.clone()
+    table[0, 1], table[1, 0] = -7, 1 << 30
+    q = torch.randn(2, 4, 64, generator=so.generator(8)).half()
+    o = m.attention_kv4(q.cuda(), cache, table.cuda(), seqs.kv_lens.cuda()).cpu()
+    for b, left in ((0, list(range(16)) + list(range(32, 48))), (1, list(range(16, 40)))):
+        k, v = so.values4(seqs.k[b])[left], so.values4(seqs.v[b])[left]
+        want = so.attention(q[b:b + 1], k, v, 0.125, False)
+        assert ((o[b:b + 1].double() - want).abs() <= so.attention_error(q[b:b + 1], k, v, 0.125, torch.float16, want)).all()
+
+
+def test_strides_and_in_place_output():
+    m = mq()
+    seqs = so.Sequences([20, 70], 2, 128, 16, torch.float16, 9)
+    cache = filled(seqs, 2, 128)
+    qkv = torch.randn(2, 12, 128, generator=so.generator(10)).half().cuda()
+    args = (cache, seqs.table.cuda(), seqs.kv_lens.cuda())
+    want = m.attention_kv4(qkv[:, :8].contiguous(), *args)
+    assert torch.equal(m.attention_kv4(qkv[:, :8], *args), want)
+    out = torch.full((8, 2, 136), 3.0).half().cuda()
+    m.attention_kv4(qkv[:, :8], *args, out=out.transpose(0, 1)[..., :128])
+    assert torch.equal(out.transpose(0, 1)[..., :128], want) and (out[..., 128:] == 3).all()
+
+
+def test_another_stream_a_workspace_and_the_same_again():
+    m = mq()
+    q, cache, seqs, _, o = check([3000, 100], None, 2, 4, 128, 16, torch.float16)
+    qd, args = q.cuda(), (cache, seqs.table.cuda(), seqs.kv_lens.cuda())
+    need = m.attention_kv4_workspace_bytes(2, 2, 2, 4, 128, 1, seqs.table.shape[1] * 16)
+    assert need > 0
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        got = m.attention_kv4(qd, *args, workspace=ws, stream=stream)
+        stream.synchronize()
+        assert torch.equal(got.cpu(), o)
+
+
+def test_in_a_graph():
+    m = mq()
+    q, cache, seqs, _, o = check([3000, 100], None, 2, 4, 128, 16, torch.float16)
+    qd, table, lens = q.cuda(), seqs.table.cuda(), seqs.kv_lens.cuda()
+    out = torch.empty_like(qd)
+    ws = torch.empty(m.attention_kv4_workspace_bytes(2, 2, 2, 4, 128, 1, seqs.table.shape[1] * 16), dtype=torch.uint8, device="cuda")
+    m.attention_kv4(qd, cache, table, lens, out=out, workspace=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.attention_kv4(qd, cache, table, lens, out=out, workspace=ws)
+    for i in range(4):
+        lens[0] = 3000 - 700 * i                            # the lengths are read when it runs
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, m.attention_kv4(qd, cache, table, lens))
+    lens[0] = 3000
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), o)
+
+
+def test_a_cache_past_32_bits():
+    """Pages near the end of more than 4 GB of codes."""
+    m = mq()
+    heads, dim, page = 64, 128, 256
+    cache = m.kv4_cache(4200, page, heads, dim)
+    g = so.generator(11)
+    k, v = torch.randn(300, heads, dim, generator=g).half(), torch.randn(300, heads, dim, generator=g).half()
+    t = torch.arange(300)
+    table = torch.tensor([[4199, 4198]], dtype=torch.int32)
+    m.kv4_append(cache, k.cuda(), v.cuda(), (table[0, t // page].long() * page + t % page).cuda())
+    q = torch.randn(1, heads, dim, generator=g).half()
+    o = m.attention_kv4(q.cuda(), cache, table.cuda(), torch.tensor([300], dtype=torch.int32).cuda()).cpu()
+    kd, vd, scale = so.values4(k), so.values4(v), 1 / math.sqrt(dim)
+    want = so.attention(q, kd, vd, scale, True)
+    assert ((o.double() - want).abs() <= so.attention_error(q, kd, vd, scale, torch.float16, want)).all()
+
+
+def test_refusals():
+    m = mq()
+    cache = m.kv4_cache(4, 16, 2, 64)
+    q, table, lens = torch.zeros(2, 4, 64).half().cuda(), torch.zeros(2, 2, dtype=torch.int32).cuda(), torch.ones(2, dtype=torch.int32).cuda()
+    cu = torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    for error, call in [
+        (TypeError, lambda: m.attention_kv4(q.float(), cache, table, lens)),
+        (ValueError, lambda: m.attention_kv4(q[:, :3], cache, table, lens)),
+        (ValueError, lambda: m.attention_kv4(q[..., :32], cache, table, lens)),
+        (ValueError, lambda: m.attention_kv4(q[:1], cache, table, lens)),
+        (TypeError, lambda: m.attention_kv4(q, cache, table.long(), lens)),
+        (TypeError, lambda: m.attention_kv4(q, cache, table, lens.long())),
+        (ValueError, lambda: m.attention_kv4(q, cache, table, lens[:1])),
+        (ValueError, lambda: m.attention_kv4(q, cache, table, lens, cu_q=cu[:2])),
+        (ValueError, lambda: m.attention_kv4(q, cache, table, lens, max_kv=33)),
+        (m.MQError, lambda: m.attention_kv4(q, cache, table, lens, scale=-1.0)),
+        (m.MQError, lambda: m.attention_kv4(q, cache, table, lens, scale=math.nan)),
+        (m.MQError, lambda: m.attention_kv4(q, cache, table, lens, cu_q=cu, max_q=-1)),
+        (m.MQError, lambda: m.attention_kv4(torch.zeros(2, 4, 72).half().cuda()[..., 4:68], cache, table, lens)),
+        (ValueError, lambda: m.attention_kv4(q, cache, table, lens, out=torch.zeros(2, 4, 32).half().cuda())),
+        (TypeError, lambda: m.attention_kv4(q, cache, table, lens, out=torch.zeros(2, 4, 64).cuda())),
+        (TypeError, lambda: m.attention_kv4(q.cpu(), cache, table, lens)),
+    ]:
+        with pytest.raises(error):
+            call()

@@ -1,0 +1,164 @@
+"""W8A8 product with scales for each token and channel, against exact integer sums."""
+import pytest
+import torch
+
+import serving_oracle as so
+
+pytestmark = pytest.mark.gpu
+
+
+def mq():
+    import paper_2606_15652_amd as m
+    return m
+
+
+def operands(M, N, K, seed=0):
+    g = so.generator(M, N, K, seed)
+    pad = -(-K // 16) * 16
+    x = torch.randint(-128, 128, (M, pad), generator=g, dtype=torch.int8)    # what lies past K counts for nothing
+    w = torch.randint(-128, 128, (N, K), generator=g, dtype=torch.int8)
+    return x[:, :K], 0.01 + torch.rand(M, generator=g), w, 1e-4 + 1e-3 * torch.rand(N, generator=g)
+
+
+def check(M, N, K, dtype=torch.float16, bias=False, seed=0, rows=None):
+    m = mq()
+    x, sx, w, sw = operands(M, N, K, seed)
+    b = torch.randn(N, generator=so.generator(N, 1)).to(dtype) if bias else None
+    base = torch.empty(M, x.stride(0) if M > 1 else -(-K // 16) * 16, dtype=torch.int8)
+    base[:, :K] = x
+    base[:, K:] = 77
+    xd = base.cuda()[:, :K]
+    pw = m.repack_weight8(w.cuda(), sw.cuda())
+    y = m.gemm_w8a8(xd, sx.cuda(), pw, bias=None if b is None else b.cuda(), out_dtype=dtype)
+    assert y.dtype == dtype and y.shape == (M, N)
+    i = torch.arange(M) if rows is None else torch.tensor(sorted(rows))
+    # integer sums are exact in double: |sum| <= 128^2 131056 < 2^53
+    total = (xd[i.cuda()].double() @ w.cuda().double().t()).cpu()
+    prod = total * (sx[i].double()[:, None] * sw.double())
+    want = prod if b is None else prod + b.double()
+    # the sum in fp32, the product of the scales and with it, the bias: four fp32 roundings, and the type's own
+    tol = 4 * 2.0 ** -24 * (prod.abs() + (want - prod).abs()) + so.UNIT[dtype] * want.abs() * 1.001 + so.TINY[dtype]
+    off = (y.cpu()[i].double() - want).abs()
+    assert (off <= tol).all(), (off / tol).max()
+    return xd, sx.cuda(), pw, y
+
+
+@pytest.mark.parametrize("K", [1, 15, 16, 17, 64, 65, 127, 512, 1000, 4096, 14336])
+@pytest.mark.parametrize("M,N", [(1, 1), (1, 1000), (3, 130), (16, 16), (17, 255), (33, 512), (130, 129)])
+def test_sizes(M, N, K):
+    check(M, N, K, [torch.float16, torch.bfloat16, torch.float32][(M + N + K) % 3], bias=(M + K) % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,K", [(64, 4096, 4096), (77, 25599, 640), (200, 1024, 5120), (256, 1024, 1024), (300, 513, 2000),
+                                   (512, 2048, 192), (1157, 1536, 4096), (2048, 4096, 1024), (2050, 4099, 513)])
+def test_larger(M, N, K, dtype):
+    check(M, N, K, dtype, bias=True)
+
+
+def test_longest_sums():
+    m = mq()
+    K = 131056
+    x, w = torch.full((2, K), -128, dtype=torch.int8), torch.full((3, K), -128, dtype=torch.int8)
+    w[1], w[2] = 127, 0
+    y = m.gemm_w8a8(x.cuda(), torch.ones(2).cuda(), m.repack_weight8(w.cuda(), torch.ones(3).cuda()), out_dtype=torch.float32)
+    assert torch.equal(y.cpu().double(), torch.tensor([[128.0 * 128 * K, -128.0 * 127 * K, 0.0]] * 2).double())
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 14336, 4096), (1, 4096, 14336), (4, 8192, 8192), (8, 28672, 8192), (32, 4096, 28672)])
+def test_decode_shapes(M, N, K):
+    check(M, N, K, torch.bfloat16)
+
+
+def test_large_prefill():
+    check(4097, 8200, 4096, torch.float16, bias=True, rows=[0, 1, 127, 128, 255, 256, 2047, 2048, 4095, 4096])
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (16, 64), (100, 1000), (513, 130), (4096, 512)])
+def test_weight_layout(N, K):
+    m = mq()
+    _, _, w, sw = operands(1, N, K, 9)
+    pw = m.repack_weight8(w.cuda(), sw.cuda())
+    assert torch.equal(m.unpack_weight8(pw).cpu(), w)
+    raw = pw.Wq.cpu().view(torch.int8).reshape(-(-N // 16), -(-K // 64), 4, 16, 16)     # piece, quarter of 64 codes, row, code
+    want = torch.zeros(-(-N // 16) * 16, -(-K // 64) * 64, dtype=torch.int8)
+    want[:N, :K] = w
+    assert torch.equal(raw, want.reshape(-(-N // 16), 16, -(-K // 64), 4, 16).permute(0, 2, 3, 1, 4))
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (37, 100), (512, 4096)])
+def test_quantize_weight(N, K):
+    m = mq()
+    w = torch.randn(N, K, generator=so.generator(N, K)) * 0.02
+    if N > 2:
+        w[1] = 0
+        w[2, 5] = float("inf")
+    pw = m.quantize_weight8(w.cuda())
+    codes, s = m.unpack_weight8(pw).cpu(), pw.s_w.cpu()
+    s32 = w.abs().amax(-1) / 127
+    assert torch.equal(s, s32)
+    ok = torch.isfinite(s32) & (s32 > 0)
+    assert not codes[~ok].any()
+    assert torch.equal(codes[ok], (w[ok] / s32[ok, None]).round().clamp(-127, 127).to(torch.int8))
+
+
+def test_strided_output_and_stream():
+    m = mq()
+    xd, sx, pw, y = check(70, 300, 512)
+    out = torch.full((70, 304), 5.0, dtype=torch.float16, device="cuda")
+    m.gemm_w8a8(xd, sx, pw, out=out[:, :300])
+    assert torch.equal(out[:, :300], y) and (out[:, 300:] == 5).all()
+    out = torch.full((70, 301), 5.0, dtype=torch.float16, device="cuda")                # rows at odd addresses
+    m.gemm_w8a8(xd, sx, pw, out=out[:, 1:])
+    assert torch.equal(out[:, 1:], y) and (out[:, 0] == 5).all()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    again = m.gemm_w8a8(xd, sx, pw, stream=stream)
+    stream.synchronize()
+    assert torch.equal(again, y)
+
+
+def test_the_same_again():
+    xd, sx, pw, y = check(40, 4096, 8192)
+    for _ in range(5):
+        assert torch.equal(mq().gemm_w8a8(xd, sx, pw), y)
+
+
+def test_a_scale_that_is_not_finite_stays_in_its_row():
+    m = mq()
+    xd, sx, pw, y = check(20, 64, 128)
+    sx[3] = float("nan")
+    z = m.gemm_w8a8(xd, sx, pw)
+    assert torch.isnan(z[3]).all() and torch.equal(torch.cat((z[:3], z[4:])), torch.cat((y[:3], y[4:])))
+
+
+def test_empty():
+    m = mq()
+    _, _, w, sw = operands(1, 32, 64)
+    assert m.gemm_w8a8(torch.empty(0, 64, dtype=torch.int8).cuda(), torch.empty(0).cuda(),
+                       m.repack_weight8(w.cuda(), sw.cuda())).shape == (0, 32)
+
+
+def test_refusals():
+    m = mq()
+    x, sx, w, sw = operands(4, 32, 64)
+    x, sx, pw = x.contiguous().cuda(), sx.cuda(), m.repack_weight8(w.cuda(), sw.cuda())
+    odd = torch.zeros(4, 72, dtype=torch.int8).cuda()
+    for error, call in [
+        (TypeError, lambda: m.gemm_w8a8(x.float(), sx, pw)),
+        (TypeError, lambda: m.gemm_w8a8(x, sx.half(), pw)),
+        (TypeError, lambda: m.gemm_w8a8(x.cpu(), sx, pw)),
+        (ValueError, lambda: m.gemm_w8a8(x, sx[:3], pw)),
+        (ValueError, lambda: m.gemm_w8a8(x[:, :48].contiguous(), sx, pw)),
+        (ValueError, lambda: m.gemm_w8a8(odd[:, :64], sx, pw)),                         # a row stride of 72
+        (ValueError, lambda: m.gemm_w8a8(torch.zeros(64, 4, dtype=torch.int8).cuda().t(), sx, pw)),
+        (m.MQError, lambda: m.gemm_w8a8(torch.zeros(4 * 64 + 8, dtype=torch.int8).cuda()[8:].view(4, 64), sx, pw)),
+        (TypeError, lambda: m.gemm_w8a8(x, sx, pw, bias=torch.zeros(32).cuda())),
+        (ValueError, lambda: m.gemm_w8a8(x, sx, pw, bias=torch.zeros(31).half().cuda())),
+        (ValueError, lambda: m.gemm_w8a8(x, sx, pw, out=torch.zeros(4, 31).half().cuda())),
+        (TypeError, lambda: m.gemm_w8a8(x, sx, pw, out_dtype=torch.float64)),
+        (ValueError, lambda: m.repack_weight8(torch.zeros(2, 131057, dtype=torch.int8).cuda(), sw[:2].cuda())),
+        (TypeError, lambda: m.repack_weight8(w.cuda().float(), sw.cuda())),
+    ]:
+        with pytest.raises(error):
+            call()

@@ -1,0 +1,165 @@
+"""The paged 4-bit cache: what a write leaves in it, and what is read back."""
+import math
+
+import pytest
+import torch
+
+import serving_oracle as so
+
+pytestmark = pytest.mark.gpu
+
+
+def mq():
+    import paper_2606_15652_amd as m
+    return m
+
+
+def rows(T, H, D, dtype, seed):
+    g = so.generator(T, H, D, seed)
+    k = torch.randn(T, H, D, generator=g)
+    k[..., ::16] += 4.0
+    return k.to(dtype), (torch.randn(T, H, D, generator=g) * 0.1).to(dtype)
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a, nan=1e4), torch.nan_to_num(b, nan=1e4)) and torch.equal(torch.isnan(a), torch.isnan(b))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,H,D,page", [(1, 1, 64, 16), (5, 3, 128, 16), (64, 8, 128, 64), (33, 2, 64, 32), (1000, 5, 64, 128),
+                                        (300, 8, 128, 256), (16, 40, 128, 16)])
+def test_write_and_read(T, H, D, page, dtype):
+    m = mq()
+    k, v = rows(T, H, D, dtype, 1)
+    pages = -(-T // page) + 3
+    cache = m.kv4_cache(pages, page, H, D)
+    slots = torch.randperm(pages * page, generator=so.generator(T, page))[:T]
+    m.kv4_append(cache, k.cuda(), v.cuda(), slots.cuda())
+    for out in (torch.float16, torch.bfloat16):
+        gk, gv = m.kv4_read(cache, slots.cuda(), out)
+        assert torch.equal(gk.cpu(), so.values4(k).to(out)) and torch.equal(gv.cpu(), so.values4(v).to(out))
+    # slots that nothing was written to are as they were
+    other = torch.ones(pages * page, dtype=torch.bool)
+    other[slots] = False
+    gk, gv = m.kv4_read(cache, other.nonzero()[:, 0].cuda())
+    assert not gk.any() and not gv.any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_layout_of_the_cache(D):
+    m = mq()
+    T, H, page = 64, 2, 32
+    k, v = rows(T, H, D, torch.float16, 2)
+    cache = m.kv4_cache(2, page, H, D)
+    m.kv4_append(cache, k.cuda(), v.cuda(), torch.arange(T).cuda())
+    for x, codes, params in ((k, cache.k, cache.k_params), (v, cache.v, cache.v_params)):
+        n, s, z = so.quantise4(x)
+        want = torch.stack((s[..., 0], z[..., 0]), -1).half().reshape(2, page, H, 2).transpose(1, 2)
+        assert torch.equal(params.cpu(), want)
+        n = n.reshape(2, page, H, D).transpose(1, 2)                                    # [page][head][token][channel]
+        if x is k:
+            dword = codes.cpu().view(torch.int32).long().reshape(2, H, page, D // 8) & 0xFFFFFFFF
+            got = torch.stack([(dword >> (4 * (j // 2) + 16 * (j % 2))) & 15 for j in range(8)], -1).flatten(-2)
+        else:
+            word = codes.cpu().view(torch.int16).long().reshape(2, H, page // 4, D // 4, 4) & 0xFFFF     # block, channels / 4, token
+            got = torch.stack([(word >> (4 * j)) & 15 for j in range(4)], -1).permute(0, 1, 2, 4, 3, 5).reshape(2, H, page, D)
+        assert torch.equal(got, n)
+
+
+def test_rows_that_are_hard():
+    m = mq()
+    k, v = rows(12, 1, 64, torch.bfloat16, 3)
+    k[0] = 0                                                # no spread: scale 0
+    k[1] = -2.5
+    k[2, 0, 5] = math.inf
+    v[3, 0, 63] = math.nan
+    k[4, 0, 0], k[4, 0, 1] = -60000.0, 60000.0              # a range that passes fp16's largest
+    k[5] *= 1e-6                                            # a scale that is 0 in fp16, or nearly
+    k[6, 0, 9] = 1e6                                        # the scale does not fit fp16
+    v[7, 0, 3] = -1e6                                       # nor this minimum
+    cache = m.kv4_cache(1, 16, 1, 64)
+    m.kv4_append(cache, k.cuda(), v.cuda(), torch.arange(12).cuda())
+    gk, gv = m.kv4_read(cache, torch.arange(12).cuda(), torch.bfloat16)
+    wk, wv = so.values4(k).bfloat16(), so.values4(v).bfloat16()
+    assert same(gk.cpu(), wk) and same(gv.cpu(), wv)
+    assert torch.isnan(gk[2]).all() and torch.isnan(gv[3]).all() and torch.isnan(gv[7]).all()
+    assert torch.isfinite(gk[[0, 1, 3, 4, 5, 7]]).all()
+
+
+def test_slots_outside_are_skipped():
+    m = mq()
+    k, v = rows(6, 2, 128, torch.float16, 4)
+    cache = m.kv4_cache(1, 16, 2, 128)
+    slots = torch.tensor([-1, 3, 16, 1 << 40, 0, -(1 << 50)])
+    m.kv4_append(cache, k.cuda(), v.cuda(), slots.cuda())
+    gk, gv = m.kv4_read(cache, torch.arange(16).cuda())
+    assert torch.equal(gk[[3, 0]].cpu(), so.values4(k[[1, 4]]).half()) and torch.equal(gv[[3, 0]].cpu(), so.values4(v[[1, 4]]).half())
+    gk[[3, 0]], gv[[3, 0]] = 0, 0
+    assert not gk.any() and not gv.any()
+    gk, gv = m.kv4_read(cache, slots.cuda())
+    assert not gk[[0, 2, 3, 5]].any() and not gv[[0, 2, 3, 5]].any() and gk[1].any() and gv[4].any()
+
+
+def test_strides():
+    """Keys and values as slices of one projection, and head-major."""
+    m = mq()
+    g = so.generator(77)
+    qkv = torch.randn(20, 6, 128, generator=g).half()
+    heads_first = torch.randn(2, 20, 128, generator=g).half().transpose(0, 1)
+    cache = m.kv4_cache(2, 16, 2, 128)
+    m.kv4_append(cache, qkv.cuda()[:, 2:4], heads_first.cuda(), torch.arange(20).cuda())
+    out = torch.zeros(20, 4, 128).half().cuda()
+    m.kv4_read(cache, torch.arange(20).cuda(), out=(out[:, :2], out[:, 2:]))
+    assert torch.equal(out[:, :2].cpu(), so.values4(qkv[:, 2:4]).half()) and torch.equal(out[:, 2:].cpu(), so.values4(heads_first).half())
+
+
+def test_offsets_past_32_bits():
+    """A cache of more than 4 GB of codes: slots near its end."""
+    m = mq()
+    cache = m.kv4_cache(4200, 256, 64, 128)
+    assert cache.k.numel() > (1 << 32)
+    k, v = rows(40, 64, 128, torch.float16, 5)
+    slots = torch.cat((torch.arange(20), 4200 * 256 - 20 + torch.arange(20)))
+    m.kv4_append(cache, k.cuda(), v.cuda(), slots.cuda())
+    gk, gv = m.kv4_read(cache, slots.cuda())
+    assert torch.equal(gk.cpu(), so.values4(k).half()) and torch.equal(gv.cpu(), so.values4(v).half())
+
+
+def test_empty_and_stream():
+    m = mq()
+    cache = m.kv4_cache(1, 16, 1, 64)
+    none = torch.empty(0, 1, 64).half().cuda()
+    m.kv4_append(cache, none, none, torch.empty(0, dtype=torch.int64).cuda())
+    assert m.kv4_read(cache, torch.empty(0, dtype=torch.int64).cuda())[0].shape == (0, 1, 64)
+    k, v = rows(16, 1, 64, torch.float16, 6)
+    kd, vd, slots = k.cuda(), v.cuda(), torch.arange(16).cuda()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    m.kv4_append(cache, kd, vd, slots, stream=stream)
+    gk, _ = m.kv4_read(cache, slots, stream=stream)
+    stream.synchronize()
+    assert torch.equal(gk.cpu(), so.values4(k).half())
+
+
+def test_refusals():
+    m = mq()
+    cache = m.kv4_cache(2, 16, 2, 64)
+    k, slots = torch.zeros(4, 2, 64).half().cuda(), torch.arange(4).cuda()
+    wide = torch.zeros(4, 2, 68).half().cuda()
+    for error, call in [
+        (ValueError, lambda: m.kv4_cache(2, 24, 2, 64)),
+        (ValueError, lambda: m.kv4_cache(2, 16, 2, 96)),
+        (ValueError, lambda: m.kv4_cache(0, 16, 2, 64)),
+        (TypeError, lambda: m.kv4_append(cache, k.float(), k.float(), slots)),
+        (TypeError, lambda: m.kv4_append(cache, k, k.bfloat16(), slots)),
+        (TypeError, lambda: m.kv4_append(cache, k, k, slots.int())),
+        (ValueError, lambda: m.kv4_append(cache, k, k, slots[:3])),
+        (ValueError, lambda: m.kv4_append(cache, k, k[:3], slots)),
+        (ValueError, lambda: m.kv4_append(cache, k[:, :1], k[:, :1], slots)),
+        (ValueError, lambda: m.kv4_append(cache, k.transpose(1, 2).contiguous().transpose(1, 2), k, slots)),
+        (m.MQError, lambda: m.kv4_append(cache, wide[..., :64], k, slots)),            # a head stride of 68
+        (m.MQError, lambda: m.kv4_append(cache, torch.zeros(4, 2, 72).half().cuda()[..., 4:68], k, slots)),   # not aligned
+        (TypeError, lambda: m.kv4_append(cache, k.cpu(), k.cpu(), slots.cpu())),
+    ]:
+        with pytest.raises(error):
+            call()
