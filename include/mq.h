@@ -433,11 +433,13 @@ mq_status mq_dequantize_act8(int M, int K, mq_act8_layout layout, const void* Xq
 #define MQ_W8A8_MAX_K 131056
 
 /*
- * INT8 weights, one fp32 scale for each of N output channels.  Library layout:
- * pieces of 16 channels x 64 codes of 1 KB, piece (n / 16, k / 64) at
- * ((n / 16) ceil(K / 64) + k / 64) 1024, in it code (n, k) at byte
- * 16 (n % 16 + 16 ((k % 64) / 16)) + k % 16; channels past N and codes past K
- * are 0.  Any N in [1, 2^24] and K in [1, MQ_W8A8_MAX_K].
+ * INT8 weights, one fp32 scale for each of N output channels.  Library layout,
+ * with K padded to a multiple of 128 (Kp) and N to one of 64: blocks of 64
+ * channels, in them pieces of 64 codes, in them four pieces of 16 channels of 1 KB.
+ * Code (n, k), with c = n % 64, i = (c % 16) / 4 and r = 4 (c / 16) + c % 4, is at byte
+ *     (((n / 64) Kp / 64 + k / 64) 4 + i) 1024 + 16 (r + 16 ((k % 64) / 16)) + k % 16;
+ * channels past N and codes past K are 0.  Any N in [1, 2^24] and K in
+ * [1, MQ_W8A8_MAX_K].
  */
 size_t mq_weight8_bytes(int N, int K);
 /* s_w[n] = max_k |W[n,k]| / 127, q = clamp(round_half_even(W / s_w), -127, 127)

@@ -2,14 +2,27 @@
 // channel:  Y[m,n] = rn(s_x[m] s_w[n] sum_k Xq[m,k] Wq[n,k] + bias[n]).
 //
 // The sums run on v_mfma_i32_16x16x64_i8 in exact int32.  Weights are laid out
-// once in the instruction's operand order: the piece of 16 rows (channels) and
-// 64 codes is 1 KB, lane l's 16 bytes (row l % 16, codes 16 (l / 16) ..) at 16 l.
-// Rows past N and codes past K are zero, so whatever X holds past K adds nothing.
+// once in the instruction's operand order: a block of 64 channels holds, for
+// every 64 codes, four pieces of 16 channels x 64 codes, 1 KB each, lane l's 16
+// bytes (row l % 16, codes 16 (l / 16) ..) at 16 l.  Row 4 a + b of piece i is
+// channel 16 a + 4 i + b of the block: a lane's results of the four pieces are
+// 16 neighbouring channels.  Channels past N and codes past K are zero, so
+// whatever X holds past K adds nothing.
+//
+// Two kernels:
+//  * tiled: output tiles of 256 x 256 or 128 x 128, both operands through two
+//    LDS slots of 128 codes, filled by the LDS DMA;
+//  * streaming (few rows): weights go straight to registers, once; the eight
+//    waves of a workgroup share out K and add their sums in LDS (integers: in
+//    any order).
+#include "lds_dma.h"
 #include "mq_float.h"
 
 namespace mq {
 
-constexpr int kPieceRows = 16, kPieceK = 64, kPieceBytes = 1024;
+constexpr int kBlock8 = 64;             // channels of a block
+constexpr int kPieceK = 64, kPieceBytes = 1024;
+constexpr int kStageK = 128;            // codes of a slot; K is padded to a multiple
 
 struct Product8Args {
     int M, N, K;
@@ -21,55 +34,212 @@ struct Product8Args {
     const void* bias;
     void* Y;
     int64_t ldy;
+    int y16;                            // rows of Y 16-byte aligned
 };
 
-template <typename T>
-__device__ __forceinline__ float to_float(T v) { return (float)v; }
+__host__ __device__ __forceinline__ int padded_k8(int K) { return (K + kStageK - 1) / kStageK * kStageK; }
 
-// 32 x 32 outputs a wave, four waves a workgroup side by side along N.
+// y[c] = s_x s_w sum + bias for 16 channels n .. n + 15 of row m, stored.
 template <typename T>
-__global__ __launch_bounds__(256) void product8_kernel(Product8Args a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, quad = lane >> 4;
-    const int tiles_n = (a.N + 127) / 128;
-    const int n0 = (blockIdx.x % tiles_n * 4 + wave) * 32, m0 = blockIdx.x / tiles_n * 32;
-    const int pieces_k = (a.K + kPieceK - 1) / kPieceK, pieces_n = (a.N + kPieceRows - 1) / kPieceRows;
-    if (n0 >= a.N) return;
-    const uint8_t* w[2];
-    const uint8_t* x[2];
+struct Scales16 {
+    float w[16], b[16];
+    __device__ __forceinline__ Scales16(const Product8Args& a, int n) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        w[i] = a.W + (int64_t)min(n0 / kPieceRows + i, pieces_n - 1) * pieces_k * kPieceBytes + 16 * lane;
-        x[i] = a.X + min(m0 + 16 * i + row, a.M - 1) * a.ldx;
-    }
-    i32x4 acc[2][2] = {};
-    const int last = (a.K - 1) / 16 * 16;                   // first code of a row's last 16
-    for (int p = 0; p < pieces_k; ++p) {
-        i32x4 wv[2], xv[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            wv[i] = *reinterpret_cast<const i32x4*>(w[i] + (int64_t)p * kPieceBytes);
-            xv[i] = *reinterpret_cast<const i32x4*>(x[i] + min(p * kPieceK + 16 * quad, last));
+        for (int c = 0; c < 16; ++c) {
+            w[c] = n + c < a.N ? a.s_w[n + c] : 0.0f;
+            b[c] = a.bias && n + c < a.N ? (float)static_cast<const T*>(a.bias)[n + c] : 0.0f;
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[i], xv[j], acc[i][j], 0, 0, 0);
     }
+};
+template <typename T>
+__device__ __forceinline__ void store_row16(const Product8Args& a, int m, int n, const int (&sum)[16], const Scales16<T>& s) {
+    const float sx = a.s_x[m];
+    float y[16];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int m = m0 + 16 * j + row;
-        if (m >= a.M) continue;
-        const float sx = a.s_x[m];
+    for (int c = 0; c < 16; ++c) {
+        y[c] = (float)sum[c] * (sx * s.w[c]);
+        if (a.bias) y[c] += s.b[c];
+    }
+    T* row = static_cast<T*>(a.Y) + m * a.ldy + n;
+    if (a.y16 && n + 16 <= a.N) {
+        constexpr int per = 16 / sizeof(T);
+        typedef T vec __attribute__((ext_vector_type(per)));
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int c = 0; c < 16; c += per) {
+            vec v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = n0 + 16 * i + 4 * quad + r;
-                if (n >= a.N) continue;
-                float y = (float)acc[i][j][r] * (sx * a.s_w[n]);
-                if (a.bias) y += to_float(static_cast<const T*>(a.bias)[n]);
-                static_cast<T*>(a.Y)[m * a.ldy + n] = (T)y;
-            }
+            for (int e = 0; e < per; ++e) v[e] = (T)y[c + e];
+            *reinterpret_cast<vec*>(row + c) = v;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+            if (n + c < a.N) row[c] = (T)y[c];
+    }
+}
+
+// --------------------------------------------------------------------------
+// Tiled kernel: WM x WN waves, each 16 MI rows of X by one block of 64 channels.
+// --------------------------------------------------------------------------
+// A stage is 128 codes: rows of 128 bytes of X (16-byte chunk q of row r at q ^
+// (r % 8): reads of 16 rows are free of bank conflicts, and every load of eight
+// rows takes whole lines) and 8 KB of W for each block, in order.  One barrier a
+// stage, in its middle: it says that the next stage has landed and that this one
+// has been read (its second half is in registers by then), and the loads of the
+// stage after next go into its slot.
+template <typename T, int WM, int WN, int MI>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product8Args a) {
+    constexpr int TM = 16 * MI * WM, TN = kBlock8 * WN, NW = WM * WN;
+    static_assert(TM == 32 * NW && TN == 32 * NW, "four loads of each operand a wave");
+    __shared__ __attribute__((aligned(16))) struct {
+        uint8_t x[2][TM * kStageK];
+        uint8_t w[2][TN * kStageK];
+    } L;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, lq = lane >> 4;
+    const int kp = padded_k8(a.K), stages = kp / kStageK, blocks = (a.N + kBlock8 - 1) / kBlock8;
+    int tm, tn;
+    tile_coords(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
+    const int m0 = tm * TM, b0 = tn * WN;
+
+    const i32x4 rx = make_desc(a.X + m0 * a.ldx, (uint32_t)((min(TM, a.M - m0) - 1) * a.ldx + (a.K + 15) / 16 * 16));
+    const i32x4 rw = make_desc(a.W + (int64_t)b0 * kp * kBlock8, (uint32_t)min(WN, blocks - b0) * (uint32_t)(kp * kBlock8));
+    const uint32_t ldx = (uint32_t)a.ldx;
+    const uint32_t vx = (uint32_t)(lane >> 3) * ldx + (uint32_t)(((lane & 7) ^ (lane >> 3)) << 4);
+    const uint32_t vw = (uint32_t)lane * 16;
+    const uint32_t sx0 = (uint32_t)(32 * wave) * ldx, sw0 = (uint32_t)(wave / 2) * (uint32_t)(kp * kBlock8) + (uint32_t)(wave % 2) * 4096u;
+    auto issue = [&](int slot, int s) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            dma16s(rx, lds_addr(&L.x[slot][(4 * wave + k) * 1024]), vx, sx0 + (uint32_t)(8 * k) * ldx + (uint32_t)(s * kStageK));
+        dma16x4(rw, lds_addr(&L.w[slot][wave * 4096]), vw, sw0 + (uint32_t)(s * 8192));
+    };
+    const uint32_t xa = lds_addr(L.x) + (uint32_t)(wm * 16 * MI + lrow) * kStageK + (uint32_t)((lq ^ (lrow & 7)) << 4);
+    const uint32_t wa = lds_addr(L.w) + (uint32_t)(wn * 8192 + lane * 16);
+    struct Half {
+        i32x4 w[4], x[MI];
+    };
+    auto read = [&](Half& h, int slot, int kk) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h.w[i] = __builtin_bit_cast(i32x4, lds_read16(wa + slot * (TN * kStageK) + kk * 4096 + i * 1024));
+#pragma unroll
+        for (int j = 0; j < MI; ++j) h.x[j] = __builtin_bit_cast(i32x4, lds_read16((kk ? xa ^ 64u : xa) + slot * (TM * kStageK) + j * 2048));
+    };
+    i32x4 acc[4][MI] = {};
+    auto multiply = [&](const Half& h) {
+#pragma unroll
+        for (int j = 0; j < MI; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(h.w[i], h.x[j], acc[i][j], 0, 0, 0);
+    };
+
+    issue(0, 0);
+    if (stages > 1) {
+        issue(1, 1);
+        asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
+    } else {
+        wait_loads_and_sync();
+    }
+    Half h0, h1;
+    read(h0, 0, 0);
+    for (int s = 0; s < stages; s += 2) {
+#pragma unroll
+        for (int slot = 0; slot < 2; ++slot) {
+            if (s + slot >= stages) break;
+            read(h1, slot, 1);
+            multiply(h0);
+            wait_loads_and_sync();
+            if (s + slot + 2 < stages) issue(slot, s + slot + 2);
+            if (s + slot + 1 < stages) read(h0, slot ^ 1, 0);
+            multiply(h1);
+        }
+    }
+
+    const int n = (b0 + wn) * kBlock8 + 16 * lq;
+    if (n >= a.N) return;
+    const Scales16<T> scales(a, n);
+#pragma unroll
+    for (int j = 0; j < MI; ++j) {
+        const int m = m0 + wm * 16 * MI + 16 * j + lrow;
+        if (m >= a.M) break;
+        int sum[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[4 * i + r] = acc[i][j][r];
+        store_row16(a, m, n, sum, scales);
+    }
+}
+
+// --------------------------------------------------------------------------
+// Streaming kernel: P pieces of a block and all rows (16 MT) a workgroup.
+// --------------------------------------------------------------------------
+constexpr int kStreamWaves = 8;
+template <typename T, int P, int MT>
+__global__ __launch_bounds__(64 * kStreamWaves) void product8_stream_kernel(Product8Args a) {
+    constexpr int U = P + MT >= 8 ? 1 : 12 / (P + MT);       // pieces of K in flight, twice
+    __shared__ int sums[16 * MT][16 * P + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lrow = lane & 15, lq = lane >> 4;
+    const int kp = padded_k8(a.K), pieces = kp / kPieceK;
+    const int block = blockIdx.x / (4 / P), i0 = blockIdx.x % (4 / P) * P;
+    const uint8_t* w = a.W + (int64_t)block * kp * kBlock8 + i0 * kPieceBytes + 16 * lane;
+    uint32_t x[MT];                                         // rows, from X: at most 16 MT of 2^17 bytes
+#pragma unroll
+    for (int j = 0; j < MT; ++j) x[j] = (uint32_t)min(16 * j + lrow, a.M - 1) * (uint32_t)a.ldx;
+    const int last = (a.K - 1) / 16 * 16;                   // first code of a row's last 16
+    for (int i = threadIdx.x; i < 16 * MT * (16 * P + 1); i += 64 * kStreamWaves) (&sums[0][0])[i] = 0;
+
+    struct Batch {
+        i32x4 w[U][P], x[U][MT];
+    };
+    auto load = [&](Batch& b, int p0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = min(p0 + u * kStreamWaves, pieces - 1);
+#pragma unroll
+            for (int i = 0; i < P; ++i) b.w[u][i] = *reinterpret_cast<const i32x4*>(w + (int64_t)p * 4096 + i * kPieceBytes);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) b.x[u][j] = *reinterpret_cast<const i32x4*>(a.X + (x[j] + (uint32_t)min(p * kPieceK + 16 * lq, last)));
+        }
+    };
+    i32x4 acc[P][MT] = {};
+    auto multiply = [&](const Batch& b, int p0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + u * kStreamWaves >= pieces) break;
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int i = 0; i < P; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.w[u][i], b.x[u][j], acc[i][j], 0, 0, 0);
+        }
+    };
+    Batch b0, b1;
+    constexpr int step = U * kStreamWaves;
+    load(b0, wave);
+    for (int p = wave; p < pieces; p += 2 * step) {
+        if (p + step < pieces) load(b1, p + step);
+        multiply(b0, p);
+        if (p + step >= pieces) break;
+        if (p + 2 * step < pieces) load(b0, p + 2 * step);
+        multiply(b1, p + step);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) atomicAdd(&sums[16 * j + lrow][(4 * lq) * P + 4 * i + r], acc[i][j][r]);
+    __syncthreads();
+    // columns 4 P a + 4 i + b are channels 16 a + 4 (i0 + i) + b
+    for (int e = threadIdx.x; e < 16 * P * min(a.M, 16 * MT); e += 64 * kStreamWaves) {
+        const int m = e / (16 * P), c = e % (16 * P);
+        const int n = block * kBlock8 + c / (4 * P) * 16 + 4 * i0 + c % (4 * P);
+        if (n >= a.N) continue;
+        float y = (float)sums[m][c] * (a.s_x[m] * a.s_w[n]);
+        if (a.bias) y += (float)static_cast<const T*>(a.bias)[n];
+        static_cast<T*>(a.Y)[m * a.ldy + n] = (T)y;
     }
 }
 
@@ -85,14 +255,17 @@ struct FromCodes {
     int64_t ldw;
 };
 
+// channel of row r of piece i of its block
+__device__ __forceinline__ int channel8(int i, int r) { return 16 * (r / 4) + 4 * i + r % 4; }
+
 template <typename From>
 __global__ __launch_bounds__(1024) void pack_weight8_kernel(From from, int N, int K, uint8_t* __restrict__ Wq) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int pieces_k = (K + kPieceK - 1) / kPieceK;
-    const int row0 = blockIdx.x * kPieceRows;
-    __shared__ float scale[kPieceRows];
+    const int pieces = padded_k8(K) / kPieceK * 4;
+    const int row0 = blockIdx.x * kBlock8;
+    __shared__ float scale[kBlock8];
     if constexpr (__is_same(From, FromFloat)) {
-        for (int r = wave; r < kPieceRows; r += waves) {
+        for (int r = wave; r < kBlock8; r += waves) {
             uint32_t amax = 0;
             if (row0 + r < N)
                 for (int k = lane; k < K; k += 64)
@@ -106,26 +279,25 @@ __global__ __launch_bounds__(1024) void pack_weight8_kernel(From from, int N, in
         }
         __syncthreads();
     }
-    const int row = row0 + (lane & 15);
-    for (int p = wave; p < pieces_k; p += waves) {
-        const int k0 = p * kPieceK + 16 * (lane >> 4);
+    for (int p = wave; p < pieces; p += waves) {
+        const int k0 = p / 4 * kPieceK + 16 * (lane >> 4), c = channel8(p % 4, lane & 15), row = row0 + c;
         uint32_t b[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             int q = 0;
             if (row < N && k0 + e < K) {
                 if constexpr (__is_same(From, FromFloat)) {
-                    const float s = scale[lane & 15];
-                    const float c = rintf(from.W[row * from.ldw + k0 + e] / s);
+                    const float s = scale[c];
+                    const float f = rintf(from.W[row * from.ldw + k0 + e] / s);
                     // a row that is not finite: codes 0 (its scale is not finite either)
-                    q = s > 0.0f && __float_as_uint(s) < kFloatInf ? (int)__builtin_amdgcn_fmed3f(c, -127.0f, 127.0f) : 0;
+                    q = s > 0.0f && __float_as_uint(s) < kFloatInf ? (int)__builtin_amdgcn_fmed3f(f, -127.0f, 127.0f) : 0;
                 } else {
                     q = from.W[row * from.ldw + k0 + e];
                 }
             }
             b[e / 4] |= ((uint32_t)q & 0xFFu) << (8 * (e % 4));
         }
-        *reinterpret_cast<uint4*>(Wq + ((int64_t)blockIdx.x * pieces_k + p) * kPieceBytes + 16 * lane) = make_uint4(b[0], b[1], b[2], b[3]);
+        *reinterpret_cast<uint4*>(Wq + ((int64_t)blockIdx.x * pieces + p) * kPieceBytes + 16 * lane) = make_uint4(b[0], b[1], b[2], b[3]);
     }
 }
 
@@ -133,9 +305,10 @@ __global__ __launch_bounds__(256) void unpack_weight8_kernel(const uint8_t* __re
                                                              int8_t* __restrict__ Wc, int64_t ldw) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (int64_t)N * K) return;
-    const int n = (int)(i / K), k = (int)(i % K), pieces_k = (K + kPieceK - 1) / kPieceK;
-    const int lane = n % 16 + 16 * (k % kPieceK / 16);
-    Wc[n * ldw + k] = (int8_t)Wq[((int64_t)(n / 16) * pieces_k + k / kPieceK) * kPieceBytes + 16 * lane + k % 16];
+    const int n = (int)(i / K), k = (int)(i % K), c = n % kBlock8;
+    const int row = c / 16 * 4 + c % 4, piece = c % 16 / 4;     // channel8's inverse
+    const int64_t at = ((int64_t)(n / kBlock8) * (padded_k8(K) / kPieceK) + k / kPieceK) * 4 + piece;
+    Wc[n * ldw + k] = (int8_t)Wq[at * kPieceBytes + 16 * (row + 16 * (k % kPieceK / 16)) + k % 16];
 }
 
 static bool shape8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
@@ -146,7 +319,7 @@ using namespace mq;
 
 extern "C" size_t mq_weight8_bytes(int N, int K) {
     if (!shape8_ok(N, K)) return 0;
-    return (size_t)((N + kPieceRows - 1) / kPieceRows) * ((K + kPieceK - 1) / kPieceK) * kPieceBytes;
+    return (size_t)((N + kBlock8 - 1) / kBlock8) * kBlock8 * padded_k8(K);
 }
 
 extern "C" mq_status mq_quantize_weight8(const float* W, int N, int K, int ldw, uint8_t* Wq8, float* s_w, hipStream_t stream) {
@@ -154,7 +327,7 @@ extern "C" mq_status mq_quantize_weight8(const float* W, int N, int K, int ldw, 
     if (!shape8_ok(N, K) || ldw < K) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (!W || !Wq8 || !s_w) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(W, 4) || !mq_host::aligned(Wq8, 16) || !mq_host::aligned(s_w, 4)) return MQ_ERR_MISALIGNED;
-    hipLaunchKernelGGL(pack_weight8_kernel<FromFloat>, dim3((N + 15) / 16), dim3(1024), 0, stream, FromFloat{W, ldw, s_w}, N, K, Wq8);
+    hipLaunchKernelGGL(pack_weight8_kernel<FromFloat>, dim3((N + kBlock8 - 1) / kBlock8), dim3(1024), 0, stream, FromFloat{W, ldw, s_w}, N, K, Wq8);
     return mq_host::launch_status();
 }
 
@@ -163,7 +336,7 @@ extern "C" mq_status mq_repack_weight8(int N, int K, const int8_t* Wc, int ldw, 
     if (!shape8_ok(N, K) || ldw < K) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (!Wc || !Wq8) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(Wq8, 16)) return MQ_ERR_MISALIGNED;
-    hipLaunchKernelGGL(pack_weight8_kernel<FromCodes>, dim3((N + 15) / 16), dim3(1024), 0, stream, FromCodes{Wc, ldw}, N, K, Wq8);
+    hipLaunchKernelGGL(pack_weight8_kernel<FromCodes>, dim3((N + kBlock8 - 1) / kBlock8), dim3(1024), 0, stream, FromCodes{Wc, ldw}, N, K, Wq8);
     return mq_host::launch_status();
 }
 
@@ -196,12 +369,28 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
         return MQ_ERR_MISALIGNED;
     const size_t need = mq_gemm_w8a8_workspace_size(M, N, K);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
-    const Product8Args a{M, N, K, reinterpret_cast<const uint8_t*>(Xq8), ldx, s_x, Wq8, s_w, bias, Y, ldy};
+    const Product8Args a{M, N, K, reinterpret_cast<const uint8_t*>(Xq8), ldx, s_x, Wq8, s_w, bias, Y, ldy,
+                         mq_host::aligned(Y, 16) && ldy * size % 16 == 0};
     auto run = [&](auto z) {
         using T = decltype(z);
-        const int64_t tiles = (int64_t)((N + 127) / 128) * ((M + 31) / 32);
-        if (tiles > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
-        hipLaunchKernelGGL(product8_kernel<T>, dim3((unsigned)tiles), dim3(256), 0, stream, a);
+        const int blocks = (N + kBlock8 - 1) / kBlock8;
+        if (M <= 128) {
+            auto stream_rows = [&](auto mt) {
+                constexpr int MT = decltype(mt)::value;
+                if (blocks >= 384 && MT < 8) hipLaunchKernelGGL((product8_stream_kernel<T, MT < 8 ? 4 : 2, MT>), dim3(blocks), dim3(512), 0, stream, a);
+                else if (blocks >= 128 || MT == 8) hipLaunchKernelGGL((product8_stream_kernel<T, 2, MT>), dim3(2 * blocks), dim3(512), 0, stream, a);
+                else hipLaunchKernelGGL((product8_stream_kernel<T, MT < 8 ? 1 : 2, MT>), dim3(4 * blocks), dim3(512), 0, stream, a);
+            };
+            if (M <= 16) stream_rows(std::integral_constant<int, 1>{});
+            else if (M <= 32) stream_rows(std::integral_constant<int, 2>{});
+            else if (M <= 64) stream_rows(std::integral_constant<int, 4>{});
+            else stream_rows(std::integral_constant<int, 8>{});
+            return mq_host::launch_status();
+        }
+        auto tiles = [&](int tile) { return (int64_t)((M + tile - 1) / tile) * ((N + tile - 1) / tile); };
+        if (tiles(128) > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+        if (tiles(256) >= 256) hipLaunchKernelGGL((product8_tiled_kernel<T, 2, 4, 8>), dim3((unsigned)tiles(256)), dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((product8_tiled_kernel<T, 2, 2, 4>), dim3((unsigned)tiles(128)), dim3(256), 0, stream, a);
         return mq_host::launch_status();
     };
     return type == MQ_FP32 ? run(float{}) : mq_host::with_half_type(type, run);

@@ -38,9 +38,9 @@ def test_rows8(lib):
 
 
 def test_weight8(lib):
-    assert lib.mq_weight8_bytes(17, 65) == 2 * 2 * 1024
+    assert lib.mq_weight8_bytes(17, 65) == 64 * 128 and lib.mq_weight8_bytes(65, 129) == 128 * 256
     assert lib.mq_weight8_bytes(0, 64) == 0 and lib.mq_weight8_bytes(16, 131057) == 0
-    assert lib.mq_weight8_bytes(1 << 24, 131056) == (1 << 20) * 2048 * 1024
+    assert lib.mq_weight8_bytes(1 << 24, 131056) == (1 << 24) * 131072
     for f in (lambda N=16, K=64, W=A, ld=64, q=A: lib.mq_quantize_weight8(W, N, K, ld, q, A, None),
               lambda N=16, K=64, W=A, ld=64, q=A: lib.mq_repack_weight8(N, K, W, ld, q, None),
               lambda N=16, K=64, W=A, ld=64, q=A: lib.mq_unpack_weight8(N, K, q, W, ld, None)):

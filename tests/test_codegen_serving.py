@@ -45,6 +45,12 @@ def test_matrix_instructions(asm):
 
 def test_results_read_across_blocks_are_far(asm, monkeypatch):
     problems = {}
+    touches = tc._touches
+
+    def touches_but_sums(op, ops, pending):
+        # a matrix instruction that adds to the same registers needs no wait states (and is looked at itself)
+        return touches(op, ["", *ops[1:3]] if op.startswith("v_mfma") and ops[0] == ops[3] else ops, pending)
+    monkeypatch.setattr(tc, "_touches", touches_but_sums)
     for k, lines in asm.items():
         used = {l.split()[0] for l in lines if l.strip().startswith("v_mfma")}
         if used:

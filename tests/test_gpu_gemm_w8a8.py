@@ -80,10 +80,12 @@ def test_weight_layout(N, K):
     _, _, w, sw = operands(1, N, K, 9)
     pw = m.repack_weight8(w.cuda(), sw.cuda())
     assert torch.equal(m.unpack_weight8(pw).cpu(), w)
-    raw = pw.Wq.cpu().view(torch.int8).reshape(-(-N // 16), -(-K // 64), 4, 16, 16)     # piece, quarter of 64 codes, row, code
-    want = torch.zeros(-(-N // 16) * 16, -(-K // 64) * 64, dtype=torch.int8)
+    pn, pk = -(-N // 64), -(-K // 128) * 2
+    want = torch.zeros(pn * 64, pk * 64, dtype=torch.int8)
     want[:N, :K] = w
-    assert torch.equal(raw, want.reshape(-(-N // 16), 16, -(-K // 64), 4, 16).permute(0, 2, 3, 1, 4))
+    # block, row / 4, piece, row % 4; piece of 64 codes, quarter, code -> block, codes, piece, quarter, row, code
+    want = want.reshape(pn, 4, 4, 4, pk, 4, 16).permute(0, 4, 2, 5, 1, 3, 6)
+    assert torch.equal(pw.Wq.cpu().view(torch.int8), want.reshape(-1))
 
 
 @pytest.mark.parametrize("N,K", [(1, 1), (37, 100), (512, 4096)])
