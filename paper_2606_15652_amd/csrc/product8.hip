@@ -18,6 +18,8 @@
 #include "lds_dma.h"
 #include "mq_float.h"
 
+#include <algorithm>
+
 namespace mq {
 
 constexpr int kBlock8 = 64;             // channels of a block
@@ -39,10 +41,13 @@ struct Product8Args {
 
 __host__ __device__ __forceinline__ int padded_k8(int K) { return (K + kStageK - 1) / kStageK * kStageK; }
 
+__host__ __device__ __forceinline__ int padded_n8(int N) { return (N + kBlock8 - 1) / kBlock8 * kBlock8; }
+
 // y[c] = s_x s_w sum + bias for 16 channels n .. n + 15 of row m, stored.
 template <typename T>
 struct Scales16 {
     float w[16], b[16];
+    __device__ __forceinline__ Scales16() {}
     __device__ __forceinline__ Scales16(const Product8Args& a, int n) {
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
@@ -86,18 +91,23 @@ __device__ __forceinline__ void store_row16(const Product8Args& a, int m, int n,
 // rows takes whole lines) and 8 KB of W for each block, in order.  One barrier a
 // stage, in its middle: it says that the next stage has landed and that this one
 // has been read (its second half is in registers by then), and the loads of the
-// stage after next go into its slot.
-template <typename T, int WM, int WN, int MI>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product8Args a) {
+// stage SLOTS on go into its slot.  Loads past the last stage read nothing: they
+// keep the number in flight the same throughout.
+// SPLIT: workgroup y takes the stages [y, y + 1) per_split and writes its sums,
+// int32, to part[y][M][N].
+template <typename T, int WM, int WN, int MI, int SLOTS, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product8Args a, int per_split, int* __restrict__ part) {
     constexpr int TM = 16 * MI * WM, TN = kBlock8 * WN, NW = WM * WN;
-    static_assert(TM == 32 * NW && TN == 32 * NW, "four loads of each operand a wave");
+    constexpr int XL = TM / 8 / NW, WL = TN / 8 / NW;       // 1 KB loads of a wave and stage
+    static_assert(XL * NW * 8 == TM && (WL == 2 || WL == 4), "whole loads");
     __shared__ __attribute__((aligned(16))) struct {
-        uint8_t x[2][TM * kStageK];
-        uint8_t w[2][TN * kStageK];
+        uint8_t x[SLOTS][TM * kStageK];
+        uint8_t w[SLOTS][TN * kStageK];
     } L;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, lq = lane >> 4;
-    const int kp = padded_k8(a.K), stages = kp / kStageK, blocks = (a.N + kBlock8 - 1) / kBlock8;
+    const int kp = padded_k8(a.K), blocks = (a.N + kBlock8 - 1) / kBlock8;
+    const int first = SPLIT ? blockIdx.y * per_split : 0, stages = SPLIT ? min(per_split, kp / kStageK - first) : kp / kStageK;
     int tm, tn;
     tile_coords(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
     const int m0 = tm * TM, b0 = tn * WN;
@@ -107,23 +117,33 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product
     const uint32_t ldx = (uint32_t)a.ldx;
     const uint32_t vx = (uint32_t)(lane >> 3) * ldx + (uint32_t)(((lane & 7) ^ (lane >> 3)) << 4);
     const uint32_t vw = (uint32_t)lane * 16;
-    const uint32_t sx0 = (uint32_t)(32 * wave) * ldx, sw0 = (uint32_t)(wave / 2) * (uint32_t)(kp * kBlock8) + (uint32_t)(wave % 2) * 4096u;
-    auto issue = [&](int slot, int s) {
+    uint32_t sx = (uint32_t)(8 * XL * wave) * ldx + (uint32_t)(first * kStageK);
+    uint32_t sw = (uint32_t)(WL * wave / 8) * (uint32_t)(kp * kBlock8) + (uint32_t)(WL * wave % 8) * 1024u + (uint32_t)(first * 8192);
+    int to_load = stages;
+    auto issue = [&](int slot) {
+        const bool there = to_load-- > 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            dma16s(rx, lds_addr(&L.x[slot][(4 * wave + k) * 1024]), vx, sx0 + (uint32_t)(8 * k) * ldx + (uint32_t)(s * kStageK));
-        dma16x4(rw, lds_addr(&L.w[slot][wave * 4096]), vw, sw0 + (uint32_t)(s * 8192));
+        for (int k = 0; k < XL; ++k)
+            dma16s(rx, lds_addr(L.x) + (uint32_t)(slot * (TM * kStageK) + (XL * wave + k) * 1024), vx, there ? sx + (uint32_t)(8 * k) * ldx : kPastEnd);
+        const uint32_t dst = lds_addr(L.w) + (uint32_t)(slot * (TN * kStageK) + WL * wave * 1024);
+        if constexpr (WL == 4) dma16x4(rw, dst, vw, there ? sw : kPastEnd);
+        else dma16x2(rw, dst, vw, there ? sw : kPastEnd);
+        sx += kStageK;
+        sw += 8192;
     };
+    // the stage after the one being read has landed: those of SLOTS - 2 more are in flight
+    auto wait_and_sync = [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SLOTS - 2) * (XL + WL)) : "memory"); };
     const uint32_t xa = lds_addr(L.x) + (uint32_t)(wm * 16 * MI + lrow) * kStageK + (uint32_t)((lq ^ (lrow & 7)) << 4);
     const uint32_t wa = lds_addr(L.w) + (uint32_t)(wn * 8192 + lane * 16);
     struct Half {
         i32x4 w[4], x[MI];
     };
     auto read = [&](Half& h, int slot, int kk) {
+        const uint32_t xs = (kk ? xa ^ 64u : xa) + (uint32_t)(slot * (TM * kStageK)), ws = wa + (uint32_t)(slot * (TN * kStageK));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h.w[i] = __builtin_bit_cast(i32x4, lds_read16(wa + slot * (TN * kStageK) + kk * 4096 + i * 1024));
+        for (int i = 0; i < 4; ++i) h.w[i] = __builtin_bit_cast(i32x4, lds_read16(ws + kk * 4096 + i * 1024));
 #pragma unroll
-        for (int j = 0; j < MI; ++j) h.x[j] = __builtin_bit_cast(i32x4, lds_read16((kk ? xa ^ 64u : xa) + slot * (TM * kStageK) + j * 2048));
+        for (int j = 0; j < MI; ++j) h.x[j] = __builtin_bit_cast(i32x4, lds_read16(xs + j * 2048));
     };
     i32x4 acc[4][MI] = {};
     auto multiply = [&](const Half& h) {
@@ -133,42 +153,61 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product
             for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(h.w[i], h.x[j], acc[i][j], 0, 0, 0);
     };
 
-    issue(0, 0);
-    if (stages > 1) {
-        issue(1, 1);
-        asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
-    } else {
-        wait_loads_and_sync();
-    }
+    for (int s = 0; s < SLOTS; ++s) issue(s);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((SLOTS - 1) * (XL + WL)) : "memory");
     Half h0, h1;
     read(h0, 0, 0);
-    for (int s = 0; s < stages; s += 2) {
-#pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {
-            if (s + slot >= stages) break;
-            read(h1, slot, 1);
-            multiply(h0);
-            wait_loads_and_sync();
-            if (s + slot + 2 < stages) issue(slot, s + slot + 2);
-            if (s + slot + 1 < stages) read(h0, slot ^ 1, 0);
-            multiply(h1);
-        }
+    int slot = 0;
+    for (int s = 0; s < stages; ++s) {
+        const int next = slot + 1 == SLOTS ? 0 : slot + 1;
+        read(h1, slot, 1);
+        multiply(h0);
+        wait_and_sync();
+        issue(slot);
+        read(h0, next, 0);                                  // past the last stage: zeros, unused
+        multiply(h1);
+        slot = next;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // nothing may write LDS after the workgroup has gone
 
     const int n = (b0 + wn) * kBlock8 + 16 * lq;
     if (n >= a.N) return;
-    const Scales16<T> scales(a, n);
+    const Scales16<T> scales = SPLIT ? Scales16<T>{} : Scales16<T>(a, n);
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
         const int m = m0 + wm * 16 * MI + 16 * j + lrow;
         if (m >= a.M) break;
-        int sum[16];
+        if constexpr (SPLIT) {
+            int* p = part + ((int64_t)blockIdx.y * a.M + m) * padded_n8(a.N) + n;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<i32x4*>(p + 4 * i) = acc[i][j];
+        } else {
+            int sum[16];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum[4 * i + r] = acc[i][j][r];
-        store_row16(a, m, n, sum, scales);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[4 * i + r] = acc[i][j][r];
+            store_row16(a, m, n, sum, scales);
+        }
     }
+}
+
+// Sums of the splits -> Y, 16 channels a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void product8_join_kernel(Product8Args a, int splits, const int* __restrict__ part) {
+    const int np = padded_n8(a.N), per = np / 16;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)a.M * per) return;
+    const int m = (int)(i / per), n = (int)(i % per) * 16;
+    if (n >= a.N) return;
+    i32x4 sum[4] = {};
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += *reinterpret_cast<const i32x4*>(part + ((int64_t)s * a.M + m) * np + n + 4 * c);
+    int flat[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) flat[c] = sum[c / 4][c % 4];
+    store_row16(a, m, n, flat, Scales16<T>(a, n));
 }
 
 // --------------------------------------------------------------------------
@@ -313,6 +352,62 @@ __global__ __launch_bounds__(256) void unpack_weight8_kernel(const uint8_t* __re
 
 static bool shape8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
 
+// ---------------------------------------------------------------- host side --
+// Which kernel takes a product.  Up to 16 rows, and up to 32 where the weight is
+// small, the streaming kernel (K = N = 4096: M = 16 5.9 us, M = 32 7.9; the 64 x
+// 64 tiles 9.7 and 9.8; 4096 -> 14336 at M = 32 14.4 and 13.4).  Beyond, of four
+// tiles and one, two or four splits of K the one with the least estimated time:
+// stages of 128 codes by the time of one (a workgroup alone on its CU waits for
+// memory; more of them share the CU), or W at the rate that the tiles reach,
+// whichever is longer; and what writing, reading and joining a split's sums
+// takes.  The estimates are within a fifth of what was measured (K = 14336, N =
+// 4096: M = 64 in four splits 19.9 us, unsplit 34.5; M = 512 by 128 x 64 51.2,
+// 64 x 64 56.5, 128 x 128 91; K = N = 8192 at M = 1157 by 256 x 256 97, 128 x 128
+// 114; 5120 -> 25599 at M = 77 by 128 x 64 38.1, 64 x 64 44.5, 128 x 128 42.8).
+struct Tile8 {
+    int rows, cols;
+    double alone, share;                // us of a stage: one workgroup a CU, and of each of several
+    bool splits;
+};
+constexpr Tile8 kTiles8[4] = {
+    {64, 64, 0.26, 0.25, true},
+    {128, 64, 0.45, 0.345, true},
+    {128, 128, 0.95, 0.60, false},
+    {256, 256, 1.60, 1.60, false},
+};
+struct Plan8 {
+    int rows, cols;                     // of a workgroup's tile; cols of the streaming kernel: 16 P
+    bool streams;
+    int splits, per_split;              // stages of a split
+};
+static Plan8 plan8(int M, int N, int K) {
+    const int blocks = (N + kBlock8 - 1) / kBlock8, stages = padded_k8(K) / kStageK;
+    if (M <= 16 || (M <= 32 && blocks < 192 && K <= 8192)) {
+        // pieces of 16 channels a workgroup: four where that still makes three workgroups for four CUs (4096 -> 14336
+        // 11.6 us, two 13.1), two where K is short and they fill half the CUs (K = N = 4096 5.7, one 6.6; 14336 ->
+        // 4096 13.1 and 11.8), else one
+        const int p = blocks >= 192 ? 4 : blocks >= 64 && K <= 8192 ? 2 : 1;
+        return Plan8{M <= 16 ? 16 : 32, 16 * p, true, 1, stages};
+    }
+    Plan8 best{};
+    double least = 0.0;
+    for (const Tile8& t : kTiles8)
+        for (int splits = 1; splits <= (t.splits ? 4 : 1); splits *= 2) {
+            if (splits > 1 && stages < 8 * splits) break;
+            const int64_t groups = (int64_t)((M + t.rows - 1) / t.rows) * ((N + t.cols - 1) / t.cols) * splits;
+            const int64_t a_cu = (groups + 255) / 256;
+            const int per = (stages + splits - 1) / splits;
+            const double compute = per * std::max(t.alone, a_cu * t.share), memory = (double)N * K / 4.6e6;
+            const double join = splits == 1 ? 0.0 : 7.0 + (double)M * N * 4 * (splits + 1) / 5.0e6;
+            const double us = std::max(compute, memory) + join;
+            if (least == 0.0 || us < least) {
+                least = us;
+                best = Plan8{t.rows, t.cols, false, (stages + per - 1) / per, per};
+            }
+        }
+    return best;
+}
+
 }  // namespace mq
 
 using namespace mq;
@@ -352,8 +447,9 @@ extern "C" mq_status mq_unpack_weight8(int N, int K, const uint8_t* Wq8, int8_t*
 }
 
 extern "C" size_t mq_gemm_w8a8_workspace_size(int M, int N, int K) {
-    (void)M, (void)N, (void)K;
-    return 0;
+    if (M < 1 || M > (1 << 24) || !shape8_ok(N, K)) return 0;
+    const Plan8 p = plan8(M, N, K);
+    return p.splits == 1 ? 0 : (size_t)p.splits * M * padded_n8(N) * sizeof(int);
 }
 
 extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ldx, const float* s_x, const uint8_t* Wq8,
@@ -367,30 +463,43 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
     if (!mq_host::aligned(Xq8, 16) || !mq_host::aligned(Wq8, 16) || !mq_host::aligned(s_x, 4) || !mq_host::aligned(s_w, 4) ||
         !mq_host::aligned(bias, size) || !mq_host::aligned(Y, size))
         return MQ_ERR_MISALIGNED;
+    const Plan8 p = plan8(M, N, K);
     const size_t need = mq_gemm_w8a8_workspace_size(M, N, K);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     const Product8Args a{M, N, K, reinterpret_cast<const uint8_t*>(Xq8), ldx, s_x, Wq8, s_w, bias, Y, ldy,
                          mq_host::aligned(Y, 16) && ldy * size % 16 == 0};
     auto run = [&](auto z) {
         using T = decltype(z);
-        const int blocks = (N + kBlock8 - 1) / kBlock8;
-        if (M <= 128) {
-            auto stream_rows = [&](auto mt) {
-                constexpr int MT = decltype(mt)::value;
-                if (blocks >= 384 && MT < 8) hipLaunchKernelGGL((product8_stream_kernel<T, MT < 8 ? 4 : 2, MT>), dim3(blocks), dim3(512), 0, stream, a);
-                else if (blocks >= 128 || MT == 8) hipLaunchKernelGGL((product8_stream_kernel<T, 2, MT>), dim3(2 * blocks), dim3(512), 0, stream, a);
-                else hipLaunchKernelGGL((product8_stream_kernel<T, MT < 8 ? 1 : 2, MT>), dim3(4 * blocks), dim3(512), 0, stream, a);
-            };
-            if (M <= 16) stream_rows(std::integral_constant<int, 1>{});
-            else if (M <= 32) stream_rows(std::integral_constant<int, 2>{});
-            else if (M <= 64) stream_rows(std::integral_constant<int, 4>{});
-            else stream_rows(std::integral_constant<int, 8>{});
-            return mq_host::launch_status();
+        const int64_t groups = p.streams ? (int64_t)((N + kBlock8 - 1) / kBlock8) * (kBlock8 / p.cols)
+                                         : (int64_t)((M + p.rows - 1) / p.rows) * ((N + p.cols - 1) / p.cols);
+        if (groups > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+        int* part = static_cast<int*>(workspace);
+        auto stream_rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * kStreamWaves), 0, stream, a); };
+        auto tile = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups, p.splits), dim3(threads), 0, stream, a, p.per_split, part);
+        };
+        if (p.streams && p.rows == 16) {
+            if (p.cols == 64) stream_rows(product8_stream_kernel<T, 4, 1>);
+            else if (p.cols == 32) stream_rows(product8_stream_kernel<T, 2, 1>);
+            else stream_rows(product8_stream_kernel<T, 1, 1>);
+        } else if (p.streams) {
+            if (p.cols == 32) stream_rows(product8_stream_kernel<T, 2, 2>);
+            else stream_rows(product8_stream_kernel<T, 1, 2>);
+        } else if (p.rows == 256) {
+            tile(product8_tiled_kernel<T, 2, 4, 8, 2, false>, 512);
+        } else if (p.cols == 128) {
+            tile(product8_tiled_kernel<T, 4, 2, 2, 2, false>, 512);
+        } else if (p.rows == 128) {
+            if (p.splits > 1) tile(product8_tiled_kernel<T, 4, 1, 2, 3, true>, 256);
+            else tile(product8_tiled_kernel<T, 4, 1, 2, 3, false>, 256);
+        } else {
+            if (p.splits > 1) tile(product8_tiled_kernel<T, 4, 1, 1, 4, true>, 256);
+            else tile(product8_tiled_kernel<T, 4, 1, 1, 4, false>, 256);
         }
-        auto tiles = [&](int tile) { return (int64_t)((M + tile - 1) / tile) * ((N + tile - 1) / tile); };
-        if (tiles(128) > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
-        if (tiles(256) >= 256) hipLaunchKernelGGL((product8_tiled_kernel<T, 2, 4, 8>), dim3((unsigned)tiles(256)), dim3(512), 0, stream, a);
-        else hipLaunchKernelGGL((product8_tiled_kernel<T, 2, 2, 4>), dim3((unsigned)tiles(128)), dim3(256), 0, stream, a);
+        if (p.splits > 1) {
+            const int64_t joins = ((int64_t)M * (padded_n8(N) / 16) + 255) / 256;
+            hipLaunchKernelGGL(product8_join_kernel<T>, dim3((unsigned)joins), dim3(256), 0, stream, a, p.splits, part);
+        }
         return mq_host::launch_status();
     };
     return type == MQ_FP32 ? run(float{}) : mq_host::with_half_type(type, run);

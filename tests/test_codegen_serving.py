@@ -36,7 +36,7 @@ def asm():
 
 
 def test_matrix_instructions(asm):
-    matrix = [k for k in asm if re.search(r"attention4_kernel|\dproduct8_\w*kernel", k)]
+    matrix = [k for k in asm if re.search(r"attention4_kernel|product8_(tiled|stream)_kernel", k)]
     assert matrix
     for k in matrix:
         used = {l.split()[0] for l in asm[k] if l.strip().startswith("v_mfma")}
