@@ -96,68 +96,21 @@ __device__ __forceinline__ f16x8 value_operand(uint32_t a0, uint32_t a1, uint32_
     return __builtin_bit_cast(f16x8, u32x4{(a0 >> shift) & mask, (a1 >> shift) & mask, (b0 >> shift) & mask, (b1 >> shift) & mask});
 }
 
-// What a wave loads for 16 tokens: lane (r, g) has token r's key channels
-// (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r .. and parameters.
+// Operands and scales of 16 columns of queries: fp16, each column scaled by a power of two (its largest
+// value near 2^8, so that neither type's range matters), channels of the codes that come 16 times too
+// large divided by 16.  A lane has the channels (D / 4) g .. of its column.
 template <int D>
-struct Tile4 {
-    uint32_t k[D / 32], v[D / 32];
-    uint4 kp, vp;
-    bool there;
-};
-template <int D>
-__device__ __forceinline__ Tile4<D> load_tile(const Attn4Args& a, int b, int head, int t, int last, int lane) {
-    Tile4<D> x;
-    const int r = lane & 15, g = lane >> 4;
-    const int at = min(t, last);                            // the table is read for tokens that there are
-    const int page = __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.table_pages + (at >> a.c.page_bits)]);
-    x.there = (uint32_t)page < (uint32_t)a.c.pages;
-    const int64_t first = (((int64_t)(x.there ? page : 0) * a.c.heads + head) << a.c.page_bits);
-    const int in_page = t & ((1 << a.c.page_bits) - 1);
-    const uint8_t* k = a.c.k + (first + in_page) * (D / 2) + r * (D / 2) + g * (D / 8);
-    const uint8_t* v = a.c.v + (first + in_page) * (D / 2) + g * (2 * D) + r * (D / 8);
-    __builtin_memcpy(x.k, __builtin_assume_aligned(k, D / 8), D / 8);
-    __builtin_memcpy(x.v, __builtin_assume_aligned(v, D / 8), D / 8);
-    x.kp = *reinterpret_cast<const uint4*>(a.c.kp + first + in_page + 4 * g);
-    x.vp = *reinterpret_cast<const uint4*>(a.c.vp + first + in_page + 4 * g);
-    return x;
-}
+struct Queries {
+    f16x8 op[D / 32];
+    // x = sk (q'.n) + zk of_minimum is the score over to_score, in powers of 2
+    float to_score, of_minimum;
 
-// C: tiles of 16 columns a wave; WT: waves that share the columns and split the
-// tokens (4, or 1: every wave has columns of its own).
-template <typename T, int D, int C, int WT>
-__global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
-    constexpr int KK = D / 32, VT = D / 16, WaveCols = 16 * C, BlockCols = WaveCols * (4 / WT);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, g = lane >> 4;
-    const int blocks = (a.max_q * a.group + BlockCols - 1) / BlockCols;
-    int u = blockIdx.x;
-    const int split = u % a.splits;
-    u /= a.splits;
-    const int cb = u % blocks;
-    u /= blocks;
-    const int head = u % a.c.heads, b = u / a.c.heads;
-    const Sequence s = sequence(a, b);
-    const int cols = s.nq * a.group, col0 = cb * BlockCols + (WT == 1 ? wave * WaveCols : 0);
-    if (col0 >= cols) return;                               // WT == 1: no barrier follows
-    const int low = visible(a, s, col0 / a.group), high = visible(a, s, (min(col0 + WaveCols, cols) - 1) / a.group);
-    const int64_t first = (int64_t)split * a.chunk;
-    if (a.splits > 1 && first >= high) return;
-    const int begin = (int)first, end = (int)min((int64_t)high, first + a.chunk);
-
-    // Queries: fp16 operands, each column scaled by a power of two (its largest value near 2^8, so that
-    // neither type's range matters); channels of the codes that come 16 times too large divided by 16.
-    f16x8 qop[C][KK];
-    float to_score[C], of_minimum[C];
-    int limit[C];
-#pragma unroll
-    for (int j = 0; j < C; ++j) {
-        const int col = min(col0 + 16 * j + r, cols - 1), qi = col / a.group;
-        limit[j] = visible(a, s, qi);
-        const T* q = static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4);
-        f32x8 x[KK];
+    template <typename T>
+    __device__ __forceinline__ void load(const T* q, float scale) {
+        f32x8 x[D / 32];
         float sum = 0.0f, amax = 0.0f;
 #pragma unroll
-        for (int i = 0; i < KK; ++i) {
+        for (int i = 0; i < D / 32; ++i) {
             x[i] = load8(q + 8 * i);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -169,60 +122,173 @@ __global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
         amax = quads_max(amax);
         const int up = amax > 0.0f && amax < INFINITY ? 8 - ilogbf(amax) : 0;
 #pragma unroll
-        for (int i = 0; i < KK; ++i) {
+        for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = ldexpf(x[i][e], e & 2 ? up - 4 : up);
-            qop[j][i] = __builtin_convertvector(x[i], f16x8);
+            op[i] = __builtin_convertvector(x[i], f16x8);
         }
-        // of x = sk (q'.n) + zk of_minimum, in powers of 2; never zero or infinite, so that a hidden token's -infinity stays that
-        to_score[j] = fminf(fmaxf(ldexpf(a.scale * kLog2e, 24 - up), FLT_MIN), FLT_MAX);
-        of_minimum[j] = ldexpf(sum, up - 24);
+        // never zero or infinite, so that a hidden token's -infinity stays that
+        to_score = fminf(fmaxf(ldexpf(scale * kLog2e, 24 - up), FLT_MIN), FLT_MAX);
+        of_minimum = ldexpf(sum, up - 24);
+    }
+};
+
+// A result row (or part of one) of column col, not yet divided by the weights' sum: to the output, or
+// with splits to the partial results.
+template <typename T, int D, int N>
+__device__ __forceinline__ void store_result(const Attn4Args& a, const Sequence& s, int head, int split, int col, int channel,
+                                             const float (&values)[N], float mx, float sum, bool first) {
+    const int qi = col / a.group, h = head * a.group + col % a.group;
+    if (a.splits > 1) {
+        const int64_t row = ((int64_t)split * a.tokens + s.q0 + qi) * (a.c.heads * a.group) + h;
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            *reinterpret_cast<f32x4*>(a.part_o + row * D + channel + e) = f32x4{values[e], values[e + 1], values[e + 2], values[e + 3]};
+        if (first) {
+            a.part_m[row] = mx;
+            a.part_l[row] = sum;
+        }
+    } else {
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;       // a row that sees nothing is 0
+        T* o = static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + h * a.o_head + channel;
+        typedef T half4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+            *reinterpret_cast<half4*>(o + e) = __builtin_convertvector(
+                (f32x4{values[e] * by, values[e + 1] * by, values[e + 2] * by, values[e + 3] * by}), half4);
+    }
+}
+
+// --------------------------------------------------------------------------
+// Few columns: codes go from memory to registers and into the products.
+// --------------------------------------------------------------------------
+// What a wave loads for 16 tokens: lane (r, g) has token r's key channels
+// (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r .. and parameters.
+template <int D>
+struct Tile4 {
+    uint32_t k[D / 32], v[D / 32];
+    u32x4 kp, vp;
+};
+// The pages of a step's two tiles (the last token's where a tile is past the end: its page is there to be
+// read); negative: outside the cache.
+struct Pages {
+    int of[2];
+};
+__device__ __forceinline__ Pages find_pages(const Attn4Args& a, int b, int t, int last) {
+    Pages p;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int page = a.table[(int64_t)b * a.table_pages + (min(t + 16 * h, last) >> a.c.page_bits)];
+        p.of[h] = __builtin_amdgcn_readfirstlane((uint32_t)page < (uint32_t)a.c.pages ? page : -1);
+    }
+    return p;
+}
+template <int D>
+__device__ __forceinline__ void load_tile(Tile4<D>& x, const Attn4Args& a, int head, int page, int t, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+    const int64_t row = (((int64_t)max(page, 0) * a.c.heads + head) << a.c.page_bits) + (t & ((1 << a.c.page_bits) - 1));
+    const uint8_t* k = a.c.k + row * (D / 2);
+    const uint8_t* v = a.c.v + row * (D / 2);
+    __builtin_memcpy(x.k, __builtin_assume_aligned(k + (uint32_t)(r * (D / 2) + g * (D / 8)), D / 8), D / 8);
+    __builtin_memcpy(x.v, __builtin_assume_aligned(v + (uint32_t)(g * (2 * D) + r * (D / 8)), D / 8), D / 8);
+    x.kp = *reinterpret_cast<const u32x4*>(a.c.kp + row + (uint32_t)(4 * g));
+    x.vp = *reinterpret_cast<const u32x4*>(a.c.vp + row + (uint32_t)(4 * g));
+}
+
+// Every wave takes all the columns (16 C) and a share of the tokens; the step after
+// the one in hand is loaded meanwhile.  The parameters stay fp16 and are widened
+// inside mixed multiply-adds.  Weights w = p sv (in units of `unit`, at least every
+// sv) are rounded to fp16 for the second product, of which 7.5 sum(w) is taken off
+// again: codes about their middle, so that the rounding of w counts against values
+// about their middle.
+template <typename T, int D, int C>
+__global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
+    constexpr int KK = D / 32, VT = D / 16, WT = 4, Cols = 16 * C;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int blocks = (a.max_q * a.group + Cols - 1) / Cols;
+    int u = blockIdx.x;
+    const int split = u % a.splits;
+    u /= a.splits;
+    const int col0 = u % blocks * Cols;
+    u /= blocks;
+    const int head = u % a.c.heads, b = u / a.c.heads;
+    const Sequence s = sequence(a, b);
+    const int cols = s.nq * a.group;
+    if (col0 >= cols) return;
+    const int low = visible(a, s, col0 / a.group), high = visible(a, s, (min(col0 + Cols, cols) - 1) / a.group);
+    const int64_t first = (int64_t)split * a.chunk;
+    if (a.splits > 1 && first >= high) return;
+    const int begin = (int)first + wave * kStep, end = (int)min((int64_t)high, first + a.chunk);
+    constexpr int stride = kStep * WT;
+
+    Tile4<D> tile[2];
+    Pages pages{}, next{};
+    if (begin < end) {
+        pages = find_pages(a, b, begin, end - 1);
+        next = find_pages(a, b, begin + stride, end - 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_tile<D>(tile[h], a, head, pages.of[h], begin + 16 * h, lane);
+    }
+    Queries<D> q[C];
+    int limit[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const int col = min(col0 + 16 * j + r, cols - 1), qi = col / a.group;
+        limit[j] = visible(a, s, qi);
+        q[j].load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
     }
 
     f32x4 acc[C][VT] = {};
-    float m[C], l[C] = {}, zs[C] = {};
-    float unit = 0.0f, per_unit = 0.0f;                     // weights are held as multiples of unit, at least every sv
+    float m[C], l[C] = {}, zs[C] = {}, ws[C] = {};
+    float unit = 0.0f, per_unit = 0.0f;
 #pragma unroll
     for (int j = 0; j < C; ++j) m[j] = kLowest;
 
-    const int stride = kStep * WT;
-    for (int t = begin + (WT > 1 ? wave * kStep : 0); t < end; t += stride) {
-        const Tile4<D> tile[2] = {load_tile<D>(a, b, head, t, end - 1, lane), load_tile<D>(a, b, head, t + 16, end - 1, lane)};
+    for (int t = begin; t < end; t += stride) {
+        const Tile4<D> now[2] = {tile[0], tile[1]};
+        const bool all = pages.of[0] >= 0 && pages.of[1] >= 0, there[2] = {pages.of[0] >= 0, pages.of[1] >= 0};
+        pages = next;
+        if (t + stride < end) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) load_tile<D>(tile[h], a, head, pages.of[h], t + stride + 16 * h, lane);
+            next = find_pages(a, b, t + 2 * stride, end - 1);
+        }
         f32x4 x[C][2] = {};
-        float sv[2][4], zv[2][4];
+        f16x2 vp[2][4];                                     // scale, minimum; finite
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int i = 0; i < KK; ++i) {
-                const f16x8 k = key_operand(tile[h].k[i]);
+                const f16x8 k = key_operand(now[h].k[i]);
 #pragma unroll
-                for (int j = 0; j < C; ++j) x[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qop[j][i], x[j][h], 0, 0, 0);
+                for (int j = 0; j < C; ++j) x[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[j].op[i], x[j][h], 0, 0, 0);
             }
-            const uint32_t kp[4] = {tile[h].kp.x, tile[h].kp.y, tile[h].kp.z, tile[h].kp.w};
-            uint32_t vp[4] = {tile[h].vp.x, tile[h].vp.y, tile[h].vp.z, tile[h].vp.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float sk = half_bits_to_float((uint16_t)kp[e]);
-                float zk = half_bits_to_float((uint16_t)(kp[e] >> 16));
-                // a value row that is not finite: a score that is not, for the queries that see it
-                const bool bad = (vp[e] & 0x7C00u) == 0x7C00u || (vp[e] & 0x7C000000u) == 0x7C000000u;
-                if (bad) zk = NAN;
-                sv[h][e] = bad ? 0.0f : half_bits_to_float((uint16_t)vp[e]);
-                zv[h][e] = bad ? 0.0f : half_bits_to_float((uint16_t)(vp[e] >> 16));
+                const uint32_t kw = now[h].kp[e], vw = now[h].vp[e];
+                const f16x2 kp = __builtin_bit_cast(f16x2, kw), v = __builtin_bit_cast(f16x2, vw);
+                // a value row that is not finite makes the score NaN, for the queries that see it
+                const float bad = __builtin_fmaf((float)v[0], 0.0f, __builtin_fmaf((float)v[1], 0.0f, 0.0f));
+                vp[h][e] = __builtin_elementwise_max(v, (f16x2)(_Float16)-65504.0f);    // and its weight 0 stays 0
 #pragma unroll
-                for (int j = 0; j < C; ++j) x[j][h][e] = __builtin_fmaf(x[j][h][e], sk, zk * of_minimum[j]);
+                for (int j = 0; j < C; ++j)
+                    x[j][h][e] = __builtin_fmaf(x[j][h][e], (float)kp[0], __builtin_fmaf((float)kp[1], q[j].of_minimum, bad));
             }
         }
-        if (t + kStep > low || !tile[0].there || !tile[1].there) {
+        if (t + kStep > low || !all) {
 #pragma unroll
-            for (int j = 0; j < C; ++j)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int e = 0; e < 4; ++e) {
+                    const int token = t + 16 * h + 4 * g + e;
+                    if (!there[h] || token >= end) vp[h][e] = f16x2{};                  // whatever memory holds there
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!tile[h].there || t + 16 * h + 4 * g + e >= limit[j]) x[j][h][e] = -INFINITY;
+                    for (int j = 0; j < C; ++j)
+                        if (!there[h] || token >= limit[j]) x[j][h][e] = -INFINITY;
+                }
         }
-        float top[C], most = 0.0f;
+        float top[C];
         bool moves = false;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -231,13 +297,14 @@ __global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top[j] = fmaxf(top[j], x[j][h][e]);
-            top[j] = quads_max(top[j]) * to_score[j];
+            top[j] *= q[j].to_score;
             moves = moves || top[j] > m[j] + kSlack;
         }
+        // the largest scale, and minimum, of which only the scale is used
+        f16x2 both = __builtin_elementwise_max(vp[0][0], vp[0][1]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) most = fmaxf(most, sv[h][e]);
+        for (int i = 2; i < 8; ++i) both = __builtin_elementwise_max(both, vp[i / 4][i % 4]);
+        const float most = (float)both[0];
         moves = moves || most > unit;
         if (__any(moves)) {
             const float old = unit;
@@ -245,34 +312,46 @@ __global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
             per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                const float to = fmaxf(m[j], top[j]), down = exp2f(m[j] - to);
+                const float to = fmaxf(m[j], quads_max(top[j])), down = __builtin_amdgcn_exp2f(m[j] - to);
                 m[j] = to;
                 l[j] *= down;
                 zs[j] *= down;
+                ws[j] *= down * (old * per_unit);
 #pragma unroll
                 for (int i = 0; i < VT; ++i) acc[j][i] *= down * (old * per_unit);
             }
         }
         f16x8 p[C];
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
+        for (int h = 0; h < 2; ++h) {
+            float sv[4], middle[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int e = 0; e < 4; ++e) {
+                sv[e] = (float)vp[h][e][0] * per_unit;
+                middle[e] = __builtin_fmaf((float)vp[h][e][0], 7.5f, (float)vp[h][e][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
                 f32x4 w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][h][e], to_score[j], -m[j]));
+                    const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][h][e], q[j].to_score, -m[j]));
                     l[j] += pe;
-                    zs[j] = __builtin_fmaf(pe, zv[h][e], zs[j]);
-                    w[e] = pe * (sv[h][e] * per_unit);
+                    zs[j] = __builtin_fmaf(pe, middle[e], zs[j]);
+                    w[e] = pe * sv[e];
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[j][4 * h + e] = (_Float16)w[e];
+                for (int e = 0; e < 4; e += 2) {
+                    const f16x2 pair = __builtin_convertvector((f32x2{w[e], w[e + 1]}), f16x2);
+                    ws[j] = __builtin_amdgcn_fdot2(pair, (f16x2)(_Float16)1.0f, ws[j], false);
+                    p[j][4 * h + e] = pair[0];
+                    p[j][4 * h + e + 1] = pair[1];
+                }
             }
         }
 #pragma unroll
         for (int h = 0; h < D / 64; ++h) {
-            const uint32_t a0 = tile[0].v[2 * h], a1 = tile[0].v[2 * h + 1], b0 = tile[1].v[2 * h], b1 = tile[1].v[2 * h + 1];
+            const uint32_t a0 = now[0].v[2 * h], a1 = now[0].v[2 * h + 1], b0 = now[1].v[2 * h], b1 = now[1].v[2 * h + 1];
             const f16x8 v[4] = {value_operand<0>(a0, a1, b0, b1), value_operand<1>(a0, a1, b0, b1),
                                 value_operand<2>(a0, a1, b0, b1), value_operand<3>(a0, a1, b0, b1)};
 #pragma unroll
@@ -283,80 +362,44 @@ __global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
         }
     }
 
-    // The lane's column and its D / 4 channels (D / 4) g .., not yet divided by the weights' sum.
+    // The lane's column and its D / 4 channels (D / 4) g .., not yet divided by the weights' sum; joined over the waves.
+    __shared__ float shared_o[WT][Cols][D + 4];
+    __shared__ float shared_m[WT][Cols], shared_l[WT][Cols];
     const float of_unit = unit * 0x1p24f;
-    float out[C][D / 4];
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        l[j] = quads_sum(l[j]);
-        zs[j] = quads_sum(zs[j]);
+        const int col = 16 * j + r;
+        const float rest = quads_sum(__builtin_fmaf(-7.5f * unit, ws[j], zs[j])), sum = quads_sum(l[j]);
+        float out[D / 4];
 #pragma unroll
         for (int i = 0; i < VT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                out[j][e * VT + i] = __builtin_fmaf(acc[j][i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), zs[j]);
+            for (int e = 0; e < 4; ++e) out[e * VT + i] = __builtin_fmaf(acc[j][i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), rest);
+        if (col0 + col < cols) {
+#pragma unroll
+            for (int e = 0; e < D / 4; e += 4)
+                *reinterpret_cast<f32x4*>(&shared_o[wave][col][g * (D / 4) + e]) = f32x4{out[e], out[e + 1], out[e + 2], out[e + 3]};
+        }
+        if (g == 0) {
+            shared_m[wave][col] = m[j];
+            shared_l[wave][col] = sum;
+        }
     }
-
-    // rows of the partial results and of the output
-    auto store = [&](int col, int channel, auto& values, float mx, float sum, bool first) {
-        constexpr int n = sizeof(values) / sizeof(float);
-        const int qi = col / a.group, h = head * a.group + col % a.group;
-        if (a.splits > 1) {
-            const int64_t row = ((int64_t)split * a.tokens + s.q0 + qi) * (a.c.heads * a.group) + h;
+    __syncthreads();
+    for (int i = threadIdx.x; i < Cols * (D / 4); i += 256) {
+        const int col = i / (D / 4), ch = 4 * (i % (D / 4));
+        if (col0 + col >= cols) break;
+        float mx = shared_m[0][col], sum = 0.0f, o[4] = {};
 #pragma unroll
-            for (int e = 0; e < n; e += 4)
-                *reinterpret_cast<f32x4*>(a.part_o + row * D + channel + e) = f32x4{values[e], values[e + 1], values[e + 2], values[e + 3]};
-            if (first) {
-                a.part_m[row] = mx;
-                a.part_l[row] = sum;
-            }
-        } else {
-            const float by = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees nothing is 0
-            T* o = static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + h * a.o_head + channel;
-            typedef T half4 __attribute__((ext_vector_type(4)));
+        for (int w = 1; w < WT; ++w) mx = fmaxf(mx, shared_m[w][col]);
 #pragma unroll
-            for (int e = 0; e < n; e += 4)
-                *reinterpret_cast<half4*>(o + e) = __builtin_convertvector(
-                    (f32x4{values[e] * by, values[e + 1] * by, values[e + 2] * by, values[e + 3] * by}), half4);
+        for (int w = 0; w < WT; ++w) {
+            const float by = __builtin_amdgcn_exp2f(shared_m[w][col] - mx);
+            sum = __builtin_fmaf(shared_l[w][col], by, sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(shared_o[w][col][ch + e], by, o[e]);
         }
-    };
-    if constexpr (WT == 1) {
-#pragma unroll
-        for (int j = 0; j < C; ++j)
-            if (col0 + 16 * j + r < cols) store(col0 + 16 * j + r, g * (D / 4), out[j], m[j], l[j], g == 0);
-    } else {
-        __shared__ float shared_o[WT][WaveCols][D + 4];
-        __shared__ float shared_m[WT][WaveCols], shared_l[WT][WaveCols];
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            const int col = 16 * j + r;
-            if (col0 + col < cols) {
-#pragma unroll
-                for (int e = 0; e < D / 4; e += 4)
-                    *reinterpret_cast<f32x4*>(&shared_o[wave][col][g * (D / 4) + e]) =
-                        f32x4{out[j][e], out[j][e + 1], out[j][e + 2], out[j][e + 3]};
-            }
-            if (g == 0) {
-                shared_m[wave][col] = m[j];
-                shared_l[wave][col] = l[j];
-            }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < WaveCols * (D / 4); i += 256) {
-            const int col = i / (D / 4), ch = 4 * (i % (D / 4));
-            if (col0 + col >= cols) break;
-            float mx = shared_m[0][col], sum = 0.0f, o[4] = {};
-#pragma unroll
-            for (int w = 1; w < WT; ++w) mx = fmaxf(mx, shared_m[w][col]);
-#pragma unroll
-            for (int w = 0; w < WT; ++w) {
-                const float by = exp2f(shared_m[w][col] - mx);
-                sum = __builtin_fmaf(shared_l[w][col], by, sum);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(shared_o[w][col][ch + e], by, o[e]);
-            }
-            store(col0 + col, ch, o, mx, sum, ch == 0);
-        }
+        store_result<T, D, 4>(a, s, head, split, col0 + col, ch, o, mx, sum, ch == 0);
     }
 }
 
@@ -397,25 +440,20 @@ __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
 // ---------------------------------------------------------------- host side --
 struct Plan4 {
     int columns;                        // of a workgroup
-    int waves_on_tokens;
     int blocks, splits, chunk;
 };
 
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
-    p.waves_on_tokens = cols <= 16 ? 4 : 1;
-    p.columns = cols <= 16 ? 16 : 128;
+    p.columns = cols <= 16 ? 16 : 32;
     p.blocks = (int)((cols + p.columns - 1) / p.columns);
     const int64_t units = (int64_t)sequences * heads * p.blocks, least = 4 * kStep;
-    int64_t splits = 1;
-    if (p.waves_on_tokens > 1) {
-        splits = (1024 + units - 1) / units;
-        splits = splits > kMostSplits ? kMostSplits : splits;
-        const int64_t room = (max_kv + least - 1) / least;
-        splits = splits > room ? room : splits;
-        if (splits < 1) splits = 1;
-    }
+    int64_t splits = (1024 + units - 1) / units;
+    splits = splits > kMostSplits ? kMostSplits : splits;
+    const int64_t room = (max_kv + least - 1) / least;
+    splits = splits > room ? room : splits;
+    if (splits < 1) splits = 1;
     const int64_t chunk = ((max_kv + splits - 1) / splits + least - 1) / least * least;
     p.chunk = (int)(chunk < least ? least : chunk > (INT32_MAX / least) * least ? (INT32_MAX / least) * least : chunk);
     p.splits = splits == 1 ? 1 : (int)((max_kv + p.chunk - 1) / p.chunk);
@@ -471,10 +509,8 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
         using T = decltype(z);
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            if (p.waves_on_tokens > 1)
-                hipLaunchKernelGGL((attention4_kernel<T, D, 1, 4>), dim3((unsigned)grid), dim3(256), 0, stream, a);
-            else
-                hipLaunchKernelGGL((attention4_kernel<T, D, 2, 1>), dim3((unsigned)grid), dim3(256), 0, stream, a);
+            if (p.columns == 16) hipLaunchKernelGGL((attention4_kernel<T, D, 1>), dim3((unsigned)grid), dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((attention4_kernel<T, D, 2>), dim3((unsigned)grid), dim3(256), 0, stream, a);
             if (p.splits > 1) hipLaunchKernelGGL((attention4_join_kernel<T, D>), dim3((unsigned)joins), dim3(256), 0, stream, a);
             return mq_host::launch_status();
         };
