@@ -31,7 +31,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kStep = 32;               // tokens that a wave takes at a time
 constexpr int kMostSplits = 64;         // of a sequence's tokens
 constexpr float kLowest = -1e30f;       // below every score: running maximum of none
 constexpr float kLog2e = 1.4426950408889634f;
@@ -96,9 +95,9 @@ __device__ __forceinline__ f16x8 value_operand(uint32_t a0, uint32_t a1, uint32_
     return __builtin_bit_cast(f16x8, u32x4{(a0 >> shift) & mask, (a1 >> shift) & mask, (b0 >> shift) & mask, (b1 >> shift) & mask});
 }
 
-// Operands and scales of 16 columns of queries: fp16, each column scaled by a power of two (its largest
-// value near 2^8, so that neither type's range matters), channels of the codes that come 16 times too
-// large divided by 16.  A lane has the channels (D / 4) g .. of its column.
+// Operands and scales of 16 columns of queries: fp16, scaled by a power of two (the largest value near
+// 2^8, so that neither type's range matters), channels of the codes that come 16 times too large divided
+// by 16.  A lane has the channels (D / 4) g .. of its column.
 template <int D>
 struct Queries {
     f16x8 op[D / 32];
@@ -120,6 +119,8 @@ struct Queries {
         }
         sum = quads_sum(sum);
         amax = quads_max(amax);
+#pragma unroll
+        for (int i = 1; i < 16; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
         const int up = amax > 0.0f && amax < INFINITY ? 8 - ilogbf(amax) : 0;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -160,233 +161,321 @@ __device__ __forceinline__ void store_result(const Attn4Args& a, const Sequence&
 }
 
 // --------------------------------------------------------------------------
-// Few columns: codes go from memory to registers and into the products.
+// Few columns (at most RP): codes go from memory to registers and into the products.
 // --------------------------------------------------------------------------
-// What a wave loads for 16 tokens: lane (r, g) has token r's key channels
-// (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r .. and parameters.
+// A wave takes 64 tokens at a time, four tiles of 16.  S = Q K^T with the queries
+// repeated in the 16 rows (row i holds column i % RP), so each tile's scores are
+// in every group of RP rows, and the lanes keep of tile i those that they alone
+// keep: with RP = 4 a lane ends up with one token (16 g + r) and all the columns
+// in its registers.  A row of 16 columns for four queries would leave three lanes
+// of four with nothing (the work on scores, parameters and weights was half of
+// the kernel: a batch of 64 contexts of up to 8191 tokens 70 us, this XX).
+// The weights cross to the lanes of the second product, O^T = V^T P^T, through LDS.
+//
+// Weights are held as multiples of `unit` (at least every scale), w = p sv / unit,
+// rounded to fp16; of the products 7.5 sum(w) is taken off again and made up for in
+// fp32: codes about their middle, so that the rounding of w counts against values
+// about their middle.
+//
+// What a wave loads for 64 tokens: lane (r, g), tile i: token r's key channels
+// (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r ..; and the
+// parameters of the tokens whose scores it keeps.
+constexpr int kStep = 64;               // tokens that a wave takes at a time
 template <int D>
-struct Tile4 {
-    uint32_t k[D / 32], v[D / 32];
-    u32x4 kp, vp;
+struct Keys4 {
+    uint32_t k[4][D / 32];
 };
-// The pages of a step's two tiles (the last token's where a tile is past the end: its page is there to be
-// read); negative: outside the cache.
+template <int D>
+struct Values4 {
+    uint32_t v[4][D / 32];
+};
+// The pages of a step's tiles (the last token's where a tile is past the end: its
+// page is there to be read); negative: outside the cache.
 struct Pages {
-    int of[2];
+    int of[4];
+    __device__ __forceinline__ bool all() const { return (of[0] | of[1] | of[2] | of[3]) >= 0; }
 };
 __device__ __forceinline__ Pages find_pages(const Attn4Args& a, int b, int t, int last) {
     Pages p;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 4; ++h) {
         const int page = a.table[(int64_t)b * a.table_pages + (min(t + 16 * h, last) >> a.c.page_bits)];
         p.of[h] = __builtin_amdgcn_readfirstlane((uint32_t)page < (uint32_t)a.c.pages ? page : -1);
     }
     return p;
 }
-template <int D>
-__device__ __forceinline__ void load_tile(Tile4<D>& x, const Attn4Args& a, int head, int page, int t, int lane) {
-    const int r = lane & 15, g = lane >> 4;
-    const int64_t row = (((int64_t)max(page, 0) * a.c.heads + head) << a.c.page_bits) + (t & ((1 << a.c.page_bits) - 1));
-    const uint8_t* k = a.c.k + row * (D / 2);
-    const uint8_t* v = a.c.v + row * (D / 2);
-    __builtin_memcpy(x.k, __builtin_assume_aligned(k + (uint32_t)(r * (D / 2) + g * (D / 8)), D / 8), D / 8);
-    __builtin_memcpy(x.v, __builtin_assume_aligned(v + (uint32_t)(g * (2 * D) + r * (D / 8)), D / 8), D / 8);
-    x.kp = *reinterpret_cast<const u32x4*>(a.c.kp + row + (uint32_t)(4 * g));
-    x.vp = *reinterpret_cast<const u32x4*>(a.c.vp + row + (uint32_t)(4 * g));
+// row of the cache's first token of a tile at token t
+__device__ __forceinline__ int64_t tile_row(const Attn4Args& a, int head, int page, int t) {
+    return (((int64_t)max(page, 0) * a.c.heads + head) << a.c.page_bits) + (t & ((1 << a.c.page_bits) - 1));
 }
 
-// Every wave takes all the columns (16 C) and a share of the tokens; the step after
-// the one in hand is loaded meanwhile.  The parameters stay fp16 and are widened
-// inside mixed multiply-adds.  Weights w = p sv (in units of `unit`, at least every
-// sv) are rounded to fp16 for the second product, of which 7.5 sum(w) is taken off
-// again: codes about their middle, so that the rounding of w counts against values
-// about their middle.
-template <typename T, int D, int C>
-__global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
-    constexpr int KK = D / 32, VT = D / 16, WT = 4, Cols = 16 * C;
+template <int RP>
+struct Shape4 {
+    static constexpr int kTokens = RP / 4;          // of a step, that a lane keeps
+    static constexpr int kTiles = 16 / RP;          // tiles that share the lanes
+};
+template <typename T, int D, int RP, int R>
+__global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
+    constexpr int KK = D / 32, VT = D / 16, WT = 4, NT = Shape4<RP>::kTokens, Row = kStep + 8;
+    // the waves' weights, and when the tokens are through, their results
+    union Shared {
+        _Float16 p[WT][RP][Row];
+        float o[WT][RP][D + 4];
+    };
+    __shared__ __attribute__((aligned(16))) Shared shared;
+    __shared__ float shared_m[WT][16], shared_l[WT][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int blocks = (a.max_q * a.group + Cols - 1) / Cols;
+    const int blocks = (a.max_q * a.group + RP - 1) / RP;
+    // splits last: later ones are there for the longer sequences only, and as many for every XCD
     int u = blockIdx.x;
-    const int split = u % a.splits;
-    u /= a.splits;
-    const int col0 = u % blocks * Cols;
+    const int head = u % a.c.heads;
+    u /= a.c.heads;
+    const int col0 = u % blocks * RP;
     u /= blocks;
-    const int head = u % a.c.heads, b = u / a.c.heads;
+    const int b = u % a.sequences, split = u / a.sequences;
     const Sequence s = sequence(a, b);
     const int cols = s.nq * a.group;
     if (col0 >= cols) return;
-    const int low = visible(a, s, col0 / a.group), high = visible(a, s, (min(col0 + Cols, cols) - 1) / a.group);
+    const int low = visible(a, s, col0 / a.group), high = visible(a, s, (min(col0 + RP, cols) - 1) / a.group);
     const int64_t first = (int64_t)split * a.chunk;
     if (a.splits > 1 && first >= high) return;
     const int begin = (int)first + wave * kStep, end = (int)min((int64_t)high, first + a.chunk);
     constexpr int stride = kStep * WT;
+    // the lane's scores: columns (within the block) mine + e, tokens of tile base + kTiles * i, i < NT
+    const int mine = RP == 4 ? 0 : RP == 8 ? 4 * (g & 1) : 4 * g, base = RP == 4 ? g : RP == 8 ? g >> 1 : 0;
 
-    Tile4<D> tile[2];
+    Keys4<D> keys;
+    Values4<D> values;
+    uint32_t kp[NT], vp[NT];
     Pages pages{}, next{};
+    auto load_keys = [&](const Pages& p, int t) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const uint8_t* k = a.c.k + tile_row(a, head, p.of[h], t + 16 * h) * (D / 2);
+            __builtin_memcpy(keys.k[h], __builtin_assume_aligned(k + (uint32_t)(r * (D / 2) + g * (D / 8)), D / 8), D / 8);
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            int64_t row = tile_row(a, head, p.of[i * Shape4<RP>::kTiles], t + 16 * i * Shape4<RP>::kTiles);
+#pragma unroll
+            for (int h = 1; h < Shape4<RP>::kTiles; ++h)
+                if (base == h) row = tile_row(a, head, p.of[i * Shape4<RP>::kTiles + h], t + 16 * (i * Shape4<RP>::kTiles + h));
+            kp[i] = a.c.kp[row + r];
+            vp[i] = a.c.vp[row + r];
+        }
+    };
+    auto load_values = [&](const Pages& p, int t) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const uint8_t* v = a.c.v + tile_row(a, head, p.of[h], t + 16 * h) * (D / 2);
+            __builtin_memcpy(values.v[h], __builtin_assume_aligned(v + (uint32_t)(g * (2 * D) + r * (D / 8)), D / 8), D / 8);
+        }
+    };
     if (begin < end) {
         pages = find_pages(a, b, begin, end - 1);
+        load_keys(pages, begin);
+        load_values(pages, begin);
         next = find_pages(a, b, begin + stride, end - 1);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) load_tile<D>(tile[h], a, head, pages.of[h], begin + 16 * h, lane);
     }
-    Queries<D> q[C];
-    int limit[C];
+    f16x8 q[KK];
+    float of_minimum[R], to_score;
+    int limit[R];
+    {
+        const int col = min(col0 + r % RP, cols - 1), qi = col / a.group;
+        Queries<D> mq;
+        mq.load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
+        const int seen = visible(a, s, qi);
+        to_score = mq.to_score;
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        const int col = min(col0 + 16 * j + r, cols - 1), qi = col / a.group;
-        limit[j] = visible(a, s, qi);
-        q[j].load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
+        for (int i = 0; i < KK; ++i) q[i] = mq.op[i];
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
+            of_minimum[e] = __shfl(mq.of_minimum, mine + e);
+            limit[e] = __shfl(seen, mine + e);
+        }
     }
 
-    f32x4 acc[C][VT] = {};
-    float m[C], l[C] = {}, zs[C] = {}, ws[C] = {};
+    f32x4 acc[VT] = {};
+    float m[R], l[R] = {}, rest[R] = {};                    // rest: what the codes about their middle leave out
     float unit = 0.0f, per_unit = 0.0f;
 #pragma unroll
-    for (int j = 0; j < C; ++j) m[j] = kLowest;
+    for (int e = 0; e < R; ++e) m[e] = kLowest;
+    // over the lanes that keep the same columns
+    auto all_max = [&](float v) {
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1)
+            if (!(RP == 8 && i == 16) && !(RP == 16 && i >= 16)) v = fmaxf(v, __shfl_xor(v, i));
+        return v;
+    };
+    auto all_sum = [&](float v) {
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1)
+            if (!(RP == 8 && i == 16) && !(RP == 16 && i >= 16)) v += __shfl_xor(v, i);
+        return v;
+    };
 
     for (int t = begin; t < end; t += stride) {
-        const Tile4<D> now[2] = {tile[0], tile[1]};
-        const bool all = pages.of[0] >= 0 && pages.of[1] >= 0, there[2] = {pages.of[0] >= 0, pages.of[1] >= 0};
+        const bool more = t + stride < end;
+        const Pages now = pages;
         pages = next;
-        if (t + stride < end) {
+        float x[NT][R];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) load_tile<D>(tile[h], a, head, pages.of[h], t + stride + 16 * h, lane);
-            next = find_pages(a, b, t + 2 * stride, end - 1);
-        }
-        f32x4 x[C][2] = {};
-        f16x2 vp[2][4];                                     // scale, minimum; finite
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < Shape4<RP>::kTiles; ++h) {
+                const int tile = i * Shape4<RP>::kTiles + h;
+                f32x4 y = {};
 #pragma unroll
-            for (int i = 0; i < KK; ++i) {
-                const f16x8 k = key_operand(now[h].k[i]);
+                for (int c = 0; c < KK; ++c) y = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[c], key_operand(keys.k[tile][c]), y, 0, 0, 0);
 #pragma unroll
-                for (int j = 0; j < C; ++j) x[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[j].op[i], x[j][h], 0, 0, 0);
+                for (int e = 0; e < R; ++e) x[i][e] = h == 0 || base == h ? y[e] : x[i][e];
+                if (tile % 2) __builtin_amdgcn_sched_barrier(0);    // two tiles' operands at a time in registers
             }
+        float sv[NT], middle[NT];
+        uint32_t vps[NT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t kw = now[h].kp[e], vw = now[h].vp[e];
-                const f16x2 kp = __builtin_bit_cast(f16x2, kw), v = __builtin_bit_cast(f16x2, vw);
-                // a value row that is not finite makes the score NaN, for the queries that see it
-                const float bad = __builtin_fmaf((float)v[0], 0.0f, __builtin_fmaf((float)v[1], 0.0f, 0.0f));
-                vp[h][e] = __builtin_elementwise_max(v, (f16x2)(_Float16)-65504.0f);    // and its weight 0 stays 0
+        for (int i = 0; i < NT; ++i) {
+            const f16x2 k = __builtin_bit_cast(f16x2, kp[i]), v = __builtin_bit_cast(f16x2, vp[i]);
+            // a value row that is not finite (both its parameters are NaN) makes the score NaN, for the
+            // queries that see it, and its weight 0 stays 0
+            const float bad = __builtin_fmaf((float)v[0], 0.0f, 0.0f);
+            vps[i] = v[0] == v[0] ? vp[i] : 0u;
 #pragma unroll
-                for (int j = 0; j < C; ++j)
-                    x[j][h][e] = __builtin_fmaf(x[j][h][e], (float)kp[0], __builtin_fmaf((float)kp[1], q[j].of_minimum, bad));
+            for (int e = 0; e < R; ++e) x[i][e] = __builtin_fmaf(x[i][e], (float)k[0], __builtin_fmaf((float)k[1], of_minimum[e], bad));
+        }
+        if (more) load_keys(pages, t + stride);
+        if (t + kStep > low || !now.all()) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                int page = now.of[i * Shape4<RP>::kTiles];
+#pragma unroll
+                for (int h = 1; h < Shape4<RP>::kTiles; ++h) page = base == h ? now.of[i * Shape4<RP>::kTiles + h] : page;
+                const int token = t + 16 * (i * Shape4<RP>::kTiles + base) + r;
+                if (page < 0 || token >= end) vps[i] = 0u;      // whatever memory holds there
+#pragma unroll
+                for (int e = 0; e < R; ++e)
+                    if (page < 0 || token >= limit[e]) x[i][e] = -INFINITY;
             }
         }
-        if (t + kStep > low || !all) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int token = t + 16 * h + 4 * g + e;
-                    if (!there[h] || token >= end) vp[h][e] = f16x2{};                  // whatever memory holds there
-#pragma unroll
-                    for (int j = 0; j < C; ++j)
-                        if (!there[h] || token >= limit[j]) x[j][h][e] = -INFINITY;
-                }
-        }
-        float top[C];
+        float most = 0.0f;
         bool moves = false;
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            top[j] = -INFINITY;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top[j] = fmaxf(top[j], x[j][h][e]);
-            top[j] *= q[j].to_score;
-            moves = moves || top[j] > m[j] + kSlack;
+        for (int i = 0; i < NT; ++i) {
+            const f16x2 v = __builtin_bit_cast(f16x2, vps[i]);
+            sv[i] = (float)v[0];
+            middle[i] = __builtin_fmaf((float)v[0], 7.5f, (float)v[1]);
+            most = fmaxf(most, sv[i]);
         }
-        // the largest scale, and minimum, of which only the scale is used
-        f16x2 both = __builtin_elementwise_max(vp[0][0], vp[0][1]);
+        float top[R];
 #pragma unroll
-        for (int i = 2; i < 8; ++i) both = __builtin_elementwise_max(both, vp[i / 4][i % 4]);
-        const float most = (float)both[0];
+        for (int e = 0; e < R; ++e) {
+            top[e] = x[0][e];
+#pragma unroll
+            for (int i = 1; i < NT; ++i) top[e] = fmaxf(top[e], x[i][e]);
+            top[e] *= to_score;
+            moves = moves || top[e] > m[e] + kSlack;
+        }
         moves = moves || most > unit;
         if (__any(moves)) {
             const float old = unit;
-            unit = fmaxf(unit, 2.0f * quads_max(most));
+#pragma unroll
+            for (int i = 1; i < 64; i <<= 1) most = fmaxf(most, __shfl_xor(most, i));
+            unit = fmaxf(unit, 2.0f * most);
             per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
+            float down[R];
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                const float to = fmaxf(m[j], quads_max(top[j])), down = __builtin_amdgcn_exp2f(m[j] - to);
-                m[j] = to;
-                l[j] *= down;
-                zs[j] *= down;
-                ws[j] *= down * (old * per_unit);
+            for (int e = 0; e < R; ++e) {
+                const float to = fmaxf(m[e], all_max(top[e]));
+                down[e] = __builtin_amdgcn_exp2f(m[e] - to);
+                m[e] = to;
+                l[e] *= down[e];
+                rest[e] *= down[e];
+                down[e] *= old * per_unit;
+            }
+            // the factor of the second product's column r: register r % 4 of a lane that keeps it
+            float by = 1.0f;
 #pragma unroll
-                for (int i = 0; i < VT; ++i) acc[j][i] *= down * (old * per_unit);
+            for (int e = 0; e < R; ++e) {
+                const float v = __shfl(down[e], RP == 4 ? 0 : RP == 8 ? r % 8 / 4 * 16 : r / 4 * 16);
+                by = r % 4 == e ? v : by;
+            }
+#pragma unroll
+            for (int i = 0; i < VT; ++i) acc[i] *= by;
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int tile = i * Shape4<RP>::kTiles + base;
+            // tokens of 32 in the order of the second product's operand: 4 g .. + 3 of one tile, then of the other
+            const int at = tile / 2 * 32 + r / 4 * 8 + tile % 2 * 4 + r % 4;
+            const float by = sv[i] * per_unit, off = -7.5f * unit;
+#pragma unroll
+            for (int e = 0; e < R; ++e) {
+                const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], to_score, -m[e]));
+                l[e] += pe;
+                const _Float16 w = (_Float16)(pe * by);
+                rest[e] = __builtin_fmaf((float)w, off, __builtin_fmaf(pe, middle[i], rest[e]));
+                shared.p[wave][mine + e][at] = w;
             }
         }
-        f16x8 p[C];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own, read by its other lanes
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float sv[4], middle[4];
+            const f16x8 p = *reinterpret_cast<const f16x8*>(&shared.p[wave][r % RP][32 * h + 8 * g]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sv[e] = (float)vp[h][e][0] * per_unit;
-                middle[e] = __builtin_fmaf((float)vp[h][e][0], 7.5f, (float)vp[h][e][1]);
-            }
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                f32x4 w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][h][e], q[j].to_score, -m[j]));
-                    l[j] += pe;
-                    zs[j] = __builtin_fmaf(pe, middle[e], zs[j]);
-                    w[e] = pe * sv[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const f16x2 pair = __builtin_convertvector((f32x2{w[e], w[e + 1]}), f16x2);
-                    ws[j] = __builtin_amdgcn_fdot2(pair, (f16x2)(_Float16)1.0f, ws[j], false);
-                    p[j][4 * h + e] = pair[0];
-                    p[j][4 * h + e + 1] = pair[1];
-                }
+            for (int w = 0; w < D / 64; ++w) {
+                const uint32_t a0 = values.v[2 * h][2 * w], a1 = values.v[2 * h][2 * w + 1];
+                const uint32_t b0 = values.v[2 * h + 1][2 * w], b1 = values.v[2 * h + 1][2 * w + 1];
+                acc[4 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<0>(a0, a1, b0, b1), p, acc[4 * w], 0, 0, 0);
+                acc[4 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<1>(a0, a1, b0, b1), p, acc[4 * w + 1], 0, 0, 0);
+                acc[4 * w + 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<2>(a0, a1, b0, b1), p, acc[4 * w + 2], 0, 0, 0);
+                acc[4 * w + 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<3>(a0, a1, b0, b1), p, acc[4 * w + 3], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-#pragma unroll
-        for (int h = 0; h < D / 64; ++h) {
-            const uint32_t a0 = now[0].v[2 * h], a1 = now[0].v[2 * h + 1], b0 = now[1].v[2 * h], b1 = now[1].v[2 * h + 1];
-            const f16x8 v[4] = {value_operand<0>(a0, a1, b0, b1), value_operand<1>(a0, a1, b0, b1),
-                                value_operand<2>(a0, a1, b0, b1), value_operand<3>(a0, a1, b0, b1)};
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < C; ++j)
-                    acc[j][4 * h + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[i], p[j], acc[j][4 * h + i], 0, 0, 0);
+        if (more) {
+            load_values(pages, t + stride);
+            next = find_pages(a, b, t + 2 * stride, end - 1);
         }
+        asm volatile("" ::: "memory");                      // the weights are read before the next are written
     }
 
-    // The lane's column and its D / 4 channels (D / 4) g .., not yet divided by the weights' sum; joined over the waves.
-    __shared__ float shared_o[WT][Cols][D + 4];
-    __shared__ float shared_m[WT][Cols], shared_l[WT][Cols];
-    const float of_unit = unit * 0x1p24f;
+    // Column r's D / 4 channels (D / 4) g .., not yet divided by the weights' sum; joined over the waves.
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        const int col = 16 * j + r;
-        const float rest = quads_sum(__builtin_fmaf(-7.5f * unit, ws[j], zs[j])), sum = quads_sum(l[j]);
-        float out[D / 4];
+    for (int e = 0; e < R; ++e) {
+        l[e] = all_sum(l[e]);
+        rest[e] = all_sum(rest[e]);
+    }
+    float add = 0.0f;
 #pragma unroll
-        for (int i = 0; i < VT; ++i)
+    for (int e = 0; e < R; ++e) {
+        const float v = __shfl(rest[e], RP == 4 ? 0 : RP == 8 ? r % 8 / 4 * 16 : r / 4 * 16);
+        add = r % 4 == e ? v : add;
+    }
+    if (r == 0 && (RP == 16 || g < RP / 4)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e * VT + i] = __builtin_fmaf(acc[j][i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), rest);
-        if (col0 + col < cols) {
-#pragma unroll
-            for (int e = 0; e < D / 4; e += 4)
-                *reinterpret_cast<f32x4*>(&shared_o[wave][col][g * (D / 4) + e]) = f32x4{out[e], out[e + 1], out[e + 2], out[e + 3]};
+        for (int e = 0; e < R; ++e) {
+            shared_m[wave][mine + e] = m[e];
+            shared_l[wave][mine + e] = l[e];
         }
-        if (g == 0) {
-            shared_m[wave][col] = m[j];
-            shared_l[wave][col] = sum;
+    }
+    const float of_unit = unit * 0x1p24f;
+    __syncthreads();                                        // every wave has read its last weights
+    if (r < RP && col0 + r < cols) {
+#pragma unroll
+        for (int c = 0; c < D / 4; c += 4) {
+            f32x4 out;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = (c + k) % VT, e = (c + k) / VT;
+                out[k] = __builtin_fmaf(acc[i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), add);
+            }
+            *reinterpret_cast<f32x4*>(&shared.o[wave][r][g * (D / 4) + c]) = out;
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < Cols * (D / 4); i += 256) {
+    for (int i = threadIdx.x; i < RP * (D / 4); i += 256) {
         const int col = i / (D / 4), ch = 4 * (i % (D / 4));
         if (col0 + col >= cols) break;
         float mx = shared_m[0][col], sum = 0.0f, o[4] = {};
@@ -397,44 +486,54 @@ __global__ __launch_bounds__(256) void attention4_kernel(Attn4Args a) {
             const float by = __builtin_amdgcn_exp2f(shared_m[w][col] - mx);
             sum = __builtin_fmaf(shared_l[w][col], by, sum);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(shared_o[w][col][ch + e], by, o[e]);
+            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(shared.o[w][col][ch + e], by, o[e]);
         }
         store_result<T, D, 4>(a, s, head, split, col0 + col, ch, o, mx, sum, ch == 0);
     }
 }
 
-// Joins the splits of a row, one wave a row: lane i weighs split i.
+// Joins the splits of a row, one workgroup a row: lane i weighs split i, and each
+// half (D = 64: quarter) of a wave adds up its share of the splits.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int heads = a.c.heads * a.group, head = (int)(u % heads), qi = (int)(u / heads % a.max_q);
-    const int64_t b = u / heads / a.max_q;
-    if (b >= a.sequences) return;
-    const Sequence s = sequence(a, (int)b);
+    constexpr int Lanes = D / 4, Shares = 256 / Lanes;
+    const int lane = threadIdx.x & 63, share = threadIdx.x / Lanes, at = threadIdx.x % Lanes;
+    const int heads = a.c.heads * a.group, head = blockIdx.x % heads, qi = blockIdx.x / heads % a.max_q;
+    const int b = blockIdx.x / heads / a.max_q;
+    const Sequence s = sequence(a, b);
     if (qi >= s.nq) return;
-    const int seen = visible(a, s, qi), active = seen > 0 ? (seen - 1) / a.chunk + 1 : 0;   // at most a.splits: chunk splits >= n
+    const int seen = visible(a, s, qi), active = seen > 0 ? min((seen - 1) / a.chunk + 1, a.splits) : 0;
     const int64_t row = (int64_t)(s.q0 + qi) * heads + head, step = (int64_t)a.tokens * heads;
-    const bool mine = lane < min(active, a.splits);
-    const float m = mine ? a.part_m[row + lane * step] : kLowest;
+    f32x4 o = {};
+    const float m = lane < active ? a.part_m[row + lane * step] : kLowest, l = lane < active ? a.part_l[row + lane * step] : 0.0f;
+    f32x4 ahead[2];                                         // the first two are loaded beside the weights
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        ahead[i] = share + i * Shares < active ? *reinterpret_cast<const f32x4*>(a.part_o + (row + (share + i * Shares) * step) * D + 4 * at) : f32x4{};
     float mx = m;
 #pragma unroll
     for (int i = 32; i >= 1; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
-    const float by = mine ? exp2f(m - mx) : 0.0f;
-    float sum = mine ? by * a.part_l[row + lane * step] : 0.0f;
+    const float by = lane < active ? __builtin_amdgcn_exp2f(m - mx) : 0.0f;
+    float sum = by * l;
 #pragma unroll
     for (int i = 32; i >= 1; i >>= 1) sum += __shfl_xor(sum, i);
-    constexpr int N = D / 64;
-    float o[N] = {};
-    for (int i = 0; i < min(active, a.splits); ++i) {
-        const float w = __shfl(by, i);
 #pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = __builtin_fmaf(a.part_o[(row + i * step) * D + lane * N + e], w, o[e]);
+    for (int i = 0; i < kMostSplits / Shares; ++i) {
+        if (i * Shares >= active) break;
+        const int split = share + i * Shares;
+        const float w = __shfl(by, split);                  // 0 from `active` on
+        const f32x4 v = i < 2 ? ahead[i] : split < active ? *reinterpret_cast<const f32x4*>(a.part_o + (row + split * step) * D + 4 * at) : f32x4{};
+        o += v * w;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T* out = static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + head * a.o_head + lane * N;
+    __shared__ f32x4 shared[Shares][Lanes];
+    shared[share][at] = o;
+    __syncthreads();
+    if (share > 0) return;
 #pragma unroll
-    for (int e = 0; e < N; ++e) out[e] = (T)(o[e] * inv);
+    for (int i = 1; i < Shares; ++i) o += shared[i][at];
+    typedef T half4 __attribute__((ext_vector_type(4)));
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;      // a row that sees nothing is 0
+    *reinterpret_cast<half4*>(static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + head * a.o_head + 4 * at) = __builtin_convertvector(o * inv, half4);
 }
 
 // ---------------------------------------------------------------- host side --
@@ -446,9 +545,9 @@ struct Plan4 {
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
-    p.columns = cols <= 16 ? 16 : 32;
+    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
     p.blocks = (int)((cols + p.columns - 1) / p.columns);
-    const int64_t units = (int64_t)sequences * heads * p.blocks, least = 4 * kStep;
+    const int64_t units = (int64_t)sequences * heads * p.blocks, least = kStep;
     int64_t splits = (1024 + units - 1) / units;
     splits = splits > kMostSplits ? kMostSplits : splits;
     const int64_t room = (max_kv + least - 1) / least;
@@ -503,14 +602,18 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
                       sequences, tokens, group, max_q, scale, causal != 0, p.splits, p.chunk, part,
                       part ? part + rows * cache->head_dim : nullptr, part ? part + rows * (cache->head_dim + 1) : nullptr};
     const int64_t grid = (int64_t)sequences * cache->heads * p.blocks * p.splits;
-    const int64_t joins = ((int64_t)sequences * max_q * cache->heads * group + 3) / 4;
+    const int64_t joins = (int64_t)sequences * max_q * cache->heads * group;
     if (grid > INT32_MAX || joins > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            if (p.columns == 16) hipLaunchKernelGGL((attention4_kernel<T, D, 1>), dim3((unsigned)grid), dim3(256), 0, stream, a);
-            else hipLaunchKernelGGL((attention4_kernel<T, D, 2>), dim3((unsigned)grid), dim3(256), 0, stream, a);
+            auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a); };
+            if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>);
+            else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>);
+            else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>);
+            else if (max_q * group > 1) few(attention4_kernel<T, D, 4, 2>);
+            else few(attention4_kernel<T, D, 4, 1>);
             if (p.splits > 1) hipLaunchKernelGGL((attention4_join_kernel<T, D>), dim3((unsigned)joins), dim3(256), 0, stream, a);
             return mq_host::launch_status();
         };
