@@ -31,7 +31,11 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kMostSplits = 64;         // of a sequence's tokens
+constexpr int kStep = 64;               // tokens that are taken at a time
+constexpr int kLeastSteps = 4;          // of a workgroup
+// What beginning and ending a unit takes, in steps of a workgroup (64 ragged contexts of up to 8191 tokens:
+// none counted 82.7 us, 4 68.6, 12 66.7, 24 69.0).
+constexpr int kUnitSteps = 12;
 constexpr float kLowest = -1e30f;       // below every score: running maximum of none
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;          // weights up to 2^kSlack before the running maximum moves
@@ -49,9 +53,13 @@ struct Attn4Args {
     int sequences, tokens, group, max_q;
     float scale;
     int causal;
-    int splits, chunk;                  // tokens of a split, a multiple of kStep
-    float *part_o, *part_m, *part_l;    // [split][token][head] (x D)
+    float *part_o, *part_m, *part_l;    // results of parts of a row's tokens: [place][column] (x D); null: whole rows only
+    int32_t* starts;                    // [sequence] first step of each among all, [sequences] steps of a workgroup
 };
+
+// The launch writes none of these arrays: reads by uniform indexes go through the scalar cache, beside the
+// vector loads in flight, which return in order.
+typedef __attribute__((address_space(4))) const int32_t const_int;
 
 // A sequence's queries and tokens.
 struct Sequence {
@@ -60,13 +68,14 @@ struct Sequence {
 __device__ __forceinline__ Sequence sequence(const Attn4Args& a, int b) {
     Sequence s;
     if (a.cu_q) {
-        s.q0 = min(max(a.cu_q[b], 0), a.tokens);
-        s.nq = min(max(min(a.cu_q[b + 1], a.tokens) - s.q0, 0), a.max_q);
+        const const_int* cu_q = (const const_int*)a.cu_q;
+        s.q0 = min(max(cu_q[b], 0), a.tokens);
+        s.nq = min(max(min(cu_q[b + 1], a.tokens) - s.q0, 0), a.max_q);
     } else {
         s.q0 = b;
         s.nq = 1;
     }
-    s.n = min(max(a.kv_lens[b], 0), a.max_kv);
+    s.n = min(max(((const const_int*)a.kv_lens)[b], 0), a.max_kv);
     return s;
 }
 // tokens that query qi sees: 0 .. limit - 1
@@ -134,30 +143,26 @@ struct Queries {
     }
 };
 
-// A result row (or part of one) of column col, not yet divided by the weights' sum: to the output, or
-// with splits to the partial results.
-template <typename T, int D, int N>
-__device__ __forceinline__ void store_result(const Attn4Args& a, const Sequence& s, int head, int split, int col, int channel,
-                                             const float (&values)[N], float mx, float sum, bool first) {
-    const int qi = col / a.group, h = head * a.group + col % a.group;
-    if (a.splits > 1) {
-        const int64_t row = ((int64_t)split * a.tokens + s.q0 + qi) * (a.c.heads * a.group) + h;
-#pragma unroll
-        for (int e = 0; e < N; e += 4)
-            *reinterpret_cast<f32x4*>(a.part_o + row * D + channel + e) = f32x4{values[e], values[e + 1], values[e + 2], values[e + 3]};
-        if (first) {
-            a.part_m[row] = mx;
-            a.part_l[row] = sum;
-        }
-    } else {
-        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;       // a row that sees nothing is 0
-        T* o = static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + h * a.o_head + channel;
-        typedef T half4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int e = 0; e < N; e += 4)
-            *reinterpret_cast<half4*>(o + e) = __builtin_convertvector(
-                (f32x4{values[e] * by, values[e + 1] * by, values[e + 2] * by, values[e + 3] * by}), half4);
-    }
+// Four channels of a column, divided by the sum of its weights, to the output.
+template <typename T>
+__device__ __forceinline__ void store_output(const Attn4Args& a, const Sequence& s, int head, int col, int channel, f32x4 o, float sum) {
+    typedef T half4 __attribute__((ext_vector_type(4)));
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;           // a row that sees nothing is 0
+    T* out = static_cast<T*>(a.o) + (s.q0 + col / a.group) * a.o_token + (head * a.group + col % a.group) * a.o_head + channel;
+    *reinterpret_cast<half4*>(out) = __builtin_convertvector(o * by, half4);
+}
+
+// Work of a launch: units (sequence, block of RP columns, key head) of as many steps as the sequence has
+// tokens, behind kUnitSteps that stand for the unit's own cost, one unit after the other.  Every workgroup
+// takes as many steps; its ends may lie inside units.
+struct Work4 {
+    int steps, units;
+    __device__ __forceinline__ int each() const { return steps > 0 ? steps + kUnitSteps : 0; }
+    __device__ __forceinline__ int all() const { return each() * units; }
+};
+template <int RP>
+__device__ __forceinline__ Work4 work4(const Attn4Args& a, const Sequence& s) {
+    return Work4{(s.n + kStep - 1) / kStep, (s.nq * a.group + RP - 1) / RP * a.c.heads};
 }
 
 // --------------------------------------------------------------------------
@@ -172,7 +177,7 @@ __device__ __forceinline__ void store_result(const Attn4Args& a, const Sequence&
 // the kernel: a batch of 64 contexts of up to 8191 tokens 70 us, this XX).
 // The weights cross to the lanes of the second product, O^T = V^T P^T, through LDS.
 //
-// Weights are held as multiples of `unit` (at least every scale), w = p sv / unit,
+// Weights are held as multiples of `scale` (at least every sv), w = p sv / scale,
 // rounded to fp16; of the products 7.5 sum(w) is taken off again and made up for in
 // fp32: codes about their middle, so that the rounding of w counts against values
 // about their middle.
@@ -180,7 +185,6 @@ __device__ __forceinline__ void store_result(const Attn4Args& a, const Sequence&
 // What a wave loads for 64 tokens: lane (r, g), tile i: token r's key channels
 // (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r ..; and the
 // parameters of the tokens whose scores it keeps.
-constexpr int kStep = 64;               // tokens that a wave takes at a time
 template <int D>
 struct Keys4 {
     uint32_t k[4][D / 32];
@@ -189,24 +193,23 @@ template <int D>
 struct Values4 {
     uint32_t v[4][D / 32];
 };
-// The pages of a step's tiles (the last token's where a tile is past the end: its
-// page is there to be read); negative: outside the cache.
+// The pages of a step's tiles, as the table has them (the last token's where a tile is past the end: its
+// page is there to be read).
 struct Pages {
     int of[4];
-    __device__ __forceinline__ bool all() const { return (of[0] | of[1] | of[2] | of[3]) >= 0; }
 };
 __device__ __forceinline__ Pages find_pages(const Attn4Args& a, int b, int t, int last) {
+    const const_int* table = (const const_int*)a.table + (int64_t)b * a.table_pages;
     Pages p;
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const int page = a.table[(int64_t)b * a.table_pages + (min(t + 16 * h, last) >> a.c.page_bits)];
-        p.of[h] = __builtin_amdgcn_readfirstlane((uint32_t)page < (uint32_t)a.c.pages ? page : -1);
-    }
+    for (int h = 0; h < 4; ++h) p.of[h] = table[min(t + 16 * h, last) >> a.c.page_bits];
     return p;
 }
+// Whether a page is one of the cache's; the others hold no tokens, and page 0 is read in their place.
+__device__ __forceinline__ bool there(const Attn4Args& a, int page) { return (uint32_t)page < (uint32_t)a.c.pages; }
 // row of the cache's first token of a tile at token t
 __device__ __forceinline__ int64_t tile_row(const Attn4Args& a, int head, int page, int t) {
-    return (((int64_t)max(page, 0) * a.c.heads + head) << a.c.page_bits) + (t & ((1 << a.c.page_bits) - 1));
+    return (((int64_t)(there(a, page) ? page : 0) * a.c.heads + head) << a.c.page_bits) + (t & ((1 << a.c.page_bits) - 1));
 }
 
 template <int RP>
@@ -224,23 +227,62 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
     };
     __shared__ __attribute__((aligned(16))) Shared shared;
     __shared__ float shared_m[WT][16], shared_l[WT][16];
+    __shared__ f16x8 shared_q[KK][64];                      // operands: 16 registers more would cost a wave a SIMD
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int blocks = (a.max_q * a.group + RP - 1) / RP;
-    // splits last: later ones are there for the longer sequences only, and as many for every XCD
-    int u = blockIdx.x;
-    const int head = u % a.c.heads;
-    u /= a.c.heads;
-    const int col0 = u % blocks * RP;
-    u /= blocks;
-    const int b = u % a.sequences, split = u / a.sequences;
+
+    // this workgroup's steps pos .. last - 1 of all and the sequence that they begin in, or its unit
+    int b, start = 0, pos = 0, last = 0, from = 0, unit = 0;
+    if (a.part_o) {
+        int total = 0;
+        for (int i = lane; i < a.sequences; i += 64) total += work4<RP>(a, sequence(a, i)).all();
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) total += __shfl_xor(total, i);
+        const int each = max(kLeastSteps, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.starts[a.sequences] = each;
+        from = pos = __builtin_amdgcn_readfirstlane(min((int64_t)blockIdx.x * each, (int64_t)total));
+        last = __builtin_amdgcn_readfirstlane(min(pos + each, total));
+        b = start = -1;
+        for (int i = 0, before = 0; i < a.sequences; i += 64) {
+            const int w = i + lane < a.sequences ? work4<RP>(a, sequence(a, i + lane)).all() : 0;
+            int up = w;
+#pragma unroll
+            for (int k = 1; k < 64; k <<= 1) {
+                const int v = __shfl_up(up, k);
+                up += lane >= k ? v : 0;
+            }
+            if (blockIdx.x == 0 && wave == 0 && i + lane < a.sequences) a.starts[i + lane] = before + up - w;
+            const uint64_t here = __ballot(pos < before + up);
+            if (b < 0 && here) {
+                const int at = __builtin_ctzll(here);
+                b = i + at;
+                start = __builtin_amdgcn_readfirstlane(before + __shfl(up - w, at));
+                if (blockIdx.x != 0) break;
+            }
+            before += __shfl(up, 63);
+        }
+        if (pos >= last) return;
+    } else {
+        b = blockIdx.x / (a.c.heads * ((a.max_q * a.group + RP - 1) / RP));
+        unit = blockIdx.x % (a.c.heads * ((a.max_q * a.group + RP - 1) / RP));
+        if (unit >= work4<RP>(a, sequence(a, b)).units) return;     // a unit of no steps is written too: its rows are 0
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+  do {
     const Sequence s = sequence(a, b);
-    const int cols = s.nq * a.group;
-    if (col0 >= cols) return;
+    const Work4 work = work4<RP>(a, s);
+    int step0 = 0, taken = work.steps, passed = 0;
+    if (a.part_o) {
+        unit = (pos - start) / work.each();
+        const int at = (pos - start) % work.each();
+        passed = min(work.each() - at, last - pos);
+        step0 = max(at - kUnitSteps, 0);
+        taken = max(at + passed - kUnitSteps, 0) - step0;
+    }
+    if (taken > 0 || !a.part_o) {
+    const int head = unit % a.c.heads, col0 = unit / a.c.heads * RP, cols = s.nq * a.group;
     const int low = visible(a, s, col0 / a.group), high = visible(a, s, (min(col0 + RP, cols) - 1) / a.group);
-    const int64_t first = (int64_t)split * a.chunk;
-    if (a.splits > 1 && first >= high) return;
-    const int begin = (int)first + wave * kStep, end = (int)min((int64_t)high, first + a.chunk);
+    const int begin = (step0 + wave) * kStep, end = min(high, (step0 + taken) * kStep);
     constexpr int stride = kStep * WT;
     // the lane's scores: columns (within the block) mine + e, tokens of tile base + kTiles * i, i < NT
     const int mine = RP == 4 ? 0 : RP == 8 ? 4 * (g & 1) : 4 * g, base = RP == 4 ? g : RP == 8 ? g >> 1 : 0;
@@ -278,27 +320,25 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
         load_values(pages, begin);
         next = find_pages(a, b, begin + stride, end - 1);
     }
-    f16x8 q[KK];
     float of_minimum[R], to_score;
-    int limit[R];
     {
         const int col = min(col0 + r % RP, cols - 1), qi = col / a.group;
         Queries<D> mq;
         mq.load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
-        const int seen = visible(a, s, qi);
         to_score = mq.to_score;
 #pragma unroll
-        for (int i = 0; i < KK; ++i) q[i] = mq.op[i];
+        for (int i = 0; i < KK; ++i)
+            if (wave == 0) shared_q[i][lane] = mq.op[i];
 #pragma unroll
         for (int e = 0; e < R; ++e) {
             of_minimum[e] = __shfl(mq.of_minimum, mine + e);
-            limit[e] = __shfl(seen, mine + e);
         }
+        __syncthreads();
     }
 
     f32x4 acc[VT] = {};
     float m[R], l[R] = {}, rest[R] = {};                    // rest: what the codes about their middle leave out
-    float unit = 0.0f, per_unit = 0.0f;
+    float scale = 0.0f, per_scale = 0.0f;                   // weights are held as multiples of `scale`
 #pragma unroll
     for (int e = 0; e < R; ++e) m[e] = kLowest;
     // over the lanes that keep the same columns
@@ -316,10 +356,17 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
     };
 
     for (int t = begin; t < end; t += stride) {
+        // the step after this one; behind the last the same again, so that the loads are not conditional (their
+        // registers would be copied, and the copies wait for them)
         const bool more = t + stride < end;
+        const int then = more ? t + stride : t;
         const Pages now = pages;
-        pages = next;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) pages.of[h] = more ? next.of[h] : now.of[h];
         float x[NT][R];
+        f16x8 q[KK];
+#pragma unroll
+        for (int i = 0; i < KK; ++i) q[i] = shared_q[i][lane];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -344,18 +391,19 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
 #pragma unroll
             for (int e = 0; e < R; ++e) x[i][e] = __builtin_fmaf(x[i][e], (float)k[0], __builtin_fmaf((float)k[1], of_minimum[e], bad));
         }
-        if (more) load_keys(pages, t + stride);
-        if (t + kStep > low || !now.all()) {
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(pages, then);
+        if (t + kStep > low || !there(a, now.of[0]) || !there(a, now.of[1]) || !there(a, now.of[2]) || !there(a, now.of[3])) {
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 int page = now.of[i * Shape4<RP>::kTiles];
 #pragma unroll
                 for (int h = 1; h < Shape4<RP>::kTiles; ++h) page = base == h ? now.of[i * Shape4<RP>::kTiles + h] : page;
                 const int token = t + 16 * (i * Shape4<RP>::kTiles + base) + r;
-                if (page < 0 || token >= end) vps[i] = 0u;      // whatever memory holds there
+                if (!there(a, page) || token >= end) vps[i] = 0u;      // whatever memory holds there
 #pragma unroll
                 for (int e = 0; e < R; ++e)
-                    if (page < 0 || token >= limit[e]) x[i][e] = -INFINITY;
+                    if (!there(a, page) || token >= visible(a, s, (col0 + mine + e) / a.group)) x[i][e] = -INFINITY;
             }
         }
         float most = 0.0f;
@@ -376,13 +424,13 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             top[e] *= to_score;
             moves = moves || top[e] > m[e] + kSlack;
         }
-        moves = moves || most > unit;
+        moves = moves || most > scale;
         if (__any(moves)) {
-            const float old = unit;
+            const float old = scale;
 #pragma unroll
             for (int i = 1; i < 64; i <<= 1) most = fmaxf(most, __shfl_xor(most, i));
-            unit = fmaxf(unit, 2.0f * most);
-            per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
+            scale = fmaxf(scale, 2.0f * most);
+            per_scale = scale > 0.0f ? 1.0f / scale : 0.0f;
             float down[R];
 #pragma unroll
             for (int e = 0; e < R; ++e) {
@@ -391,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
                 m[e] = to;
                 l[e] *= down[e];
                 rest[e] *= down[e];
-                down[e] *= old * per_unit;
+                down[e] *= old * per_scale;
             }
             // the factor of the second product's column r: register r % 4 of a lane that keeps it
             float by = 1.0f;
@@ -408,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             const int tile = i * Shape4<RP>::kTiles + base;
             // tokens of 32 in the order of the second product's operand: 4 g .. + 3 of one tile, then of the other
             const int at = tile / 2 * 32 + r / 4 * 8 + tile % 2 * 4 + r % 4;
-            const float by = sv[i] * per_unit, off = -7.5f * unit;
+            const float by = sv[i] * per_scale, off = -7.5f * scale;
 #pragma unroll
             for (int e = 0; e < R; ++e) {
                 const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], to_score, -m[e]));
@@ -420,24 +468,27 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own, read by its other lanes
         __builtin_amdgcn_wave_barrier();
+        f16x8 p[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) p[h] = *reinterpret_cast<const f16x8*>(&shared.p[wave][r % RP][32 * h + 8 * g]);
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(p[0]), "+v"(p[1])::"memory");
+        // scalar loads count with those of LDS: the next table entries are under way through the second product only
+        next = find_pages(a, b, t + 2 * stride, end - 1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f16x8 p = *reinterpret_cast<const f16x8*>(&shared.p[wave][r % RP][32 * h + 8 * g]);
 #pragma unroll
             for (int w = 0; w < D / 64; ++w) {
                 const uint32_t a0 = values.v[2 * h][2 * w], a1 = values.v[2 * h][2 * w + 1];
                 const uint32_t b0 = values.v[2 * h + 1][2 * w], b1 = values.v[2 * h + 1][2 * w + 1];
-                acc[4 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<0>(a0, a1, b0, b1), p, acc[4 * w], 0, 0, 0);
-                acc[4 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<1>(a0, a1, b0, b1), p, acc[4 * w + 1], 0, 0, 0);
-                acc[4 * w + 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<2>(a0, a1, b0, b1), p, acc[4 * w + 2], 0, 0, 0);
-                acc[4 * w + 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<3>(a0, a1, b0, b1), p, acc[4 * w + 3], 0, 0, 0);
+                acc[4 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<0>(a0, a1, b0, b1), p[h], acc[4 * w], 0, 0, 0);
+                acc[4 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<1>(a0, a1, b0, b1), p[h], acc[4 * w + 1], 0, 0, 0);
+                acc[4 * w + 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<2>(a0, a1, b0, b1), p[h], acc[4 * w + 2], 0, 0, 0);
+                acc[4 * w + 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_operand<3>(a0, a1, b0, b1), p[h], acc[4 * w + 3], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (more) {
-            load_values(pages, t + stride);
-            next = find_pages(a, b, t + 2 * stride, end - 1);
-        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_values(pages, then);
         asm volatile("" ::: "memory");                      // the weights are read before the next are written
     }
 
@@ -460,7 +511,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             shared_l[wave][mine + e] = l[e];
         }
     }
-    const float of_unit = unit * 0x1p24f;
+    const float of_scale = scale * 0x1p24f;
     __syncthreads();                                        // every wave has read its last weights
     if (r < RP && col0 + r < cols) {
 #pragma unroll
@@ -469,99 +520,130 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int i = (c + k) % VT, e = (c + k) / VT;
-                out[k] = __builtin_fmaf(acc[i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), add);
+                out[k] = __builtin_fmaf(acc[i][e], of_scale * (i % 2 ? 0.0625f : 1.0f), add);
             }
             *reinterpret_cast<f32x4*>(&shared.o[wave][r][g * (D / 4) + c]) = out;
         }
     }
     __syncthreads();
+    const bool whole = taken == work.steps;
+    const int64_t place = ((int64_t)blockIdx.x * 2 + (pos == from ? 0 : 1)) * RP;   // at most two parts of units a workgroup
     for (int i = threadIdx.x; i < RP * (D / 4); i += 256) {
         const int col = i / (D / 4), ch = 4 * (i % (D / 4));
         if (col0 + col >= cols) break;
-        float mx = shared_m[0][col], sum = 0.0f, o[4] = {};
+        float mx = shared_m[0][col], sum = 0.0f;
+        f32x4 o = {};
 #pragma unroll
         for (int w = 1; w < WT; ++w) mx = fmaxf(mx, shared_m[w][col]);
 #pragma unroll
         for (int w = 0; w < WT; ++w) {
             const float by = __builtin_amdgcn_exp2f(shared_m[w][col] - mx);
             sum = __builtin_fmaf(shared_l[w][col], by, sum);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(shared.o[w][col][ch + e], by, o[e]);
+            o += *reinterpret_cast<const f32x4*>(&shared.o[w][col][ch]) * by;
         }
-        store_result<T, D, 4>(a, s, head, split, col0 + col, ch, o, mx, sum, ch == 0);
+        if (whole) {
+            store_output<T>(a, s, head, col0 + col, ch, o, sum);
+        } else {
+            *reinterpret_cast<f32x4*>(a.part_o + (place + col) * D + ch) = o;
+            if (ch == 0) {
+                a.part_m[place + col] = mx;
+                a.part_l[place + col] = sum;
+            }
+        }
     }
+    }
+    pos += passed;
+    if (!a.part_o || pos >= last) return;
+    __syncthreads();                                        // the results are read before the next unit's weights
+    if (pos >= start + work.all()) {
+        start += work.all();
+        do ++b;                                             // there is one: steps are left
+        while (work4<RP>(a, sequence(a, b)).all() == 0);
+    }
+  } while (true);
 }
 
-// Joins the splits of a row, one workgroup a row: lane i weighs split i, and each
-// half (D = 64: quarter) of a wave adds up its share of the splits.
-template <typename T, int D>
+// Joins the parts of a row, one workgroup a row, D / 4 lanes a part; rows of no tokens become 0.
+template <typename T, int D, int RP>
 __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
     constexpr int Lanes = D / 4, Shares = 256 / Lanes;
-    const int lane = threadIdx.x & 63, share = threadIdx.x / Lanes, at = threadIdx.x % Lanes;
-    const int heads = a.c.heads * a.group, head = blockIdx.x % heads, qi = blockIdx.x / heads % a.max_q;
+    const int share = threadIdx.x / Lanes, at = threadIdx.x % Lanes;
+    const int heads = a.c.heads * a.group, hq = blockIdx.x % heads, qi = blockIdx.x / heads % a.max_q;
     const int b = blockIdx.x / heads / a.max_q;
     const Sequence s = sequence(a, b);
     if (qi >= s.nq) return;
-    const int seen = visible(a, s, qi), active = seen > 0 ? min((seen - 1) / a.chunk + 1, a.splits) : 0;
-    const int64_t row = (int64_t)(s.q0 + qi) * heads + head, step = (int64_t)a.tokens * heads;
-    f32x4 o = {};
-    const float m = lane < active ? a.part_m[row + lane * step] : kLowest, l = lane < active ? a.part_l[row + lane * step] : 0.0f;
-    f32x4 ahead[2];                                         // the first two are loaded beside the weights
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        ahead[i] = share + i * Shares < active ? *reinterpret_cast<const f32x4*>(a.part_o + (row + (share + i * Shares) * step) * D + 4 * at) : f32x4{};
-    float mx = m;
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
-    const float by = lane < active ? __builtin_amdgcn_exp2f(m - mx) : 0.0f;
-    float sum = by * l;
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) sum += __shfl_xor(sum, i);
-#pragma unroll
-    for (int i = 0; i < kMostSplits / Shares; ++i) {
-        if (i * Shares >= active) break;
-        const int split = share + i * Shares;
-        const float w = __shfl(by, split);                  // 0 from `active` on
-        const f32x4 v = i < 2 ? ahead[i] : split < active ? *reinterpret_cast<const f32x4*>(a.part_o + (row + split * step) * D + 4 * at) : f32x4{};
-        o += v * w;
+    const int head = hq / a.group, col = qi * a.group + hq % a.group;
+    const Work4 work = work4<RP>(a, s);
+    const int each = a.starts[a.sequences], first = a.starts[b] + (col / RP * a.c.heads + head) * work.each();
+    const int w0 = (first + kUnitSteps) / each, w1 = (first + work.each() - 1) / each, parts = w1 - w0 + 1;
+    if (parts == 1 && work.steps > 0) return;               // its workgroup wrote it
+    if (work.steps == 0) {
+        if (share == 0) store_output<T>(a, s, head, col, 4 * at, f32x4{}, 0.0f);
+        return;
     }
-    __shared__ f32x4 shared[Shares][Lanes];
-    shared[share][at] = o;
+    // where workgroup w0 + i left its part: only the first may have begun with another unit
+    auto place = [&](int i) { return ((int64_t)(w0 + i) * 2 + (i == 0 && first > w0 * each ? 1 : 0)) * RP + col % RP; };
+    f32x4 o = {};
+    float mx = kLowest, sum = 0.0f;
+    for (int i = share; i < parts; i += Shares) {
+        const int64_t p = place(i);
+        const float m = a.part_m[p], to = fmaxf(mx, m), down = __builtin_amdgcn_exp2f(mx - to), by = __builtin_amdgcn_exp2f(m - to);
+        o = o * down + *reinterpret_cast<const f32x4*>(a.part_o + p * D + 4 * at) * by;
+        sum = sum * down + a.part_l[p] * by;
+        mx = to;
+    }
+    __shared__ f32x4 shared_o[Shares][Lanes];
+    __shared__ float shared_m[Shares], shared_l[Shares];
+    shared_o[share][at] = o;
+    if (at == 0) {
+        shared_m[share] = mx;
+        shared_l[share] = sum;
+    }
     __syncthreads();
     if (share > 0) return;
 #pragma unroll
-    for (int i = 1; i < Shares; ++i) o += shared[i][at];
-    typedef T half4 __attribute__((ext_vector_type(4)));
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;      // a row that sees nothing is 0
-    *reinterpret_cast<half4*>(static_cast<T*>(a.o) + (s.q0 + qi) * a.o_token + head * a.o_head + 4 * at) = __builtin_convertvector(o * inv, half4);
+    for (int i = 1; i < Shares; ++i) mx = fmaxf(mx, shared_m[i]);
+    o = f32x4{};
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < Shares; ++i) {
+        const float by = __builtin_amdgcn_exp2f(shared_m[i] - mx);
+        o += shared_o[i][at] * by;
+        sum += shared_l[i] * by;
+    }
+    store_output<T>(a, s, head, col, 4 * at, o, sum);
 }
 
 // ---------------------------------------------------------------- host side --
 struct Plan4 {
     int columns;                        // of a workgroup
-    int blocks, splits, chunk;
+    int64_t groups;
+    bool whole;                         // a workgroup takes whole units
 };
 
+// Workgroups of a launch.  Short sequences (up to 1024 tokens: 16 steps, four for
+// each wave) are taken whole; the others are cut into as many equal shares as
+// workgroups fit on the chip, or shares of four steps if those are fewer.
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
     p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
-    p.blocks = (int)((cols + p.columns - 1) / p.columns);
-    const int64_t units = (int64_t)sequences * heads * p.blocks, least = kStep;
-    int64_t splits = (1024 + units - 1) / units;
-    splits = splits > kMostSplits ? kMostSplits : splits;
-    const int64_t room = (max_kv + least - 1) / least;
-    splits = splits > room ? room : splits;
-    if (splits < 1) splits = 1;
-    const int64_t chunk = ((max_kv + splits - 1) / splits + least - 1) / least * least;
-    p.chunk = (int)(chunk < least ? least : chunk > (INT32_MAX / least) * least ? (INT32_MAX / least) * least : chunk);
-    p.splits = splits == 1 ? 1 : (int)((max_kv + p.chunk - 1) / p.chunk);
+    const int64_t units = (int64_t)sequences * heads * ((cols + p.columns - 1) / p.columns), steps = (max_kv + kStep - 1) / kStep;
+    p.whole = steps <= 16;
+    const int64_t shares = (units * steps + kLeastSteps - 1) / kLeastSteps, resident = p.columns > 8 ? 512 : 768;
+    p.groups = p.whole ? units : shares < resident ? shares : resident;
     return p;
+}
+static size_t workspace4(const Plan4& p, int sequences, int head_dim) {
+    const size_t floats = p.whole ? 0 : (size_t)p.groups * 2 * p.columns * (head_dim + 2) + (size_t)sequences + 1;
+    return (floats * sizeof(float) + 15) / 16 * 16;
 }
 
 static bool shape4_ok(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     return sequences >= 0 && heads >= 1 && group >= 1 && max_q >= 0 && max_kv >= 0 && sequences <= (1 << 24) && heads <= 65535 &&
-           group <= 1024 && (int64_t)max_q * group < (1 << 30) && max_kv < (1ll << 31) - 65536;
+           group <= 1024 && (int64_t)max_q * group < (1 << 30) && max_kv < (1ll << 31) - 65536 &&
+           // steps of all units, counted in 32 bits
+           (double)sequences * heads * (((double)max_q * group + 15) / 4) * ((double)max_kv / kStep + 1 + kUnitSteps) < (1 << 30) * 1.0;
 }
 
 }  // namespace mq
@@ -571,8 +653,7 @@ using namespace mq;
 extern "C" size_t mq_attention_kv4_workspace_size(int sequences, int tokens, int heads, int group, int head_dim, int max_q,
                                                   int64_t max_kv) {
     if (!shape4_ok(sequences, heads, group, max_q, max_kv) || tokens < 0 || head_dim < 1 || sequences == 0 || max_q == 0) return 0;
-    const Plan4 p = plan4(sequences, heads, group, max_q, max_kv);
-    return p.splits == 1 ? 0 : (size_t)p.splits * tokens * heads * group * (head_dim + 2) * sizeof(float);
+    return workspace4(plan4(sequences, heads, group, max_q, max_kv), sequences, head_dim);
 }
 
 extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, int tokens, int group, int max_q, int64_t max_kv,
@@ -596,25 +677,27 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
     const Plan4 p = plan4(sequences, cache->heads, group, max_q, max_kv);
     const size_t need = mq_attention_kv4_workspace_size(sequences, tokens, cache->heads, group, cache->head_dim, max_q, max_kv);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
-    const int64_t rows = (int64_t)p.splits * tokens * cache->heads * group;
-    float* part = static_cast<float*>(workspace);
+    float* part = p.whole ? nullptr : static_cast<float*>(workspace);
+    const int64_t rows = p.groups * 2 * p.columns;
     const Attn4Args a{device_cache4(cache), Q, O, q_token, q_head, o_token, o_head, page_table, table_pages, (int)max_kv, kv_lens, cu_q,
-                      sequences, tokens, group, max_q, scale, causal != 0, p.splits, p.chunk, part,
-                      part ? part + rows * cache->head_dim : nullptr, part ? part + rows * (cache->head_dim + 1) : nullptr};
-    const int64_t grid = (int64_t)sequences * cache->heads * p.blocks * p.splits;
+                      sequences, tokens, group, max_q, scale, causal != 0, part, part ? part + rows * cache->head_dim : nullptr,
+                      part ? part + rows * (cache->head_dim + 1) : nullptr,
+                      part ? reinterpret_cast<int32_t*>(part + rows * (cache->head_dim + 2)) : nullptr};
     const int64_t joins = (int64_t)sequences * max_q * cache->heads * group;
-    if (grid > INT32_MAX || joins > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (p.groups > INT32_MAX || joins > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a); };
-            if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>);
-            else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>);
-            else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>);
-            else if (max_q * group > 1) few(attention4_kernel<T, D, 4, 2>);
-            else few(attention4_kernel<T, D, 4, 1>);
-            if (p.splits > 1) hipLaunchKernelGGL((attention4_join_kernel<T, D>), dim3((unsigned)joins), dim3(256), 0, stream, a);
+            auto few = [&](auto kernel, auto join) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(256), 0, stream, a);
+                if (!p.whole) hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
+            };
+            if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
+            else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>, attention4_join_kernel<T, D, 8>);
+            else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>, attention4_join_kernel<T, D, 4>);
+            else if (max_q * group > 1) few(attention4_kernel<T, D, 4, 2>, attention4_join_kernel<T, D, 4>);
+            else few(attention4_kernel<T, D, 4, 1>, attention4_join_kernel<T, D, 4>);
             return mq_host::launch_status();
         };
         return cache->head_dim == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
