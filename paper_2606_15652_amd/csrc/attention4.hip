@@ -563,6 +563,243 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
   } while (true);
 }
 
+// --------------------------------------------------------------------------
+// Many columns: keys and values of 64 tokens at a time in LDS, as operands.
+// --------------------------------------------------------------------------
+// NW waves of 32 columns each.  S^T = K Q^T: a lane holds four neighbouring tokens
+// of one query, which is what the second product, O^T = V^T P^T, takes from it.
+// Keys are staged as codes (subnormal numbers), their scales and minima, in fp32,
+// act on the scores; values are staged as fp16 values, rounded once.  A stage is
+// converted by the whole workgroup while the one before is in use, from registers
+// loaded one stage earlier still; every conversion then serves 32 NW columns.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a) {
+    constexpr int KK = D / 32, VT = D / 16, C = 2, WaveCols = 16 * C, Cols = WaveCols * NW, ValueLanes = 128 * (D / 64);
+    struct Stage {
+        f16x8 k[4][KK][64];                                 // tile, operand, lane
+        f16x8 v[2][VT][64];                                 // two tiles, operand, lane
+        f32x2 kp[64];                                       // token: scale, minimum
+    };
+    __shared__ __attribute__((aligned(16))) Stage stages[2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    // The last columns, which see most, first; the blocks of a head's columns on one XCD where heads allow; the
+    // sequences of a round one further on than in the round before, as workgroups go to the parts of an XCD in turn
+    // (four ragged sequences, always in the same order: 500 us, XX).
+    const int blocks = (a.max_q * a.group + Cols - 1) / Cols, pairs = a.sequences * a.c.heads;
+    const int round = blockIdx.x / pairs, pair = blockIdx.x % pairs, head = pair % a.c.heads, b = (pair / a.c.heads + round) % a.sequences;
+    const int block0 = (blocks - 1 - round) * Cols;
+    const Sequence s = sequence(a, b);
+    const int cols = s.nq * a.group;
+    if (block0 >= cols) return;
+    const int end = visible(a, s, (min(block0 + Cols, cols) - 1) / a.group);
+    const int col0 = block0 + wave * WaveCols;
+    const bool mine = col0 < cols;
+    const int low = mine ? visible(a, s, col0 / a.group) : 0, high = mine ? visible(a, s, (min(col0 + WaveCols, cols) - 1) / a.group) : 0;
+
+    // Loads of a stage: wave w has the keys of tile w, wave w (of eight: w - 4) the values of channels (D / 16) r +
+    // 4 (w % (D / 64)) .. of tiles 2 (w / (D / 64)) and one on, and their parameters; wave 0 those of the keys.
+    const int key_tile = wave, value_item = NW == 8 ? wave - 4 : wave;
+    const bool has_keys = wave < 4, has_values = value_item >= 0 && value_item < ValueLanes / 64;
+    const int value_tile = value_item / (D / 64) * 2, value_word = value_item % (D / 64);
+    uint32_t raw_k[D / 32], raw_v[2][2], raw_kp = 0, raw_vp = 0;
+    u32x4 raw_p[2];
+    int table = 0;                                          // lane h: page of tile h
+    auto load_table = [&](int t) {
+        const int at = min(t + 16 * (lane & 3), end - 1);
+        table = a.table[(int64_t)b * a.table_pages + (max(at, 0) >> a.c.page_bits)];
+    };
+    auto page_row = [&](int page, int t) { return tile_row(a, head, page, t); };
+    int page[4] = {};
+    auto load = [&](int t) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) page[h] = __builtin_amdgcn_readlane(table, h);
+        if (has_keys) {
+            const int64_t row = page_row(key_tile == 0 ? page[0] : key_tile == 1 ? page[1] : key_tile == 2 ? page[2] : page[3], t + 16 * key_tile);
+            __builtin_memcpy(raw_k, __builtin_assume_aligned(a.c.k + row * (D / 2) + (uint32_t)(r * (D / 2) + g * (D / 8)), D / 8), D / 8);
+        }
+        if (has_values) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t row = page_row(value_tile == 0 ? page[h] : page[2 + h], t + 16 * (value_tile + h));
+                __builtin_memcpy(raw_v[h], __builtin_assume_aligned(a.c.v + row * (D / 2) + (uint32_t)(g * (2 * D) + r * (D / 8) + 8 * value_word), 8), 8);
+                raw_p[h] = *reinterpret_cast<const u32x4*>(a.c.vp + row + 4 * g);
+            }
+        }
+        if (wave == 0) {                                    // lane: token
+            int64_t row = page_row(page[0], t);
+#pragma unroll
+            for (int h = 1; h < 4; ++h)
+                if (g == h) row = page_row(page[h], t + 16 * h);
+            raw_kp = a.c.kp[row + r];
+            raw_vp = a.c.vp[row + r];
+        }
+    };
+    auto finite = [](uint32_t p) { return (p & 0x7C00u) != 0x7C00u; };     // both parameters are NaN, or none
+    auto convert = [&](Stage& st, int t) {
+        if (has_keys) {
+#pragma unroll
+            for (int i = 0; i < KK; ++i) st.k[key_tile][i][lane] = key_operand(raw_k[i]);
+        }
+        if (has_values) {
+            u32x4 w[4];                                     // channel of the word: four pairs of tokens
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = raw_p[h][e];
+                    // a row that is not finite weighs on the scores (below); a weight of 0 leaves it out here
+                    if (!finite(p[e]) || t + 16 * (value_tile + h) + 4 * g + e >= s.n) p[e] = 0;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f16x2 sv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u));
+                    const f16x2 zv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u));
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const uint32_t code = ((raw_v[h][k] >> (4 * n)) & 0x000F000Fu) | 0x64006400u;   // 1024 + n
+                        const f16x2 v = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, code) - (f16x2)(_Float16)1024.0f, sv, zv);
+                        w[n][2 * h + k] = __builtin_bit_cast(uint32_t, v);
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) st.v[value_tile / 2][4 * value_word + n][lane] = __builtin_bit_cast(f16x8, w[n]);
+        }
+        if (wave == 0) {
+            const f16x2 k = __builtin_bit_cast(f16x2, raw_kp);
+            // a value row that is not finite makes the score NaN, for the queries that see it
+            st.kp[lane] = f32x2{(float)k[0], finite(raw_vp) ? (float)k[1] : NAN};
+        }
+    };
+
+    Queries<D> q[C];
+    int limit[C];
+    load_table(0);
+    load(0);
+    load_table(kStep);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const int col = min(col0 + 16 * j + r, cols - 1), qi = col / a.group;
+        limit[j] = visible(a, s, qi);
+        q[j].load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
+    }
+    // (kept here: the compiler would make the operands again in every step that has work)
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int i = 0; i < KK; ++i) asm volatile("" : "+v"(q[j].op[i]));
+    f32x4 acc[C][VT] = {};
+    float m[C], l[C] = {};
+#pragma unroll
+    for (int j = 0; j < C; ++j) m[j] = kLowest;
+
+    int now[4];                                             // pages of the stage in use
+    auto turn = [&](int t) {                                // the stage at t from registers to LDS, the one after into registers
+#pragma unroll
+        for (int h = 0; h < 4; ++h) now[h] = page[h];
+        convert(stages[t / kStep & 1], t);
+        if (t + kStep < end) {
+            load(t + kStep);
+            load_table(t + 2 * kStep);
+        }
+        __syncthreads();
+    };
+    turn(0);
+    for (int t = 0; t < end; t += kStep) {
+        const Stage& st = stages[t / kStep & 1];
+        if (t < high) {
+            f32x4 x[C][4] = {};
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                for (int i = 0; i < KK; ++i) {
+                    const f16x8 k = st.k[h][i][lane];
+#pragma unroll
+                    for (int j = 0; j < C; ++j) x[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[j].op[i], x[j][h], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x2 kp = st.kp[16 * h + 4 * g + e];
+#pragma unroll
+                    for (int j = 0; j < C; ++j) x[j][h][e] = __builtin_fmaf(x[j][h][e], kp[0], kp[1] * q[j].of_minimum);
+                }
+            if (t + kStep > low || !there(a, now[0]) || !there(a, now[1]) || !there(a, now[2]) || !there(a, now[3])) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < C; ++j)
+                            if (!there(a, now[h]) || t + 16 * h + 4 * g + e >= limit[j]) x[j][h][e] = -INFINITY;
+            }
+            float top[C];
+            bool moves = false;
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                top[j] = -INFINITY;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top[j] = fmaxf(top[j], x[j][h][e]);
+                top[j] *= q[j].to_score;
+                moves = moves || top[j] > m[j] + kSlack;
+            }
+            if (__any(moves)) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                    const float to = fmaxf(m[j], quads_max(top[j])), down = __builtin_amdgcn_exp2f(m[j] - to);
+                    m[j] = to;
+                    l[j] *= down;
+#pragma unroll
+                    for (int i = 0; i < VT; ++i) acc[j][i] *= down;
+                }
+            }
+            f16x8 p[C][2];
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    f32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][h][e], q[j].to_score, -m[j]));
+                        l[j] += w[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[j][h / 2][4 * (h % 2) + e] = (_Float16)w[e];
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < VT; ++i) {
+                    const f16x8 v = st.v[h][i][lane];
+#pragma unroll
+                    for (int j = 0; j < C; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[j][h], acc[j][i], 0, 0, 0);
+                }
+        }
+        if (t + kStep < end) turn(t + kStep);
+    }
+
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const float sum = quads_sum(l[j]);
+        if (col0 + 16 * j + r < cols) {
+#pragma unroll
+            for (int c = 0; c < D / 4; c += 4) {
+                f32x4 o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = acc[j][(c + k) % VT][(c + k) / VT];
+                store_output<T>(a, s, head, col0 + 16 * j + r, g * (D / 4) + c, o, sum);
+            }
+        }
+    }
+}
+
 // Joins the parts of a row, one workgroup a row, D / 4 lanes a part; rows of no tokens become 0.
 template <typename T, int D, int RP>
 __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
@@ -616,7 +853,7 @@ __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
 
 // ---------------------------------------------------------------- host side --
 struct Plan4 {
-    int columns;                        // of a workgroup
+    int columns;                        // of a workgroup: up to 16, 256
     int64_t groups;
     bool whole;                         // a workgroup takes whole units
 };
@@ -627,9 +864,9 @@ struct Plan4 {
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
-    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : 16;
+    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 128;
     const int64_t units = (int64_t)sequences * heads * ((cols + p.columns - 1) / p.columns), steps = (max_kv + kStep - 1) / kStep;
-    p.whole = steps <= 16;
+    p.whole = steps <= 16 || p.columns == 128;
     const int64_t shares = (units * steps + kLeastSteps - 1) / kLeastSteps, resident = p.columns > 8 ? 512 : 768;
     p.groups = p.whole ? units : shares < resident ? shares : resident;
     return p;
@@ -693,7 +930,8 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
                 hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(256), 0, stream, a);
                 if (!p.whole) hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
             };
-            if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
+            if (p.columns == 128) hipLaunchKernelGGL((attention4_wide_kernel<T, D, 4>), dim3((unsigned)p.groups), dim3(256), 0, stream, a);
+            else if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
             else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>, attention4_join_kernel<T, D, 8>);
             else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>, attention4_join_kernel<T, D, 4>);
             else if (max_q * group > 1) few(attention4_kernel<T, D, 4, 2>, attention4_join_kernel<T, D, 4>);
