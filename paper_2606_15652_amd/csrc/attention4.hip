@@ -104,42 +104,45 @@ __device__ __forceinline__ f16x8 value_operand(uint32_t a0, uint32_t a1, uint32_
     return __builtin_bit_cast(f16x8, u32x4{(a0 >> shift) & mask, (a1 >> shift) & mask, (b0 >> shift) & mask, (b1 >> shift) & mask});
 }
 
-// Operands and scales of 16 columns of queries: fp16, scaled by a power of two (the largest value near
-// 2^8, so that neither type's range matters), channels of the codes that come 16 times too large divided
-// by 16.  A lane has the channels (D / 4) g .. of its column.
+// Operands and scales of 16 columns of queries: fp16, scaled by a power of two that brings the largest
+// value near 2^8, so that neither type's range matters; channels of the codes that come 16 times too large
+// divided by 16.  A lane has the channels (D / 4) g .. of its column.
 template <int D>
 struct Queries {
     f16x8 op[D / 32];
-    // x = sk (q'.n) + zk of_minimum is the score over to_score, in powers of 2
-    float to_score, of_minimum;
+    // x = sk (q'.n) + zk of_minimum is the score over to_score(), in powers of 2
+    float of_minimum, amax;
+    f32x8 x[D / 32];
 
     template <typename T>
-    __device__ __forceinline__ void load(const T* q, float scale) {
-        f32x8 x[D / 32];
-        float sum = 0.0f, amax = 0.0f;
+    __device__ __forceinline__ void load(const T* q) {      // amax: of the 16 columns
+        of_minimum = amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
             x[i] = load8(q + 8 * i);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sum += x[i][e];
+                of_minimum += x[i][e];
                 amax = fmaxf(amax, fabsf(x[i][e]));
             }
         }
-        sum = quads_sum(sum);
-        amax = quads_max(amax);
+        of_minimum = quads_sum(of_minimum);
 #pragma unroll
-        for (int i = 1; i < 16; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
-        const int up = amax > 0.0f && amax < INFINITY ? 8 - ilogbf(amax) : 0;
+        for (int i = 1; i < 64; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
+    }
+    static __device__ __forceinline__ int exponent(float amax) { return amax > 0.0f && amax < INFINITY ? 8 - ilogbf(amax) : 0; }
+    __device__ __forceinline__ void finish(int up) {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = ldexpf(x[i][e], e & 2 ? up - 4 : up);
             op[i] = __builtin_convertvector(x[i], f16x8);
         }
-        // never zero or infinite, so that a hidden token's -infinity stays that
-        to_score = fminf(fmaxf(ldexpf(scale * kLog2e, 24 - up), FLT_MIN), FLT_MAX);
-        of_minimum = ldexpf(sum, up - 24);
+        of_minimum = ldexpf(of_minimum, up - 24);
+    }
+    // never zero or infinite, so that a hidden token's -infinity stays that
+    static __device__ __forceinline__ float to_score(float scale, int up) {
+        return fminf(fmaxf(ldexpf(scale * kLog2e, 24 - up), FLT_MIN), FLT_MAX);
     }
 };
 
@@ -324,8 +327,10 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
     {
         const int col = min(col0 + r % RP, cols - 1), qi = col / a.group;
         Queries<D> mq;
-        mq.load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
-        to_score = mq.to_score;
+        mq.load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4));
+        const int up = Queries<D>::exponent(mq.amax);
+        mq.finish(up);
+        to_score = Queries<D>::to_score(a.scale, up);
 #pragma unroll
         for (int i = 0; i < KK; ++i)
             if (wave == 0) shared_q[i][lane] = mq.op[i];
@@ -563,29 +568,38 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
   } while (true);
 }
 
+// what a scheduling group holds
+constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
+
 // --------------------------------------------------------------------------
 // Many columns: keys and values of 64 tokens at a time in LDS, as operands.
 // --------------------------------------------------------------------------
-// NW waves of 32 columns each.  S^T = K Q^T: a lane holds four neighbouring tokens
+// Eight waves of 32 columns each.  S^T = K Q^T: a lane holds four neighbouring tokens
 // of one query, which is what the second product, O^T = V^T P^T, takes from it.
 // Keys are staged as codes (subnormal numbers), their scales and minima, in fp32,
 // act on the scores; values are staged as fp16 values, rounded once.  A stage is
 // converted by the whole workgroup while the one before is in use, from registers
-// loaded one stage earlier still; every conversion then serves 32 NW columns.
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a) {
-    constexpr int KK = D / 32, VT = D / 16, C = 2, WaveCols = 16 * C, Cols = WaveCols * NW, ValueLanes = 128 * (D / 64);
+// loaded one stage earlier still; every conversion then serves 256 columns.
+//
+// The vector unit bounds it (an exponential takes it four times as long as
+// another operation): a score is brought under its column's running maximum by
+// the two multiply-adds that scale it, score - m = acc sk + (zk sum(q) - m), and
+// the sum of the weights, as rounded, is one more row of the second product.
+template <typename T, int D>
+__global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
+    constexpr int KK = D / 32, VT = D / 16, C = 2, WaveCols = 16 * C, NW = 8, Cols = WaveCols * NW;
     struct Stage {
         f16x8 k[4][KK][64];                                 // tile, operand, lane
         f16x8 v[2][VT][64];                                 // two tiles, operand, lane
         f32x2 kp[64];                                       // token: scale, minimum
     };
     __shared__ __attribute__((aligned(16))) Stage stages[2];
+    __shared__ float largest[NW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     // The last columns, which see most, first; the blocks of a head's columns on one XCD where heads allow; the
     // sequences of a round one further on than in the round before, as workgroups go to the parts of an XCD in turn
-    // (four ragged sequences, always in the same order: 500 us, XX).
+    // (four ragged sequences, always in the same order: 500 us, 299).
     const int blocks = (a.max_q * a.group + Cols - 1) / Cols, pairs = a.sequences * a.c.heads;
     const int round = blockIdx.x / pairs, pair = blockIdx.x % pairs, head = pair % a.c.heads, b = (pair / a.c.heads + round) % a.sequences;
     const int block0 = (blocks - 1 - round) * Cols;
@@ -597,44 +611,46 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
     const bool mine = col0 < cols;
     const int low = mine ? visible(a, s, col0 / a.group) : 0, high = mine ? visible(a, s, (min(col0 + WaveCols, cols) - 1) / a.group) : 0;
 
-    // Loads of a stage: wave w has the keys of tile w, wave w (of eight: w - 4) the values of channels (D / 16) r +
-    // 4 (w % (D / 64)) .. of tiles 2 (w / (D / 64)) and one on, and their parameters; wave 0 those of the keys.
-    const int key_tile = wave, value_item = NW == 8 ? wave - 4 : wave;
-    const bool has_keys = wave < 4, has_values = value_item >= 0 && value_item < ValueLanes / 64;
-    const int value_tile = value_item / (D / 64) * 2, value_word = value_item % (D / 64);
+    // Loads of a stage: wave w < 4 has the keys of tile w; wave 4 + w the values of channels (D / 16) r + 4 (w %
+    // (D / 64)) .. of tiles 2 (w / (D / 64)) and one on, and their parameters; wave 0 those of the keys.  (The same
+    // work for every wave is slower, 8 contexts of 4096 tokens by 2048 queries 914 us, 870: of the two waves of a
+    // SIMD one is through with its share earlier, and the one's products meet the other's vector work.)
+    const int value_item = wave - 4;
+    const bool has_keys = wave < 4, has_values = value_item >= 0 && value_item < D / 32;
+    const int key_tile = wave, value_tile = value_item / (D / 64) * 2, value_word = value_item % (D / 64);
     uint32_t raw_k[D / 32], raw_v[2][2], raw_kp = 0, raw_vp = 0;
     u32x4 raw_p[2];
     int table = 0;                                          // lane h: page of tile h
     auto load_table = [&](int t) {
         const int at = min(t + 16 * (lane & 3), end - 1);
-        table = a.table[(int64_t)b * a.table_pages + (max(at, 0) >> a.c.page_bits)];
+        table = a.table[(int64_t)b * a.table_pages + (at >> a.c.page_bits)];
     };
-    auto page_row = [&](int page, int t) { return tile_row(a, head, page, t); };
     int page[4] = {};
     auto load = [&](int t) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) page[h] = __builtin_amdgcn_readlane(table, h);
         if (has_keys) {
-            const int64_t row = page_row(key_tile == 0 ? page[0] : key_tile == 1 ? page[1] : key_tile == 2 ? page[2] : page[3], t + 16 * key_tile);
+            const int64_t row = tile_row(a, head, key_tile == 0 ? page[0] : key_tile == 1 ? page[1] : key_tile == 2 ? page[2] : page[3], t + 16 * key_tile);
             __builtin_memcpy(raw_k, __builtin_assume_aligned(a.c.k + row * (D / 2) + (uint32_t)(r * (D / 2) + g * (D / 8)), D / 8), D / 8);
         }
         if (has_values) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t row = page_row(value_tile == 0 ? page[h] : page[2 + h], t + 16 * (value_tile + h));
+                const int64_t row = tile_row(a, head, value_tile == 0 ? page[h] : page[2 + h], t + 16 * (value_tile + h));
                 __builtin_memcpy(raw_v[h], __builtin_assume_aligned(a.c.v + row * (D / 2) + (uint32_t)(g * (2 * D) + r * (D / 8) + 8 * value_word), 8), 8);
                 raw_p[h] = *reinterpret_cast<const u32x4*>(a.c.vp + row + 4 * g);
             }
         }
         if (wave == 0) {                                    // lane: token
-            int64_t row = page_row(page[0], t);
+            int64_t row = tile_row(a, head, page[0], t);
 #pragma unroll
             for (int h = 1; h < 4; ++h)
-                if (g == h) row = page_row(page[h], t + 16 * h);
+                if (g == h) row = tile_row(a, head, page[h], t + 16 * h);
             raw_kp = a.c.kp[row + r];
             raw_vp = a.c.vp[row + r];
         }
     };
+    float to_score = 0.0f;                                  // the workgroup's
     auto finite = [](uint32_t p) { return (p & 0x7C00u) != 0x7C00u; };     // both parameters are NaN, or none
     auto convert = [&](Stage& st, int t) {
         if (has_keys) {
@@ -643,19 +659,30 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
         }
         if (has_values) {
             u32x4 w[4];                                     // channel of the word: four pairs of tokens
+            uint32_t p[2][4];
+            u16x2 most{};                                   // the largest scale, as its bits
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t p[4];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = raw_p[h][e];
-                    // a row that is not finite weighs on the scores (below); a weight of 0 leaves it out here
-                    if (!finite(p[e]) || t + 16 * (value_tile + h) + 4 * g + e >= s.n) p[e] = 0;
+                    p[h][e] = raw_p[h][e];
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[h][e]));
                 }
+            // a row that is not finite weighs on the scores (below), where a weight of 0 leaves it out; and what
+            // memory holds past the end
+            if (__any(most[0] >= 0x7C00) || t + kStep > s.n) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!finite(p[h][e]) || t + 16 * (value_tile + h) + 4 * g + e >= s.n) p[h][e] = 0;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const f16x2 sv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u));
-                    const f16x2 zv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u));
+                    const f16x2 sv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[h][2 * k + 1], p[h][2 * k], 0x05040100u));
+                    const f16x2 zv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[h][2 * k + 1], p[h][2 * k], 0x07060302u));
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
                         const uint32_t code = ((raw_v[h][k] >> (4 * n)) & 0x000F000Fu) | 0x64006400u;   // 1024 + n
@@ -670,30 +697,42 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
         if (wave == 0) {
             const f16x2 k = __builtin_bit_cast(f16x2, raw_kp);
             // a value row that is not finite makes the score NaN, for the queries that see it
-            st.kp[lane] = f32x2{(float)k[0], finite(raw_vp) ? (float)k[1] : NAN};
+            st.kp[lane] = f32x2{(float)k[0] * to_score, finite(raw_vp) ? (float)k[1] * to_score : NAN};
         }
     };
 
     Queries<D> q[C];
     int limit[C];
-    load_table(0);
-    load(0);
-    load_table(kStep);
+    if (end > 0) {                                          // (of no tokens there may be no table)
+        load_table(0);
+        load(0);
+        load_table(kStep);
+    }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
         const int col = min(col0 + 16 * j + r, cols - 1), qi = col / a.group;
         limit[j] = visible(a, s, qi);
-        q[j].load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4), a.scale);
+        q[j].load(static_cast<const T*>(a.q) + (s.q0 + qi) * a.q_token + (head * a.group + col % a.group) * a.q_head + g * (D / 4));
     }
+    float amax = fmaxf(q[0].amax, q[1].amax);
+    if (lane == 0) largest[wave] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) amax = fmaxf(amax, largest[i]);
+    const int up = Queries<D>::exponent(amax);
+    to_score = Queries<D>::to_score(a.scale, up);
+#pragma unroll
+    for (int j = 0; j < C; ++j) q[j].finish(up);
     // (kept here: the compiler would make the operands again in every step that has work)
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
         for (int i = 0; i < KK; ++i) asm volatile("" : "+v"(q[j].op[i]));
-    f32x4 acc[C][VT] = {};
-    float m[C], l[C] = {};
+    f32x4 acc[C][VT] = {}, sums[C] = {};
+    float m[C] = {}, most[C];                               // scores are taken less m; above `most` of that m moves
 #pragma unroll
-    for (int j = 0; j < C; ++j) m[j] = kLowest;
+    for (int j = 0; j < C; ++j) most[j] = -INFINITY;        // to the first score that there is, then by more than kSlack
+    const f16x8 ones = (f16x8)(_Float16)1.0f;
 
     int now[4];                                             // pages of the stage in use
     auto turn = [&](int t) {                                // the stage at t from registers to LDS, the one after into registers
@@ -706,7 +745,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
         }
         __syncthreads();
     };
-    turn(0);
+    if (end > 0) turn(0);
     for (int t = 0; t < end; t += kStep) {
         const Stage& st = stages[t / kStep & 1];
         if (t < high) {
@@ -726,8 +765,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
                 for (int e = 0; e < 4; ++e) {
                     const f32x2 kp = st.kp[16 * h + 4 * g + e];
 #pragma unroll
-                    for (int j = 0; j < C; ++j) x[j][h][e] = __builtin_fmaf(x[j][h][e], kp[0], kp[1] * q[j].of_minimum);
+                    for (int j = 0; j < C; ++j) x[j][h][e] = __builtin_fmaf(x[j][h][e], kp[0], __builtin_fmaf(kp[1], q[j].of_minimum, -m[j]));
                 }
+            // operands are read two tiles ahead of their products (read as they are needed, LDS is waited for each time)
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
             if (t + kStep > low || !there(a, now[0]) || !there(a, now[1]) || !there(a, now[2]) || !there(a, now[3])) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
@@ -746,15 +794,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top[j] = fmaxf(top[j], x[j][h][e]);
-                top[j] *= q[j].to_score;
-                moves = moves || top[j] > m[j] + kSlack;
+                moves = moves || top[j] > most[j];
             }
             if (__any(moves)) {
 #pragma unroll
                 for (int j = 0; j < C; ++j) {
-                    const float to = fmaxf(m[j], quads_max(top[j])), down = __builtin_amdgcn_exp2f(m[j] - to);
-                    m[j] = to;
-                    l[j] *= down;
+                    const float to = quads_max(top[j]), by = to > most[j] ? to : 0.0f;
+                    const float down = most[j] == kSlack ? __builtin_amdgcn_exp2f(-by) : 1.0f;  // (before: sums of nothing)
+                    most[j] = to > most[j] ? kSlack : most[j];
+                    m[j] += by;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) x[j][h] -= by;
+                    sums[j] *= down;
 #pragma unroll
                     for (int i = 0; i < VT; ++i) acc[j][i] *= down;
                 }
@@ -764,30 +815,36 @@ __global__ __launch_bounds__(64 * NW, 2) void attention4_wide_kernel(Attn4Args a
             for (int j = 0; j < C; ++j)
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    f32x4 w;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][h][e], q[j].to_score, -m[j]));
-                        l[j] += w[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) p[j][h / 2][4 * (h % 2) + e] = (_Float16)w[e];
+                    for (int e = 0; e < 4; ++e) p[j][h / 2][4 * (h % 2) + e] = (_Float16)__builtin_amdgcn_exp2f(x[j][h][e]);
                 }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) sums[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[j][h], sums[j], 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < VT; ++i) {
                     const f16x8 v = st.v[h][i][lane];
 #pragma unroll
                     for (int j = 0; j < C; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[j][h], acc[j][i], 0, 0, 0);
                 }
+            }
+            // half of the value operands are read before the exponentials, the others beside the products
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, VT, 0);
+            __builtin_amdgcn_sched_group_barrier(kVector, 12 * C, 0);
+#pragma unroll
+            for (int i = 0; i < VT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, C, 0);
+                __builtin_amdgcn_sched_group_barrier(kVector, 12 * C / VT, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+            }
         }
         if (t + kStep < end) turn(t + kStep);
     }
 
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const float sum = quads_sum(l[j]);
+        const float sum = sums[j][0];
         if (col0 + 16 * j + r < cols) {
 #pragma unroll
             for (int c = 0; c < D / 4; c += 4) {
@@ -864,9 +921,9 @@ struct Plan4 {
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
-    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 128;
+    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 256;
     const int64_t units = (int64_t)sequences * heads * ((cols + p.columns - 1) / p.columns), steps = (max_kv + kStep - 1) / kStep;
-    p.whole = steps <= 16 || p.columns == 128;
+    p.whole = steps <= 16 || p.columns == 256;
     const int64_t shares = (units * steps + kLeastSteps - 1) / kLeastSteps, resident = p.columns > 8 ? 512 : 768;
     p.groups = p.whole ? units : shares < resident ? shares : resident;
     return p;
@@ -930,7 +987,7 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
                 hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(256), 0, stream, a);
                 if (!p.whole) hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
             };
-            if (p.columns == 128) hipLaunchKernelGGL((attention4_wide_kernel<T, D, 4>), dim3((unsigned)p.groups), dim3(256), 0, stream, a);
+            if (p.columns == 256) hipLaunchKernelGGL((attention4_wide_kernel<T, D>), dim3((unsigned)p.groups), dim3(512), 0, stream, a);
             else if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
             else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>, attention4_join_kernel<T, D, 8>);
             else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>, attention4_join_kernel<T, D, 4>);
