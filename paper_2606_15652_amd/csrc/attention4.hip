@@ -19,7 +19,10 @@
 #include "kv4.h"
 
 #include <float.h>
+#include <limits.h>
 #include <math.h>
+
+#include <algorithm>
 
 namespace mq {
 
@@ -54,7 +57,8 @@ struct Attn4Args {
     float scale;
     int causal;
     float *part_o, *part_m, *part_l;    // results of parts of a row's tokens: [place][column] (x D); null: whole rows only
-    int32_t* starts;                    // [sequence] first step of each among all, [sequences] steps of a workgroup
+    int32_t* starts;                    // few columns: [sequence] first step of each among all, [sequences] steps of a workgroup
+    int splits, split_steps;            // many columns: parts of a unit and their steps
 };
 
 // The launch writes none of these arrays: reads by uniform indexes go through the scalar cache, beside the
@@ -177,7 +181,7 @@ __device__ __forceinline__ Work4 work4(const Attn4Args& a, const Sequence& s) {
 // keep: with RP = 4 a lane ends up with one token (16 g + r) and all the columns
 // in its registers.  A row of 16 columns for four queries would leave three lanes
 // of four with nothing (the work on scores, parameters and weights was half of
-// the kernel: a batch of 64 contexts of up to 8191 tokens 70 us, this XX).
+// the kernel: a batch of 64 contexts of up to 8191 tokens 70 us, 65).
 // The weights cross to the lanes of the second product, O^T = V^T P^T, through LDS.
 //
 // Weights are held as multiples of `scale` (at least every sv), w = p sv / scale,
@@ -601,15 +605,20 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     // sequences of a round one further on than in the round before, as workgroups go to the parts of an XCD in turn
     // (four ragged sequences, always in the same order: 500 us, 299).
     const int blocks = (a.max_q * a.group + Cols - 1) / Cols, pairs = a.sequences * a.c.heads;
-    const int round = blockIdx.x / pairs, pair = blockIdx.x % pairs, head = pair % a.c.heads, b = (pair / a.c.heads + round) % a.sequences;
+    const int unit = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int round = unit / pairs, pair = unit % pairs, head = pair % a.c.heads, b = (pair / a.c.heads + round) % a.sequences;
     const int block0 = (blocks - 1 - round) * Cols;
     const Sequence s = sequence(a, b);
     const int cols = s.nq * a.group;
     if (block0 >= cols) return;
-    const int end = visible(a, s, (min(block0 + Cols, cols) - 1) / a.group);
+    const int all = visible(a, s, (min(block0 + Cols, cols) - 1) / a.group);
+    const int begin = (int)min((int64_t)split * a.split_steps * kStep, (int64_t)INT_MAX - kStep);
+    if (split > 0 && begin >= all) return;                  // split 0 is there for rows of no tokens, too
+    const int end = min(all, begin + a.split_steps * kStep);
     const int col0 = block0 + wave * WaveCols;
     const bool mine = col0 < cols;
-    const int low = mine ? visible(a, s, col0 / a.group) : 0, high = mine ? visible(a, s, (min(col0 + WaveCols, cols) - 1) / a.group) : 0;
+    const int low = mine ? visible(a, s, col0 / a.group) : 0;
+    const int high = mine ? min(end, visible(a, s, (min(col0 + WaveCols, cols) - 1) / a.group)) : 0;
 
     // Loads of a stage: wave w < 4 has the keys of tile w; wave 4 + w the values of channels (D / 16) r + 4 (w %
     // (D / 64)) .. of tiles 2 (w / (D / 64)) and one on, and their parameters; wave 0 those of the keys.  (The same
@@ -703,10 +712,10 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
 
     Queries<D> q[C];
     int limit[C];
-    if (end > 0) {                                          // (of no tokens there may be no table)
-        load_table(0);
-        load(0);
-        load_table(kStep);
+    if (begin < end) {                                      // (of no tokens there may be no table)
+        load_table(begin);
+        load(begin);
+        load_table(begin + kStep);
     }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
@@ -745,8 +754,8 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
         }
         __syncthreads();
     };
-    if (end > 0) turn(0);
-    for (int t = 0; t < end; t += kStep) {
+    if (begin < end) turn(begin);
+    for (int t = begin; t < end; t += kStep) {
         const Stage& st = stages[t / kStep & 1];
         if (t < high) {
             f32x4 x[C][4] = {};
@@ -846,12 +855,18 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     for (int j = 0; j < C; ++j) {
         const float sum = sums[j][0];
         if (col0 + 16 * j + r < cols) {
+            const int64_t place = (int64_t)blockIdx.x * Cols + wave * WaveCols + 16 * j + r;
 #pragma unroll
             for (int c = 0; c < D / 4; c += 4) {
                 f32x4 o;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[k] = acc[j][(c + k) % VT][(c + k) / VT];
-                store_output<T>(a, s, head, col0 + 16 * j + r, g * (D / 4) + c, o, sum);
+                if (a.splits == 1) store_output<T>(a, s, head, col0 + 16 * j + r, g * (D / 4) + c, o, sum);
+                else *reinterpret_cast<f32x4*>(a.part_o + place * D + g * (D / 4) + c) = o;
+            }
+            if (a.splits > 1 && g == 0) {
+                a.part_m[place] = most[j] == kSlack ? m[j] : kLowest;
+                a.part_l[place] = sum;
             }
         }
     }
@@ -908,28 +923,73 @@ __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Args a) {
     store_output<T>(a, s, head, col, 4 * at, o, sum);
 }
 
+// The same for many columns, where the parts are few and the rows many: D / 4 lanes a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention4_join_wide_kernel(Attn4Args a, int rows) {
+    constexpr int Lanes = D / 4, Cols = 256;
+    const int row = blockIdx.x * (256 / Lanes) + threadIdx.x / Lanes, at = threadIdx.x % Lanes;
+    if (row >= rows) return;
+    const int heads = a.c.heads * a.group, hq = row % heads, qi = row / heads % a.max_q, b = row / heads / a.max_q;
+    const Sequence s = sequence(a, b);
+    if (qi >= s.nq) return;
+    const int head = hq / a.group, col = qi * a.group + hq % a.group, block = col / Cols;
+    // the kernel's order of units, and the parts that had tokens
+    const int blocks = (a.max_q * a.group + Cols - 1) / Cols, round = blocks - 1 - block;
+    const int turn = ((b - round) % a.sequences + a.sequences) % a.sequences;
+    const int64_t place = (int64_t)((round * a.sequences + turn) * a.c.heads + head) * a.splits * Cols + col % Cols;
+    const int all = visible(a, s, (min((block + 1) * Cols, s.nq * a.group) - 1) / a.group);
+    const int parts = max(1, min(a.splits, ((all + kStep - 1) / kStep + a.split_steps - 1) / a.split_steps));
+    f32x4 o = {};
+    float mx = kLowest, sum = 0.0f;
+    for (int i = 0; i < parts; ++i) {
+        const int64_t p = place + i * Cols;
+        const float m = a.part_m[p], to = fmaxf(mx, m), down = __builtin_amdgcn_exp2f(mx - to), by = __builtin_amdgcn_exp2f(m - to);
+        o = o * down + *reinterpret_cast<const f32x4*>(a.part_o + p * D + 4 * at) * by;
+        sum = sum * down + a.part_l[p] * by;
+        mx = to;
+    }
+    store_output<T>(a, s, head, col, 4 * at, o, sum);
+}
+
 // ---------------------------------------------------------------- host side --
 struct Plan4 {
-    int columns;                        // of a workgroup: up to 16, 256
+    int columns;                        // of a workgroup: up to 16, or 256
     int64_t groups;
     bool whole;                         // a workgroup takes whole units
+    int splits, split_steps;            // 256 columns
 };
 
-// Workgroups of a launch.  Short sequences (up to 1024 tokens: 16 steps, four for
-// each wave) are taken whole; the others are cut into as many equal shares as
-// workgroups fit on the chip, or shares of four steps if those are fewer.
+// Workgroups of a launch.  Few columns: short sequences (up to 1024 tokens: 16
+// steps, four for each wave) are taken whole; the others are cut into as many
+// equal shares as workgroups fit on the chip, or shares of four steps if those are
+// fewer.  Many columns: units are split while there are fewer than CUs, into parts
+// of at least eight steps (four contexts of 4096 tokens by 128 queries XX us, in one part 127).
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
     p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 256;
     const int64_t units = (int64_t)sequences * heads * ((cols + p.columns - 1) / p.columns), steps = (max_kv + kStep - 1) / kStep;
-    p.whole = steps <= 16 || p.columns == 256;
+    p.splits = 1;
+    p.split_steps = (int)std::max<int64_t>(steps, 1);
+    if (p.columns == 256) {
+        const int64_t splits = std::min<int64_t>(256 / std::max<int64_t>(units, 1), steps / 8);
+        if (splits > 1) {
+            p.split_steps = (int)((steps + splits - 1) / splits);
+            p.splits = (int)((steps + p.split_steps - 1) / p.split_steps);
+        }
+        p.whole = p.splits == 1;
+        p.groups = units * p.splits;
+        return p;
+    }
+    p.whole = steps <= 16;
     const int64_t shares = (units * steps + kLeastSteps - 1) / kLeastSteps, resident = p.columns > 8 ? 512 : 768;
-    p.groups = p.whole ? units : shares < resident ? shares : resident;
+    p.groups = p.whole ? units : std::min(shares, resident);
     return p;
 }
+// places of partial results
+static int64_t places4(const Plan4& p) { return p.whole ? 0 : p.groups * p.columns * (p.columns == 256 ? 1 : 2); }
 static size_t workspace4(const Plan4& p, int sequences, int head_dim) {
-    const size_t floats = p.whole ? 0 : (size_t)p.groups * 2 * p.columns * (head_dim + 2) + (size_t)sequences + 1;
+    const size_t floats = p.whole ? 0 : (size_t)places4(p) * (head_dim + 2) + (size_t)sequences + 1;
     return (floats * sizeof(float) + 15) / 16 * 16;
 }
 
@@ -972,29 +1032,32 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
     const size_t need = mq_attention_kv4_workspace_size(sequences, tokens, cache->heads, group, cache->head_dim, max_q, max_kv);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     float* part = p.whole ? nullptr : static_cast<float*>(workspace);
-    const int64_t rows = p.groups * 2 * p.columns;
+    const int64_t rows = places4(p);
     const Attn4Args a{device_cache4(cache), Q, O, q_token, q_head, o_token, o_head, page_table, table_pages, (int)max_kv, kv_lens, cu_q,
                       sequences, tokens, group, max_q, scale, causal != 0, part, part ? part + rows * cache->head_dim : nullptr,
                       part ? part + rows * (cache->head_dim + 1) : nullptr,
-                      part ? reinterpret_cast<int32_t*>(part + rows * (cache->head_dim + 2)) : nullptr};
+                      part ? reinterpret_cast<int32_t*>(part + rows * (cache->head_dim + 2)) : nullptr, p.splits, p.split_steps};
     const int64_t joins = (int64_t)sequences * max_q * cache->heads * group;
     if (p.groups > INT32_MAX || joins > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
-        auto run = [&](auto d) {
+        auto with_dim = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            auto few = [&](auto kernel, auto join) {
+            auto run = [&](auto kernel, auto join) {
                 hipLaunchKernelGGL(kernel, dim3((unsigned)p.groups), dim3(256), 0, stream, a);
                 if (!p.whole) hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, stream, a);
             };
-            if (p.columns == 256) hipLaunchKernelGGL((attention4_wide_kernel<T, D>), dim3((unsigned)p.groups), dim3(512), 0, stream, a);
-            else if (p.columns == 16) few(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
-            else if (p.columns == 8) few(attention4_kernel<T, D, 8, 4>, attention4_join_kernel<T, D, 8>);
-            else if (max_q * group > 2) few(attention4_kernel<T, D, 4, 4>, attention4_join_kernel<T, D, 4>);
-            else if (max_q * group > 1) few(attention4_kernel<T, D, 4, 2>, attention4_join_kernel<T, D, 4>);
-            else few(attention4_kernel<T, D, 4, 1>, attention4_join_kernel<T, D, 4>);
+            if (p.columns == 256) {
+                hipLaunchKernelGGL((attention4_wide_kernel<T, D>), dim3((unsigned)p.groups), dim3(512), 0, stream, a);
+                const int64_t blocks = (joins + 1024 / D - 1) / (1024 / D);
+                if (!p.whole) hipLaunchKernelGGL((attention4_join_wide_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, stream, a, (int)joins);
+            } else if (p.columns == 16) run(attention4_kernel<T, D, 16, 4>, attention4_join_kernel<T, D, 16>);
+            else if (p.columns == 8) run(attention4_kernel<T, D, 8, 4>, attention4_join_kernel<T, D, 8>);
+            else if (max_q * group > 2) run(attention4_kernel<T, D, 4, 4>, attention4_join_kernel<T, D, 4>);
+            else if (max_q * group > 1) run(attention4_kernel<T, D, 4, 2>, attention4_join_kernel<T, D, 4>);
+            else run(attention4_kernel<T, D, 4, 1>, attention4_join_kernel<T, D, 4>);
             return mq_host::launch_status();
         };
-        return cache->head_dim == 64 ? run(std::integral_constant<int, 64>{}) : run(std::integral_constant<int, 128>{});
+        return cache->head_dim == 64 ? with_dim(std::integral_constant<int, 64>{}) : with_dim(std::integral_constant<int, 128>{});
     });
 }

@@ -100,6 +100,13 @@ def test_long_prompts():
     check([700], [600], 1, 2, 128, 64, torch.bfloat16)
 
 
+@pytest.mark.parametrize("lens,nqs", [([1100, 513, 0, 64], [70, 65, 3, 64]), ([4100], [66]), ([2000, 700, 20], [1, 65, 20])])
+def test_prompts_split_over_the_chip(lens, nqs):
+    """Few workgroups of many columns, cut along the tokens; sequences that reach one part, several or none."""
+    check(lens, nqs, 1, 2, 64, 32, torch.float16)
+    check(lens, nqs, 2, 1, 128, 16, torch.bfloat16)
+
+
 def test_bounds_given_by_the_host():
     q, cache, seqs, cu, o = check([30, 500, 77], [3, 7, 1], 2, 4, 128, 16, torch.float16, max_q=7, max_kv=500)
     m = mq()
