@@ -68,8 +68,9 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
             src, proc = running.pop(0)
             _, err = proc.communicate()
             if proc.returncode != 0:
-                for _, p in running:
-                    p.wait()
+                for _, p in running:        # not waited for: one whose warnings fill its pipe would never end
+                    p.kill()
+                    p.communicate()
                 raise RuntimeError(f"hipcc failed on {os.path.basename(src)} ({proc.returncode}):\n{err}")
             err = "\n".join(l for l in err.splitlines() if not any(n in l for n in _NOISE))
             if verbose and err.strip():

@@ -963,7 +963,7 @@ struct Plan4 {
 // steps, four for each wave) are taken whole; the others are cut into as many
 // equal shares as workgroups fit on the chip, or shares of four steps if those are
 // fewer.  Many columns: units are split while there are fewer than CUs, into parts
-// of at least eight steps (four contexts of 4096 tokens by 128 queries XX us, in one part 127).
+// of at least eight steps (four contexts of 4096 tokens by 128 queries 60 us, in one part 127).
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;

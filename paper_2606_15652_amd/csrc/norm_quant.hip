@@ -7,15 +7,22 @@
 // h and gamma have at most 11 significant bits, so t is exact in fp32, and in
 // rows (fp32 scales) y / s = 127 t / max|t| does not depend on rho at all.  The
 // row stays in registers from its one read to its codes; sum of squares and
-// maximum are reduced together.
+// maximum are reduced together.  The sum, and what is made of it for the row, are
+// fp64 (the scale is rounded to fp32, and in the A8 layout from there to fp16), and a code is
+// rounded from one fp32 rounding of its quotient, multiplied as two parts: memory
+// bounds the kernel, which leaves room for both.
 #include "mq_float.h"
+
+#include <math.h>
+
+#include <algorithm>
 
 namespace mq {
 
 constexpr int kNormMaxThreads = 1024;
 
 // Sum of v over the wave, in a fixed order; every lane has the result.
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
     return v;
@@ -34,12 +41,12 @@ template <typename T, bool NORM, bool A8, int P>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
     const T* X, const T* R, const T* __restrict__ gamma, T* H, int M, int K,
     int64_t ldx, int64_t ldr, int64_t ldh, float eps, uint8_t* __restrict__ Xq, int64_t ldq, void* __restrict__ s_x) {
-    __shared__ float sums[kNormMaxThreads / 64];
+    __shared__ double sums[kNormMaxThreads / 64];
     __shared__ uint32_t maxima[kNormMaxThreads / 64];
     const int m = blockIdx.x, t = threadIdx.x, threads = blockDim.x;
 
     f32x8 v[P][2];
-    float sum = 0.0f;
+    double sum = 0.0;
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -62,7 +69,10 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(v[i][e][j], v[i][e][j], sum);
+                for (int j = 0; j < 8; ++j) {
+                    const double h = (double)v[i][e][j];
+                    sum = __builtin_fma(h, h, sum);
+                }
                 v[i][e] *= g[e];
             }
         }
@@ -79,27 +89,29 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
             sums[t >> 6] = sum;
         }
         __syncthreads();
-        sum = 0.0f;
+        sum = 0.0;
         for (int w = 0; w < threads / 64; ++w) {
             amax = max(amax, maxima[w]);
             sum += sums[w];
         }
     }
-    const float rho = NORM ? 1.0f / sqrtf(sum / (float)K + eps) : 1.0f;
+    const double rho = NORM ? 1.0 / sqrt(sum / (double)K + (double)eps) : 1.0;
     const float top = __uint_as_float(amax);
-    float s = top * rho / (float)kQmax8;
-    bool finite = amax < kFloatInf && (!NORM || (__float_as_uint(sum) & 0x7FFFFFFFu) < kFloatInf);
-    float inv;                                              // codes are t inv, rounded
+    const double exact = (double)top * rho / (double)kQmax8;
+    bool finite = amax < kFloatInf && (!NORM || (float)sum < INFINITY);
+    double inv;                                             // codes are t inv, rounded
     if constexpr (A8) {
-        const uint16_t sb = float_to_half_bits(s);
+        const uint16_t sb = float_to_half_bits((float)exact);
+        const float s = half_bits_to_float(sb);
         finite = finite && sb < kHalfInf;
-        s = half_bits_to_float(sb);
-        inv = s == 0.0f ? 0.0f : rho / s;
+        inv = s == 0.0f ? 0.0 : rho / (double)s;
         if (t == 0) static_cast<uint16_t*>(s_x)[m] = finite ? sb : (uint16_t)0x7E00;
     } else {
-        inv = s == 0.0f ? 0.0f : (float)kQmax8 / top;
+        const float s = (float)exact;
+        inv = s == 0.0f ? 0.0 : (double)kQmax8 / (double)top;
         if (t == 0) static_cast<float*>(s_x)[m] = finite ? s : __uint_as_float(0x7FC00000u);
     }
+    const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
         const int k = 16 * (t + i * threads);
@@ -107,7 +119,8 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
         float q[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float c = __builtin_amdgcn_fmed3f(rintf(v[i][e / 8][e % 8] * inv) + 0.0f, -127.0f, 127.0f);   // no -0
+            const float x = v[i][e / 8][e % 8];
+            const float c = __builtin_amdgcn_fmed3f(rintf(__builtin_fmaf(x, inv_hi, x * inv_lo)) + 0.0f, -127.0f, 127.0f);   // no -0
             q[e] = finite ? c : 0.0f;
         }
         if constexpr (A8) {
@@ -140,15 +153,13 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
     }
 }
 
-// y = rn(s q): eight values a thread
+// y = rn(s q): eight values a thread, `chunks` workgroups a row
 template <typename T, bool A8>
 __global__ __launch_bounds__(256) void dequant_act8_kernel(const uint8_t* __restrict__ Xq, int64_t ldq,
-                                                           const void* __restrict__ s_x, int M, int K,
+                                                           const void* __restrict__ s_x, int M, int K, int chunks,
                                                            T* __restrict__ Y, int64_t ldy) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per = K / 8;
-    if (i >= (int64_t)M * per) return;
-    const int m = (int)(i / per), k = 8 * (int)(i % per);
+    const int m = blockIdx.x / chunks, k = 8 * (blockIdx.x % chunks * blockDim.x + threadIdx.x);
+    if (k >= K) return;
     f32x8 v;
     float s;
     if constexpr (A8) {
@@ -248,13 +259,13 @@ extern "C" mq_status mq_dequantize_act8(int M, int K, mq_act8_layout layout, con
     if (M == 0) return MQ_OK;
     if (!Y) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(Y, 16)) return MQ_ERR_MISALIGNED;
-    const int64_t blocks = ((int64_t)M * (K / 8) + 255) / 256;
-    if (blocks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const int threads = std::min((K / 8 + 63) / 64 * 64, 256), chunks = (K / 8 + threads - 1) / threads;
+    if ((int64_t)M * chunks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, static_cast<const uint8_t*>(Xq8),
-                               ldq, s_x, M, K, static_cast<T*>(Y), ldy);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(M * chunks)), dim3(threads), 0, stream, static_cast<const uint8_t*>(Xq8),
+                               ldq, s_x, M, K, chunks, static_cast<T*>(Y), ldy);
             return mq_host::launch_status();
         };
         return layout == MQ_ACT8_A8 ? run(dequant_act8_kernel<T, true>) : run(dequant_act8_kernel<T, false>);

@@ -44,26 +44,30 @@ def _empty(shape, dtype, device, stream):
 
 def _need_rows(t, name, cols=None):
     """A matrix with contiguous rows (any row stride): its row stride."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{name} must be [rows, {'columns' if cols is None else cols}], got shape {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    shape = t.shape
+    if len(shape) != 2 or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name} must be [rows, {'columns' if cols is None else cols}], got shape {tuple(shape)}")
+    row, col = t.stride()
+    if col != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return row if shape[0] > 1 else max(row, shape[1])
 
 
 def _same_device(first, name, **others):
+    at = first.get_device()
     for other, t in others.items():
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != at:
             raise ValueError(f"{other} is on {t.device}, {name} on {first.device}")
 
 
 # ------------------------------------------------- 8-bit activations --
 def _code_rows(M, K, device, stream):
-    """int8 [M, K], rows padded to 16 bytes."""
-    return _empty((M, -(-K // 16) * 16), _torch().int8, device, stream)[:, :K]
+    """int8 [M, K], rows padded to 16 bytes, and their stride."""
+    ld = -(-K // 16) * 16
+    rows = _empty((M, ld), _torch().int8, device, stream)
+    return (rows if ld == K else rows[:, :K]), ld
 
 
 def _need_codes(Xq8, K=None):
@@ -79,7 +83,7 @@ def _need_codes(Xq8, K=None):
         ld = max(padded, ld - ld % 16)          # one row: its stride says nothing
     if ld < padded or ld % 16:
         raise ValueError(f"Xq8's rows must start every multiple of 16 bytes, at least {padded}; got a row stride of {ld}")
-    if M and Xq8.storage_offset() + (M - 1) * ld + padded > Xq8.untyped_storage().nbytes():
+    if padded != K and M and Xq8.storage_offset() + (M - 1) * ld + padded > Xq8.untyped_storage().nbytes():
         raise ValueError("Xq8's last row must be followed by its padding to 16 bytes")
     return ld
 
@@ -93,32 +97,38 @@ def rms_norm_quantize8(X, weight, eps: float = 1e-6, residual=None, layout: str 
     code = _dtype_code(getattr(X, "dtype", None), "X")
     ldx = _need_rows(X, "X")
     M, K = X.shape
-    _need(weight, X.dtype, "weight", 1)
-    if weight.shape[0] != K:
-        raise ValueError(f"weight must have {K} values, got {weight.shape[0]}")
-    a8 = LAYOUTS[layout] == 1
+    _need_out(weight, (K,), X.dtype, "weight")
+    a8, H, ldq, ldr, ldh = LAYOUTS[layout] == 1, None, 0, 0, 0
+    if residual is not None:
+        if residual.dtype != X.dtype:
+            raise TypeError(f"residual must be {X.dtype}, got {residual.dtype}")
+        ldr = _need_rows(residual, "residual", K)
+        if residual.shape[0] != M:
+            raise ValueError(f"residual must have {M} rows, got {residual.shape[0]}")
     if out is None:
         dev = X.device
-        Xq8 = _empty((M, 3 * K // 2), torch.uint8, dev, stream) if a8 else _code_rows(M, K, dev, stream)
+        if a8:
+            Xq8 = _empty((M, 3 * K // 2), torch.uint8, dev, stream)
+        else:
+            Xq8, ldq = _code_rows(M, K, dev, stream)
         s_x = _empty((M,), torch.float16 if a8 else torch.float32, dev, stream)
-        H = None if residual is None else _empty((M, K), X.dtype, dev, stream)
+        if residual is not None:
+            H, ldh = _empty((M, K), X.dtype, dev, stream), K
+        _same_device(X, "X", weight=weight, residual=residual)
     else:
         Xq8, s_x, H = (*out, None) if residual is None else out
         _need_out(s_x, (M,), torch.float16 if a8 else torch.float32, "out[1] (s_x)")
         if a8:
             _need_out(Xq8, (M, 3 * K // 2), torch.uint8, "out[0] (Xq8)")
-    ldq = 0 if a8 else _need_codes(Xq8, K)
-    if not a8 and Xq8.shape[0] != M:
-        raise ValueError(f"out[0] (Xq8) must have {M} rows, got {Xq8.shape[0]}")
-    ldr = ldh = 0
-    if residual is not None:
-        for t, name in ((residual, "residual"), (H, "out[2] (H)")):
-            if t.dtype != X.dtype:
-                raise TypeError(f"{name} must be {X.dtype}, got {t.dtype}")
-            if t.shape[0] != M:
-                raise ValueError(f"{name} must have {M} rows, got {t.shape[0]}")
-        ldr, ldh = _need_rows(residual, "residual", K), _need_rows(H, "out[2] (H)", K)
-    _same_device(X, "X", weight=weight, residual=residual, Xq8=Xq8, s_x=s_x, H=H)
+        else:
+            ldq = _need_codes(Xq8, K)
+            if Xq8.shape[0] != M:
+                raise ValueError(f"out[0] (Xq8) must have {M} rows, got {Xq8.shape[0]}")
+        if residual is not None:
+            ldh = _need_rows(H, "out[2] (H)", K)
+            if H.dtype != X.dtype or H.shape[0] != M:
+                raise ValueError(f"out[2] (H) must be {X.dtype} with {M} rows, got {H.dtype} with {H.shape[0]}")
+        _same_device(X, "X", weight=weight, residual=residual, Xq8=Xq8, s_x=s_x, H=H)
     _check("mq_rms_norm_quantize8", load().mq_rms_norm_quantize8(
         M, K, code, X.data_ptr(), ldx, _ptr(residual), ldr, weight.data_ptr(), eps, _ptr(H), ldh, LAYOUTS[layout],
         Xq8.data_ptr(), ldq, s_x.data_ptr(), _stream(stream)))
@@ -131,13 +141,16 @@ def quantize_rows8(X, out=None, stream=None):
     code = _dtype_code(getattr(X, "dtype", None), "X")
     ldx = _need_rows(X, "X")
     M, K = X.shape
-    Xq8, s_x = out if out is not None else (_code_rows(M, K, X.device, stream),
-                                            _empty((M,), torch.float32, X.device, stream))
-    ldq = _need_codes(Xq8, K)
-    if Xq8.shape[0] != M:
-        raise ValueError(f"out[0] (Xq8) must have {M} rows, got {Xq8.shape[0]}")
-    _need_out(s_x, (M,), torch.float32, "out[1] (s_x)")
-    _same_device(X, "X", Xq8=Xq8, s_x=s_x)
+    if out is None:
+        Xq8, ldq = _code_rows(M, K, X.device, stream)
+        s_x = _empty((M,), torch.float32, X.device, stream)
+    else:
+        Xq8, s_x = out
+        ldq = _need_codes(Xq8, K)
+        if Xq8.shape[0] != M:
+            raise ValueError(f"out[0] (Xq8) must have {M} rows, got {Xq8.shape[0]}")
+        _need_out(s_x, (M,), torch.float32, "out[1] (s_x)")
+        _same_device(X, "X", Xq8=Xq8, s_x=s_x)
     _check("mq_quantize_rows8", load().mq_quantize_rows8(M, K, code, X.data_ptr(), ldx, Xq8.data_ptr(), ldq,
                                                          s_x.data_ptr(), _stream(stream)))
     return Xq8, s_x
