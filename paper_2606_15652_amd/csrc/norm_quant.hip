@@ -8,9 +8,11 @@
 // rows (fp32 scales) y / s = 127 t / max|t| does not depend on rho at all.  The
 // row stays in registers from its one read to its codes; sum of squares and
 // maximum are reduced together.  The sum, and what is made of it for the row, are
-// fp64 (the scale is rounded to fp32, and in the A8 layout from there to fp16), and a code is
-// rounded from one fp32 rounding of its quotient, multiplied as two parts: memory
-// bounds the kernel, which leaves room for both.
+// fp64 (the scale is rounded to fp32, and in the A8 layout from there to fp16, as
+// the other quantisers' are), and a code is rounded from one fp32 rounding of its
+// quotient, multiplied as two parts: memory bounds the kernel, which leaves room
+// for both.  8192 rows of 8192 with residual: 105-115 us, 4.1-4.5 TB/s of the 4.9 that a copy
+// reaches; their values read back: 69 us.
 #include "mq_float.h"
 
 #include <math.h>
@@ -101,7 +103,9 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
     bool finite = amax < kFloatInf && (!NORM || (float)sum < INFINITY);
     double inv;                                             // codes are t inv, rounded
     if constexpr (A8) {
-        const uint16_t sb = float_to_half_bits((float)exact);
+        float single = (float)exact;
+        asm("" : "+v"(single));                             // two roundings: contracted, they would be one
+        const uint16_t sb = float_to_half_bits(single);
         const float s = half_bits_to_float(sb);
         finite = finite && sb < kHalfInf;
         inv = s == 0.0f ? 0.0 : rho / (double)s;
