@@ -28,13 +28,7 @@ __device__ __forceinline__ int64_t row_index(const Cache4& c, int64_t slot, int 
     const int64_t page = slot >> c.page_bits;
     return ((page * c.heads + head) << c.page_bits) + (slot & ((1 << c.page_bits) - 1));
 }
-// dword of 8 codes of one token's key
-__device__ __forceinline__ uint32_t key_word(const uint32_t (&n)[8]) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w |= n[j] << (4 * (j / 2) + 16 * (j % 2));
-    return w;
-}
+// code of channel j of the eight in a key's dword
 __device__ __forceinline__ uint32_t key_code(uint32_t w, int j) { return (w >> (4 * (j / 2) + 16 * (j % 2))) & 15u; }
 // byte offset, in a page and head's values, of the 16-bit word of four channels 4 f .. 4 f + 3 of a token
 template <int D>

@@ -10,11 +10,14 @@
 // whatever X holds past K adds nothing.
 //
 // Two kernels:
-//  * tiled: output tiles of 256 x 256 or 128 x 128, both operands through two
-//    LDS slots of 128 codes, filled by the LDS DMA;
+//  * tiled: output tiles of 64 x 64 to 256 x 256, both operands through two to
+//    four LDS slots of 128 codes, filled by the LDS DMA.  The matrix unit and LDS
+//    bound it: 8192 rows of 8192 codes by 28672 channels 1480-1540 us, 2.5-2.6
+//    POP/s (63 % of the cycles have a product running);
 //  * streaming (few rows): weights go straight to registers, once; the eight
 //    waves of a workgroup share out K and add their sums in LDS (integers: in
-//    any order).
+//    any order).  Reading the weight bounds it: 4096 -> 14336 at one row 10.2 us,
+//    5.7 TB/s.
 #include "lds_dma.h"
 #include "mq_float.h"
 

@@ -163,3 +163,24 @@ def test_refusals():
     ]:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_ties_and_their_neighbours(D, dtype):
+    """Halves of a step go to the even code, their neighbours in the row's type to the nearer one."""
+    m = mq()
+    T, H = 512, 4
+    g = so.generator(D, 9)
+    step = torch.randint(64, 128, (T, H, 1), generator=g).float() * 2.0 ** -torch.randint(0, 12, (T, H, 1), generator=g)
+    low = -step * torch.randint(0, 16, (T, H, 1), generator=g)                  # exact in fp16 and, up to 8 bits, in bf16
+    half = torch.randint(0, 15, (T, H, D), generator=g) + 0.5
+    half[..., 0], half[..., D - 1] = 0.0, 15.0                                  # the minimum and the maximum
+    x = (low + step * half).to(dtype)
+    bits = x.view(torch.int16)
+    bits[..., 1:D - 1] += torch.randint(-1, 2, (T, H, D - 2), generator=g).to(torch.int16)
+    cache = m.kv4_cache(T // 16, 16, H, D)
+    slots = torch.arange(T)
+    m.kv4_append(cache, x.cuda(), x.flip(0).cuda(), slots.cuda())
+    gk, gv = m.kv4_read(cache, slots.cuda(), torch.float16)
+    assert torch.equal(gk.cpu(), so.values4(x).half()) and torch.equal(gv.cpu(), so.values4(x.flip(0)).half())
