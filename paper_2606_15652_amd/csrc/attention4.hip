@@ -30,6 +30,7 @@ mq_status check_cache4(const mq_kv4_cache* c);
 Cache4 device_cache4(const mq_kv4_cache* c);
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -581,14 +582,23 @@ constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
 // Eight waves of 32 columns each.  S^T = K Q^T: a lane holds four neighbouring tokens
 // of one query, which is what the second product, O^T = V^T P^T, takes from it.
 // Keys are staged as codes (subnormal numbers), their scales and minima, in fp32,
-// act on the scores; values are staged as fp16 values, rounded once.  A stage is
+// act on the scores.  A value z + s n = m (b (n - 7.5) + (z + 7.5 s) / m), where b
+// is the power of two and m the mantissa of s (b = s, m = 1 below fp16's normal
+// range, where steps of 2^-25 are below what s resolves): b (n - 7.5), exact in fp16,
+// is staged; the weight w = p m comes out of the
+// exponential, as log2 m over the key's scale is where the scores' sums begin, and is
+// rounded to fp16; 1 / m and (z + 7.5 s) / m, each as two fp16 numbers, are four rows
+// more of the second product.  The weights' rounding is thus the only one, and the
+// same above and below the fraction: fp16 results are off by 2.7e-4 of their norm,
+// 2.1e-4 of it their own rounding (values staged as fp16 values: 3.3e-4, four ragged
+// prompts of up to 2047 tokens 275 us, 288).  A stage is
 // converted by the whole workgroup while the one before is in use, from registers
 // loaded one stage earlier still; every conversion then serves 256 columns.
 //
 // The vector unit bounds it (an exponential takes it four times as long as
 // another operation): a score is brought under its column's running maximum by
 // the two multiply-adds that scale it, score - m = acc sk + (zk sum(q) - m), and
-// the sum of the weights, as rounded, is one more row of the second product.
+// the sums are rows of the second product.
 template <typename T, int D>
 __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     constexpr int KK = D / 32, VT = D / 16, C = 2, WaveCols = 16 * C, NW = 8, Cols = WaveCols * NW;
@@ -596,6 +606,8 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
         f16x8 k[4][KK][64];                                 // tile, operand, lane
         f16x8 v[2][VT][64];                                 // two tiles, operand, lane
         f32x2 kp[64];                                       // token: scale, minimum
+        float up[64];                                       // token: log2 m over the key's scale
+        _Float16 rest[4][64];                               // token: 1 / m, what fp16 leaves of it, the middle / m, as well
     };
     __shared__ __attribute__((aligned(16))) Stage stages[2];
     __shared__ float largest[NW];
@@ -690,12 +702,15 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const f16x2 sv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[h][2 * k + 1], p[h][2 * k], 0x05040100u));
-                    const f16x2 zv = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(p[h][2 * k + 1], p[h][2 * k], 0x07060302u));
+                    const uint32_t sv = __builtin_amdgcn_perm(p[h][2 * k + 1], p[h][2 * k], 0x05040100u);
+                    // the scale's power of two; a subnormal scale whole
+                    const u16x2 power = __builtin_elementwise_max(__builtin_bit_cast(u16x2, sv & 0x7C007C00u),
+                                                                  __builtin_elementwise_min(__builtin_bit_cast(u16x2, sv), (u16x2)(uint16_t)0x3FF));
 #pragma unroll
                     for (int n = 0; n < 4; ++n) {
-                        const uint32_t code = ((raw_v[h][k] >> (4 * n)) & 0x000F000Fu) | 0x64006400u;   // 1024 + n
-                        const f16x2 v = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, code) - (f16x2)(_Float16)1024.0f, sv, zv);
+                        const uint32_t raw = n == 0 ? raw_v[h][k] << 3 : raw_v[h][k] >> (4 * n - 3);
+                        const uint32_t code = (raw & 0x00780078u) | 0x58005800u;                        // 128 + n
+                        const f16x2 v = (__builtin_bit_cast(f16x2, code) - (f16x2)(_Float16)135.5f) * __builtin_bit_cast(f16x2, power);
                         w[n][2 * h + k] = __builtin_bit_cast(uint32_t, v);
                     }
                 }
@@ -706,7 +721,19 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
         if (wave == 0) {
             const f16x2 k = __builtin_bit_cast(f16x2, raw_kp);
             // a value row that is not finite makes the score NaN, for the queries that see it
-            st.kp[lane] = f32x2{(float)k[0] * to_score, finite(raw_vp) ? (float)k[1] * to_score : NAN};
+            float sk = (float)k[0] * to_score;
+            sk = fabsf(sk) < 0x1p-100f ? 0x1p-100f : sk;    // (no score comes of it, and it has a reciprocal)
+            st.kp[lane] = f32x2{sk, finite(raw_vp) ? (float)k[1] * to_score : NAN};
+            const uint32_t vp = finite(raw_vp) && t + lane < s.n ? raw_vp : 0;
+            const float sv = half_bits_to_float((uint16_t)vp), middle = __builtin_fmaf(sv, 7.5f, half_bits_to_float((uint16_t)(vp >> 16)));
+            const float mantissa = (vp & 0x7C00u) ? __uint_as_float(0x3F800000u | (vp & 0x3FFu) << 13) : 1.0f;
+            const float inv = __builtin_amdgcn_rcpf(mantissa), rest[2] = {inv, middle * inv};
+            st.up[lane] = __builtin_amdgcn_logf(mantissa) * __builtin_amdgcn_rcpf(sk);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                st.rest[2 * i][lane] = (_Float16)rest[i];
+                st.rest[2 * i + 1][lane] = (_Float16)(rest[i] - (float)(_Float16)rest[i]);
+            }
         }
     };
 
@@ -741,7 +768,6 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     float m[C] = {}, most[C];                               // scores are taken less m; above `most` of that m moves
 #pragma unroll
     for (int j = 0; j < C; ++j) most[j] = -INFINITY;        // to the first score that there is, then by more than kSlack
-    const f16x8 ones = (f16x8)(_Float16)1.0f;
 
     int now[4];                                             // pages of the stage in use
     auto turn = [&](int t) {                                // the stage at t from registers to LDS, the one after into registers
@@ -758,9 +784,11 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     for (int t = begin; t < end; t += kStep) {
         const Stage& st = stages[t / kStep & 1];
         if (t < high) {
-            f32x4 x[C][4] = {};
+            f32x4 x[C][4];
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) x[j][h] = *reinterpret_cast<const f32x4*>(st.up + 16 * h + 4 * g);
 #pragma unroll
                 for (int i = 0; i < KK; ++i) {
                     const f16x8 k = st.k[h][i][lane];
@@ -777,7 +805,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
                     for (int j = 0; j < C; ++j) x[j][h][e] = __builtin_fmaf(x[j][h][e], kp[0], __builtin_fmaf(kp[1], q[j].of_minimum, -m[j]));
                 }
             // operands are read two tiles ahead of their products (read as they are needed, LDS is waited for each time)
-            __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * KK, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * KK + 4, 0);
             __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
             __builtin_amdgcn_sched_group_barrier(kLdsReads, KK, 0);
             __builtin_amdgcn_sched_group_barrier(kProducts, C * KK, 0);
@@ -829,8 +857,10 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
                 }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                const _Float16* at = st.rest[r & 3] + 32 * h + 4 * g;
+                const f16x8 rest = __builtin_shufflevector(*reinterpret_cast<const f16x4*>(at), *reinterpret_cast<const f16x4*>(at + 16), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int j = 0; j < C; ++j) sums[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[j][h], sums[j], 0, 0, 0);
+                for (int j = 0; j < C; ++j) sums[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rest, p[j][h], sums[j], 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < VT; ++i) {
                     const f16x8 v = st.v[h][i][lane];
@@ -839,7 +869,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
                 }
             }
             // half of the value operands are read before the exponentials, the others beside the products
-            __builtin_amdgcn_sched_group_barrier(kLdsReads, VT, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, VT + 2, 0);
             __builtin_amdgcn_sched_group_barrier(kVector, 12 * C, 0);
 #pragma unroll
             for (int i = 0; i < VT; ++i) {
@@ -853,14 +883,14 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
 
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const float sum = sums[j][0];
+        const float sum = sums[j][0] + sums[j][1], middle = sums[j][2] + sums[j][3];
         if (col0 + 16 * j + r < cols) {
             const int64_t place = (int64_t)blockIdx.x * Cols + wave * WaveCols + 16 * j + r;
 #pragma unroll
             for (int c = 0; c < D / 4; c += 4) {
                 f32x4 o;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[k] = acc[j][(c + k) % VT][(c + k) / VT];
+                for (int k = 0; k < 4; ++k) o[k] = acc[j][(c + k) % VT][(c + k) / VT] + middle;
                 if (a.splits == 1) store_output<T>(a, s, head, col0 + 16 * j + r, g * (D / 4) + c, o, sum);
                 else *reinterpret_cast<f32x4*>(a.part_o + place * D + g * (D / 4) + c) = o;
             }

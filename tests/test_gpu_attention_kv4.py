@@ -282,3 +282,19 @@ def test_refusals():
     ]:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq", [1, 40])
+@pytest.mark.parametrize("scale", [0.125, 1e-30])
+def test_scales_of_every_size(nq, dtype, scale):
+    """Values without spread, with a scale below fp16's normal range (an absolute 2^-25 of rounding, the tolerance
+    2^-22), on a power of two, large and ordinary; keys without spread; one kind a sequence."""
+    def prepare(seqs):
+        g = so.generator(nq, 3)
+        for b, size in enumerate([0.0, 2.0 ** -11, 15.0 / 8, 15 * 2.0 ** 10, 1.0]):
+            ramp = torch.rand(77, 2, 64, generator=g)
+            ramp[..., 0], ramp[..., 1] = 0.0, 1.0
+            seqs.v[b] = ((ramp - 0.5) * size + (0.75 if b == 0 else 0.0)).to(dtype)
+        seqs.k[4] = seqs.k[4][..., :1].repeat(1, 1, 64)
+    check([77] * 5, [nq] * 5, 2, 4, 64, 16, dtype, seed=nq, scale=scale, prepare=prepare)
