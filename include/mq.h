@@ -477,7 +477,7 @@ mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ldx, const fl
  * power of two, 16 .. 65536) of every key head; head_dim is 64 or 128.  A slot
  * is page * page_size + the place in the page.  Each row of a token and head has
  * a scale s and a minimum z, both fp16, and codes n in [0, 15]:
- *     z = fp16_rn(min x), s = fp16_rn((max x - z) / 15),
+ *     z = fp16_rn(min x), s = fp16_rn(max(max x - z, 0) / 15),
  *     n = clamp(round_half_even((x - z) / s), 0, 15)     (0 if s == 0),
  * in fp32; the value is z + s n.  A row that holds infinity or NaN, or whose z or
  * s passes fp16's range, has the parameters NaN.

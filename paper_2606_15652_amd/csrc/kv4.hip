@@ -1,6 +1,6 @@
 // Keys and values of new tokens into the paged 4-bit cache, and back.
 //
-//   z = fp16(min x),  s = fp16((max x - z) / 15),  n = clamp(round_half_even((x - z) / s), 0, 15)
+//   z = fp16(min x),  s = fp16(max(max x - z, 0) / 15),  n = clamp(round_half_even((x - z) / s), 0, 15)
 //
 // for each row of a token and head; the value that a code stands for is z + s n.
 #include "kv4.h"
@@ -50,7 +50,8 @@ __device__ __forceinline__ uint32_t quantise4(const f32x8 x, float (&n)[8]) {
     const bool row_finite = ((bad >> (lane & ~(LANES - 1))) & ((1u << LANES) - 1)) == 0;
     const uint16_t zb = float_to_half_bits(lo);
     const float z = half_bits_to_float(zb);
-    const uint16_t sb = float_to_half_bits((hi - z) / 15.0f);
+    // z may be rounded past every value of a bf16 row: no spread is left then, and the scale is +0
+    const uint16_t sb = float_to_half_bits(fmaxf(hi - z, 0.0f) / 15.0f) & 0x7FFFu;
     const float s = half_bits_to_float(sb);
     const bool ok = row_finite && (zb & 0x7FFFu) < kHalfInf && sb < kHalfInf;
     const float inv = __builtin_amdgcn_rcpf(s);

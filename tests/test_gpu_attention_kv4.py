@@ -298,3 +298,14 @@ def test_scales_of_every_size(nq, dtype, scale):
             seqs.v[b] = ((ramp - 0.5) * size + (0.75 if b == 0 else 0.0)).to(dtype)
         seqs.k[4] = seqs.k[4][..., :1].repeat(1, 1, 64)
     check([77] * 5, [nq] * 5, 2, 4, 64, 16, dtype, seed=nq, scale=scale, prepare=prepare)
+
+
+@pytest.mark.parametrize("nqs", [None, [40, 20]])
+def test_rows_without_spread_below_a_step_of_fp16(nqs):
+    """bf16 rows whose minimum rounds up past their maximum in fp16 (scale 0) are rows like others."""
+    def prepare(seqs):
+        for b in range(2):
+            for t, size in ((0, 1e-6), (7, -1e-10), (18, 1e-7)):
+                seqs.k[b][t], seqs.v[b][t] = size, -size
+    _, _, _, _, o = check([70, 20], nqs, 2, 4, 64, 16, torch.bfloat16, prepare=prepare)
+    assert torch.isfinite(o).all()

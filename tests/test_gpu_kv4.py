@@ -184,3 +184,22 @@ def test_ties_and_their_neighbours(D, dtype):
     m.kv4_append(cache, x.cuda(), x.flip(0).cuda(), slots.cuda())
     gk, gv = m.kv4_read(cache, slots.cuda(), torch.float16)
     assert torch.equal(gk.cpu(), so.values4(x).half()) and torch.equal(gv.cpu(), so.values4(x.flip(0)).half())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_whose_minimum_rounds_above_their_maximum(D):
+    """fp16 lifts the minimum of such a row past every value: it has no spread left, scale 0 and the value z."""
+    m = mq()
+    sizes = [1e-6, 1e-7, -1e-10, -1e-6, 3e-8, 5e-5, -0.0, 0.0]
+    x = torch.tensor(sizes)[:, None, None].repeat(1, 2, D).bfloat16()
+    x[5, 0] = torch.linspace(4.000e-5, 4.002e-5, D).bfloat16()                  # a few values, less than a step apart
+    x[7, :, ::2] = -0.0                                                         # zeros of both signs
+    n, s, z = so.quantise4(x)
+    assert not s.any() and not n.any() and ((z - x.float().amax(-1, keepdim=True)) > 0)[:2].all()
+    cache = m.kv4_cache(1, 16, 2, D)
+    slots = torch.arange(len(sizes)).cuda()
+    m.kv4_append(cache, x.cuda(), x.flip(0).cuda(), slots)
+    for params in (cache.k_params, cache.v_params):
+        assert not params[..., 0].view(torch.int16).any()                       # +0, not a negative zero
+    gk, gv = m.kv4_read(cache, slots, torch.bfloat16)
+    assert torch.equal(gk.cpu(), so.values4(x).bfloat16()) and torch.equal(gv.cpu(), so.values4(x.flip(0)).bfloat16())
