@@ -573,6 +573,8 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
   } while (true);
 }
 
+constexpr uint16_t kMostPower = 0x7000;     // 2^13 in fp16: the largest power of two by which codes are staged
+
 // what a scheduling group holds
 constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
 
@@ -584,11 +586,12 @@ constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
 // Keys are staged as codes (subnormal numbers), their scales and minima, in fp32,
 // act on the scores.  A value z + s n = m (b (n - 7.5) + (z + 7.5 s) / m), where b
 // is the power of two and m the mantissa of s (b = s, m = 1 below fp16's normal
-// range, where steps of 2^-25 are below what s resolves): b (n - 7.5), exact in fp16,
-// is staged; the weight w = p m comes out of the
-// exponential, as log2 m over the key's scale is where the scores' sums begin, and is
-// rounded to fp16; 1 / m and (z + 7.5 s) / m, each as two fp16 numbers, are four rows
-// more of the second product.  The weights' rounding is thus the only one, and the
+// range, where steps of 2^-25 are below what s resolves; b = 2^13, m up to 8 above 2^13,
+// so that 7.5 b is in fp16's range): b (n - 7.5), exact in fp16, is staged; the weight
+// w = p m comes out of the exponential, as log2 m over the key's scale is where the
+// scores' sums begin, and is rounded to fp16; 1 / m and (z + 7.5 s) / m, each as two
+// fp16 numbers, are four rows more of the second product (of the latter a 16th and what
+// that leaves: it passes fp16's range, as z + 15 s may in bf16).  The weights' rounding is thus the only one, and the
 // same above and below the fraction: fp16 results are off by 2.7e-4 of their norm,
 // 2.1e-4 of it their own rounding (values staged as fp16 values: 3.3e-4, four ragged
 // prompts of up to 2047 tokens 275 us, 288).  A stage is
@@ -607,7 +610,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
         f16x8 v[2][VT][64];                                 // two tiles, operand, lane
         f32x2 kp[64];                                       // token: scale, minimum
         float up[64];                                       // token: log2 m over the key's scale
-        _Float16 rest[4][64];                               // token: 1 / m, what fp16 leaves of it, the middle / m, as well
+        _Float16 rest[4][64];                               // token: 1 / m, what fp16 leaves of it, the middle / 16 m as well
     };
     __shared__ __attribute__((aligned(16))) Stage stages[2];
     __shared__ float largest[NW];
@@ -690,13 +693,15 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
                     most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, p[h][e]));
                 }
             // a row that is not finite weighs on the scores (below), where a weight of 0 leaves it out; and what
-            // memory holds past the end
-            if (__any(most[0] >= 0x7C00) || t + kStep > s.n) {
+            // memory holds past the end; scales from 2^13 on have the power 2^13
+            if (__any(most[0] >= kMostPower) || t + kStep > s.n) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!finite(p[h][e]) || t + 16 * (value_tile + h) + 4 * g + e >= s.n) p[h][e] = 0;
+                    for (int e = 0; e < 4; ++e) {
+                        const bool none = !finite(p[h][e]) || t + 16 * (value_tile + h) + 4 * g + e >= s.n;
+                        p[h][e] = none ? 0 : min(p[h][e] & 0xFFFFu, (uint32_t)kMostPower);
+                    }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -726,13 +731,16 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
             st.kp[lane] = f32x2{sk, finite(raw_vp) ? (float)k[1] * to_score : NAN};
             const uint32_t vp = finite(raw_vp) && t + lane < s.n ? raw_vp : 0;
             const float sv = half_bits_to_float((uint16_t)vp), middle = __builtin_fmaf(sv, 7.5f, half_bits_to_float((uint16_t)(vp >> 16)));
-            const float mantissa = (vp & 0x7C00u) ? __uint_as_float(0x3F800000u | (vp & 0x3FFu) << 13) : 1.0f;
+            const float mantissa = (vp & 0x7C00u) >= kMostPower ? sv * 0x1p-13f
+                                 : (vp & 0x7C00u) ? __uint_as_float(0x3F800000u | (vp & 0x3FFu) << 13) : 1.0f;
             const float inv = __builtin_amdgcn_rcpf(mantissa), rest[2] = {inv, middle * inv};
             st.up[lane] = __builtin_amdgcn_logf(mantissa) * __builtin_amdgcn_rcpf(sk);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                st.rest[2 * i][lane] = (_Float16)rest[i];
-                st.rest[2 * i + 1][lane] = (_Float16)(rest[i] - (float)(_Float16)rest[i]);
+                const float units = i == 0 ? 1.0f : 16.0f;
+                const _Float16 high = (_Float16)(rest[i] * (1.0f / units));
+                st.rest[2 * i][lane] = high;
+                st.rest[2 * i + 1][lane] = (_Float16)__builtin_fmaf((float)high, -units, rest[i]);
             }
         }
     };
@@ -883,7 +891,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
 
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const float sum = sums[j][0] + sums[j][1], middle = sums[j][2] + sums[j][3];
+        const float sum = sums[j][0] + sums[j][1], middle = __builtin_fmaf(sums[j][2], 16.0f, sums[j][3]);
         if (col0 + 16 * j + r < cols) {
             const int64_t place = (int64_t)blockIdx.x * Cols + wave * WaveCols + 16 * j + r;
 #pragma unroll

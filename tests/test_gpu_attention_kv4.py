@@ -309,3 +309,25 @@ def test_rows_without_spread_below_a_step_of_fp16(nqs):
                 seqs.k[b][t], seqs.v[b][t] = size, -size
     _, _, _, _, o = check([70, 20], nqs, 2, 4, 64, 16, torch.bfloat16, prepare=prepare)
     assert torch.isfinite(o).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nqs", [None, [90, 40]])
+def test_values_past_fp16s_range(nqs, dim):
+    """bf16 value rows that the format holds (minimum and scale fit fp16), of values that do not: those who see them
+    get them, those who do not get what they get without them."""
+    large = {70: (6e4, 3e5), 75: (-6e4, 9e5), 80: (65000.0, 1e5), 85: (-65000.0, -20000.0), 88: (6.5e4, 6.5e4)}
+
+    def prepare(seqs):
+        g = so.generator(dim, 21)
+        for b in range(2):
+            for t, (lo, hi) in large.items():
+                row = torch.rand(2, dim, generator=g)
+                row[:, 0], row[:, 1] = 0.0, 1.0
+                seqs.v[b][t] = (lo + (hi - lo) * row).bfloat16()
+    q, _, seqs, cu, o = check([90, 90], nqs, 2, 4, dim, 16, torch.bfloat16, prepare=prepare)
+    assert torch.isfinite(o).all()
+    if nqs:                                                 # queries 0 .. 69 of the first sequence see none of them
+        k, v = so.values4(seqs.k[0])[:70], so.values4(seqs.v[0])[:70]
+        want = so.attention(q[:70], k, v, 1 / math.sqrt(dim), True)
+        assert ((o[:70].double() - want).abs() <= so.attention_error(q[:70], k, v, 1 / math.sqrt(dim), torch.bfloat16, want)).all()
