@@ -404,8 +404,9 @@ typedef enum mq_act8_layout { MQ_ACT8_ROWS = 0, MQ_ACT8_A8 = 1 } mq_act8_layout;
  *     y = h gamma / sqrt(mean_k(h^2) + eps),
  *     s_x[m] = max_k |y| / 127   (fp32; in the A8 layout rounded to fp16),
  *     q = clamp(round_half_even(y / s_x), -127, 127)          (0 if s_x == 0).
- * Everything between h and the codes is fp32.  A row that is not finite (a value
- * of h or of h gamma, or the sum of squares, in fp32) has the scale NaN and codes 0.
+ * Products h gamma are fp32, sums, the root and the scale before its rounding fp64.
+ * A row that is not finite (a value of h or of h gamma, or the sum of squares, in
+ * fp32; zeros where eps is 0) has the scale NaN and codes 0.
  *   type     : of X, R, gamma and H: MQ_FP16 or MQ_BF16.
  *   X, R, H  : [M, ldx], [M, ldr], [M, ldh], leading dimensions >= K and
  *              multiples of 8, 16-byte aligned.  R may be NULL (H is NULL then);

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
     const double rho = NORM ? 1.0 / sqrt(sum / (double)K + (double)eps) : 1.0;
     const float top = __uint_as_float(amax);
     const double exact = (double)top * rho / (double)kQmax8;
-    bool finite = amax < kFloatInf && (!NORM || (float)sum < INFINITY);
+    bool finite = amax < kFloatInf && (!NORM || (float)sum < INFINITY) && exact == exact;   // (0 / 0: zeros, and no eps)
     double inv;                                             // codes are t inv, rounded
     if constexpr (A8) {
         float single = (float)exact;
@@ -112,8 +112,16 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_quant_kernel(
         if (t == 0) static_cast<uint16_t*>(s_x)[m] = finite ? sb : (uint16_t)0x7E00;
     } else {
         const float s = (float)exact;
-        inv = s == 0.0f ? 0.0 : (double)kQmax8 / (double)top;
+        // a subnormal scale has too few bits for 127 / max to be the same
+        inv = s == 0.0f ? 0.0 : s < 0x1p-126f ? rho / (double)s : (double)kQmax8 / (double)top;
         if (t == 0) static_cast<float*>(s_x)[m] = finite ? s : __uint_as_float(0x7FC00000u);
+    }
+    if (inv > 0x1p64) {                                     // rows so small that fp32 may not hold it, 2^165 at most
+        inv *= 0x1p-64;
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v[i][e] *= 0x1p64f;
     }
     const float inv_hi = (float)inv, inv_lo = (float)(inv - (double)inv_hi);
 #pragma unroll

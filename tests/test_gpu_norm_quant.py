@@ -178,3 +178,52 @@ def test_scales_are_rounded_to_single_first():
     twice = s64.numpy().astype(np.float32).astype(np.float16)
     assert (twice != s64.numpy().astype(np.float16)).any()  # the rows tell
     assert np.array_equal(s.numpy(), twice)
+
+
+@pytest.mark.parametrize("size", [1e-36, 1e-37, 2e-38, 1e-38, 1e-39, 1e-40])
+def test_tiny_rows(size):
+    """bf16 rows down to fp32's subnormal numbers, where 127 over the largest value passes fp32's range: the codes are
+    those of the scale that is held."""
+    m = mq()
+    x = so.acts(6, 520, torch.float32, 11) * 0.01
+    x = (x / x.abs().amax(-1, keepdim=True) * size).bfloat16()
+    codes, s = m.quantize_rows8(x.cuda())
+    held = x.double().abs().amax(-1) / 127
+    assert ((s.cpu().double() - held).abs() <= 2.0 ** -23 * held + 2.0 ** -149).all() and (s > 0).all()
+    held = s.cpu().double()
+    off = (codes.cpu().double() - (x.double() / held[:, None]).clamp(-127, 127)).abs()
+    assert off.max() <= 0.5 + 127 * 4 * 2.0 ** -23, off.max()
+
+
+@pytest.mark.parametrize("layout", ["rows", "a8"])
+@pytest.mark.parametrize("eps,x_size,g_size", [(1e-5, 1e-30, 1e-8), (1e-5, 1e-20, 1e-17), (0.0, 1e-37, 1.0), (0.0, 1e-20, 1e-17)])
+def test_tiny_products(eps, x_size, g_size, layout):
+    """Norms whose h gamma is below 3.7e-37, with and without an eps that hides the row."""
+    m = mq()
+    x = (so.acts(5, 512, torch.float32, 12) * x_size).bfloat16()
+    gamma = ((1 + 0.2 * torch.randn(512, generator=so.generator(512, 13))) * g_size).bfloat16()
+    codes, s = m.rms_norm_quantize8(x.cuda(), gamma.cuda(), eps, layout=layout)
+    codes = (m.unpack_act8(codes) if layout == "a8" else codes).cpu().double()
+    eps = float(np.float32(eps))
+    _, y = so.norm(x, gamma, eps)
+    top = (x.double() * gamma.double()).abs().amax(-1)
+    # h gamma has an absolute 2^-150 of fp32's subnormal numbers; beside it the roundings of the other norms' test
+    rel = (64 + 10 + 8) * 2.0 ** -24 + 2.0 ** -150 / top
+    s64 = y.abs().amax(-1) / 127
+    assert ((s.cpu().double() - s64).abs() <= ((2.0 ** -11 if layout == "a8" else 0.0) + rel) * s64
+            + (2.0 ** -25 if layout == "a8" else 2.0 ** -149)).all()
+    held = s.cpu().double()
+    ratio = torch.where(held[:, None] > 0, y / torch.where(held > 0, held, 1.0)[:, None], torch.zeros_like(y)).clamp(-127, 127)
+    off = (codes - ratio).abs()
+    assert (off <= 0.5 + 127 * (rel + 4 * 2.0 ** -23)[:, None] + (127 * 2.0 ** -149 / held)[:, None].nan_to_num(0, 0, 0)).all(), off.max()
+
+
+@pytest.mark.parametrize("layout", ["rows", "a8"])
+def test_zeros_without_eps(layout):
+    """0 / 0: such a row is not finite, and its codes are 0."""
+    m = mq()
+    x = so.acts(3, 256, torch.float16, 14)
+    x[1] = 0
+    codes, s = m.rms_norm_quantize8(x.cuda(), torch.ones(256).half().cuda(), 0.0, layout=layout)
+    codes = m.unpack_act8(codes) if layout == "a8" else codes
+    assert torch.isnan(s[1]) and not codes[1].any() and torch.isfinite(s[[0, 2]]).all() and codes[[0, 2]].abs().amax() == 127
