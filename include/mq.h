@@ -461,7 +461,8 @@ mq_status mq_unpack_weight8(int N, int K, const uint8_t* Wq8, int8_t* Wc, int ld
  * fp32, multiplied by s_x s_w there, and the result once to `type`.
  *   Xq8, s_x  : int8 [M, ldx], ldx >= K rounded up to 16, ldx % 16 == 0, 16-byte
  *               aligned; a row's bytes between K and that are read and count for
- *               nothing.  s_x fp32 [M].
+ *               nothing; (min(M, 32) - 1) ldx + K <= 2^31 - 16 (M <= 16: 2^32 - 16).
+ *               s_x fp32 [M].
  *   Wq8, s_w  : library layout, fp32 [N].
  *   type      : of bias (may be NULL) and Y: MQ_FP16, MQ_BF16 or MQ_FP32.
  *   Y         : out, [M, ldy], ldy >= N, aligned to its type.

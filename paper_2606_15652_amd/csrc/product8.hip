@@ -28,6 +28,7 @@ namespace mq {
 constexpr int kBlock8 = 64;             // channels of a block
 constexpr int kPieceK = 64, kPieceBytes = 1024;
 constexpr int kStageK = 128;            // codes of a slot; K is padded to a multiple
+constexpr int kWaveRows = 32;           // rows of X at most that a wave loads: they span less than 2 GB (streaming kernel: 4)
 
 struct Product8Args {
     int M, N, K;
@@ -102,7 +103,7 @@ template <typename T, int WM, int WN, int MI, int SLOTS, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product8Args a, int per_split, int* __restrict__ part) {
     constexpr int TM = 16 * MI * WM, TN = kBlock8 * WN, NW = WM * WN;
     constexpr int XL = TM / 8 / NW, WL = TN / 8 / NW;       // 1 KB loads of a wave and stage
-    static_assert(XL * NW * 8 == TM && (WL == 2 || WL == 4), "whole loads");
+    static_assert(XL * NW * 8 == TM && 8 * XL <= kWaveRows && (WL == 2 || WL == 4), "whole loads");
     __shared__ __attribute__((aligned(16))) struct {
         uint8_t x[SLOTS][TM * kStageK];
         uint8_t w[SLOTS][TN * kStageK];
@@ -115,12 +116,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product8_tiled_kernel(Product
     tile_coords(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
     const int m0 = tm * TM, b0 = tn * WN;
 
-    const i32x4 rx = make_desc(a.X + m0 * a.ldx, (uint32_t)((min(TM, a.M - m0) - 1) * a.ldx + (a.K + 15) / 16 * 16));
+    // X from the wave's own first row on: what a resource spans stays below 2 GB (the host sees to it), and rows past M
+    // are past its end
+    const int mw = m0 + 8 * XL * wave, rows = min(8 * XL, a.M - mw);
+    const i32x4 rx = make_desc(a.X + mw * a.ldx, rows > 0 ? (uint32_t)((rows - 1) * a.ldx + (a.K + 15) / 16 * 16) : 0u);
     const i32x4 rw = make_desc(a.W + (int64_t)b0 * kp * kBlock8, (uint32_t)min(WN, blocks - b0) * (uint32_t)(kp * kBlock8));
     const uint32_t ldx = (uint32_t)a.ldx;
     const uint32_t vx = (uint32_t)(lane >> 3) * ldx + (uint32_t)(((lane & 7) ^ (lane >> 3)) << 4);
     const uint32_t vw = (uint32_t)lane * 16;
-    uint32_t sx = (uint32_t)(8 * XL * wave) * ldx + (uint32_t)(first * kStageK);
+    uint32_t sx = (uint32_t)(first * kStageK);
     uint32_t sw = (uint32_t)(WL * wave / 8) * (uint32_t)(kp * kBlock8) + (uint32_t)(WL * wave % 8) * 1024u + (uint32_t)(first * 8192);
     int to_load = stages;
     auto issue = [&](int slot) {
@@ -219,6 +223,7 @@ __global__ __launch_bounds__(256) void product8_join_kernel(Product8Args a, int 
 constexpr int kStreamWaves = 8;
 template <typename T, int P, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves) void product8_stream_kernel(Product8Args a) {
+    static_assert(16 * MT <= kWaveRows, "rows span less than 4 GB");
     constexpr int U = P + MT >= 8 ? 1 : 12 / (P + MT);       // pieces of K in flight, twice
     __shared__ int sums[16 * MT][16 * P + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -226,7 +231,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void product8_stream_kernel(Prod
     const int kp = padded_k8(a.K), pieces = kp / kPieceK;
     const int block = blockIdx.x / (4 / P), i0 = blockIdx.x % (4 / P) * P;
     const uint8_t* w = a.W + (int64_t)block * kp * kBlock8 + i0 * kPieceBytes + 16 * lane;
-    uint32_t x[MT];                                         // rows, from X: at most 16 MT of 2^17 bytes
+    uint32_t x[MT];                                         // rows, from X: less than 4 GB (the host sees to it)
 #pragma unroll
     for (int j = 0; j < MT; ++j) x[j] = (uint32_t)min(16 * j + lrow, a.M - 1) * (uint32_t)a.ldx;
     const int last = (a.K - 1) / 16 * 16;                   // first code of a row's last 16
@@ -461,12 +466,15 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
     if (M < 0 || N < 0 || K < 0 || (!mq_host::is_half_type(type) && type != MQ_FP32)) return MQ_ERR_INVALID_ARG;
     if (M > (1 << 24) || !shape8_ok(N, K) || ldx < (K + 15) / 16 * 16 || ldx % 16 != 0 || ldy < N) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
+    const Plan8 p = plan8(M, N, K);
+    // offsets within a wave's rows: 32 bits, of which the tiled kernels' loads past the end take the upper half
+    if ((int64_t)(std::min(M, kWaveRows) - 1) * ldx + (K + 15) / 16 * 16 > (p.streams ? (int64_t)UINT32_MAX : INT32_MAX))
+        return MQ_ERR_UNSUPPORTED_SHAPE;
     if (!Xq8 || !s_x || !Wq8 || !s_w || !Y) return MQ_ERR_INVALID_ARG;
     const size_t size = type == MQ_FP32 ? 4 : 2;
     if (!mq_host::aligned(Xq8, 16) || !mq_host::aligned(Wq8, 16) || !mq_host::aligned(s_x, 4) || !mq_host::aligned(s_w, 4) ||
         !mq_host::aligned(bias, size) || !mq_host::aligned(Y, size))
         return MQ_ERR_MISALIGNED;
-    const Plan8 p = plan8(M, N, K);
     const size_t need = mq_gemm_w8a8_workspace_size(M, N, K);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     const Product8Args a{M, N, K, reinterpret_cast<const uint8_t*>(Xq8), ldx, s_x, Wq8, s_w, bias, Y, ldy,

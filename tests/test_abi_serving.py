@@ -131,3 +131,15 @@ def test_attention_workspace_is_small(lib, B, H, group, max_q, max_kv):
     """Two parts of at most 16 columns for each workgroup that the chip holds, or one of 256, and where each sequence begins."""
     size = lib.mq_attention_kv4_workspace_size(B, B * max_q, H, group, 128, max_q, max_kv)
     assert size <= 256 * 256 * 130 * 4 + 4 * B + 32
+
+
+def test_gemm_w8a8_rows_far_apart(lib):
+    """The rows of a wave's loads span less than 2 GB, up to 16 rows (all in one wave) less than 4; what fits is refused
+    for its output's address only, what does not before."""
+    def f(M, ldx, K=128):
+        return lib.mq_gemm_w8a8(M, 32, K, A, ldx, A, A, A, 0, None, A + 1, 32, None, 0, None)
+    top = (1 << 31) - 16                                    # the largest leading dimension there is
+    for M, ldx in ((1, top), (2, top), (3, top - 112), (16, 286331136), (33, 69273648), (1 << 24, 69273648)):
+        assert f(M, ldx) == MISALIGNED, (M, ldx)
+    for M, ldx in ((3, top), (16, 286331152), (33, 69273664), (1 << 24, 1 << 27)):
+        assert f(M, ldx) == SHAPE, (M, ldx)

@@ -164,3 +164,18 @@ def test_refusals():
     ]:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("M,N,K,ld", [(2, 64, 128, (1 << 31) - 128), (17, 130, 256, 1 << 26), (129, 4096, 144, 69000000),
+                                      (300, 5000, 1000, 33947648), (256, 25600, 4096, 33947648), (260, 65536, 128, 16900096)])
+def test_rows_far_apart(M, N, K, ld):
+    """Activations as a view of a larger tensor, each tile's rows more than 4 GB in all: every kernel and tile."""
+    m = mq()
+    x, sx, w, sw = operands(M, N, K, 3)
+    x, sx, pw = x.contiguous().cuda(), sx.cuda(), m.repack_weight8(w.cuda(), sw.cuda())
+    pad = -(-K // 16) * 16
+    near = torch.zeros((M, pad), dtype=torch.int8, device="cuda")[:, :K]
+    near.copy_(x)
+    far = torch.empty((M - 1) * ld + pad, dtype=torch.int8, device="cuda").as_strided((M, K), (ld, 1))
+    far.copy_(x)
+    assert torch.equal(m.gemm_w8a8(far, sx, pw), m.gemm_w8a8(near, sx, pw))
