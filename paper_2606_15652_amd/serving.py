@@ -276,21 +276,35 @@ class KVCache4:
     v: "object"
     k_params: "object"    # fp16 [pages, heads, page_size, 2]: scale, minimum
     v_params: "object"
-    _struct: "object" = field(default=None, repr=False, init=False)   # what the library takes: mq_kv4_cache, and its address
-    _c: int = field(default=0, repr=False, init=False)
+    # what the library takes (mq_kv4_cache), and the fields and addresses that it was made of
+    _struct: "object" = field(default=None, repr=False, init=False, compare=False)
+    _of: tuple = field(default=(), repr=False, init=False, compare=False)
 
     def __post_init__(self):
-        torch = _torch()
-        codes = (self.pages, self.heads, self.page_size * self.head_dim // 2)
-        params = (self.pages, self.heads, self.page_size, 2)
-        _need_out(self.k, codes, torch.uint8, "k")
-        _need_out(self.v, codes, torch.uint8, "v")
-        _need_out(self.k_params, params, torch.float16, "k_params")
-        _need_out(self.v_params, params, torch.float16, "v_params")
-        _same_device(self.k, "k", v=self.v, k_params=self.k_params, v_params=self.v_params)
-        self._struct = _CacheStruct(self.k.data_ptr(), self.v.data_ptr(), self.k_params.data_ptr(), self.v_params.data_ptr(),
-                                    self.pages, self.page_size, self.heads, self.head_dim)
-        self._c = C.addressof(self._struct)
+        self._c
+
+    @property
+    def _c(self) -> int:
+        """Address of the mq_kv4_cache of the fields as they are: made anew, and they checked again, once one has been
+        replaced or a tensor has other memory."""
+        k, v, kp, vp = self.k, self.v, self.k_params, self.v_params
+        of = self._of
+        if not (of and of[0] is k and of[1] is v and of[2] is kp and of[3] is vp and of[4] == (
+                k.data_ptr(), v.data_ptr(), kp.data_ptr(), vp.data_ptr(), self.pages, self.page_size, self.heads, self.head_dim)):
+            torch = _torch()
+            codes = (self.pages, self.heads, self.page_size * self.head_dim // 2)
+            params = (self.pages, self.heads, self.page_size, 2)
+            _need_out(k, codes, torch.uint8, "k")
+            _need_out(v, codes, torch.uint8, "v")
+            _need_out(kp, params, torch.float16, "k_params")
+            _need_out(vp, params, torch.float16, "v_params")
+            _same_device(k, "k", v=v, k_params=kp, v_params=vp)
+            now = (k.data_ptr(), v.data_ptr(), kp.data_ptr(), vp.data_ptr(), self.pages, self.page_size, self.heads, self.head_dim)
+            self._struct, self._of = _CacheStruct(*now), (k, v, kp, vp, now)
+        return C.addressof(self._struct)
+
+    def __getstate__(self):                                 # addresses mean nothing in a copy
+        return {name: value for name, value in self.__dict__.items() if name not in ("_struct", "_of")}
 
     @property
     def nbytes(self) -> int:

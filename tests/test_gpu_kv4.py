@@ -203,3 +203,50 @@ def test_rows_whose_minimum_rounds_above_their_maximum(D):
         assert not params[..., 0].view(torch.int16).any()                       # +0, not a negative zero
     gk, gv = m.kv4_read(cache, slots, torch.bfloat16)
     assert torch.equal(gk.cpu(), so.values4(x).bfloat16()) and torch.equal(gv.cpu(), so.values4(x.flip(0)).bfloat16())
+
+
+def test_a_cache_whose_tensors_are_replaced():
+    """Calls use the tensors and sizes that the cache has when they are made."""
+    m = mq()
+    k, v = rows(16, 2, 64, torch.float16, 8)
+    slots = torch.arange(16).cuda()
+    cache = m.kv4_cache(1, 16, 2, 64)
+    m.kv4_append(cache, k.cuda(), v.cuda(), slots)
+    old = cache.k, cache.v, cache.k_params, cache.v_params
+    # grown to three pages, the first of them the last
+    for name in ("k", "v", "k_params", "v_params"):
+        t = getattr(cache, name)
+        setattr(cache, name, torch.cat((torch.zeros_like(t), torch.zeros_like(t), t)))
+    cache.pages = 3
+    gk, gv = m.kv4_read(cache, slots + 32)
+    assert torch.equal(gk.cpu(), so.values4(k).half()) and torch.equal(gv.cpu(), so.values4(v).half())
+    m.kv4_append(cache, v.cuda(), k.cuda(), slots)
+    assert torch.equal(m.kv4_read(cache, slots)[0].cpu(), so.values4(v).half())
+    fresh = m.kv4_cache(1, 16, 2, 64)
+    m.kv4_append(fresh, k.cuda(), v.cuda(), slots)
+    assert all(torch.equal(a, b) for a, b in zip(old, (fresh.k, fresh.v, fresh.k_params, fresh.v_params)))   # untouched
+    cache.v.data = cache.v.clone()                          # in place, too
+    cache.v.zero_()
+    cache.v_params.zero_()
+    assert not m.kv4_read(cache, slots + 32)[1].any()
+    # tensors and sizes that do not go together are refused
+    cache.pages = 4
+    with pytest.raises(ValueError):
+        m.kv4_read(cache, slots)
+    cache.pages, cache.k = 3, cache.k.half()
+    with pytest.raises(TypeError):
+        m.attention_kv4(torch.zeros(1, 2, 64).half().cuda(), cache, torch.zeros(1, 1, dtype=torch.int32).cuda(),
+                        torch.ones(1, dtype=torch.int32).cuda())
+
+
+def test_copies_of_a_cache():
+    import copy
+    m = mq()
+    k, v = rows(16, 2, 64, torch.float16, 9)
+    slots = torch.arange(16).cuda()
+    cache = m.kv4_cache(1, 16, 2, 64)
+    m.kv4_append(cache, k.cuda(), v.cuda(), slots)
+    other, same_memory = copy.deepcopy(cache), copy.copy(cache)
+    m.kv4_append(cache, v.cuda(), k.cuda(), slots)
+    assert torch.equal(m.kv4_read(other, slots)[0].cpu(), so.values4(k).half())
+    assert torch.equal(m.kv4_read(same_memory, slots)[0].cpu(), so.values4(v).half())
