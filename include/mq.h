@@ -538,6 +538,11 @@ mq_status mq_kv4_read(const mq_kv4_cache* cache, int T, mq_dtype type, const int
  *   scale      : positive.
  *   workspace  : >= mq_attention_kv4_workspace_size() bytes, 16-byte aligned (may
  *                be NULL when that is 0).
+ * Sizes past the launch's indexes are refused: with columns = max_q group, blocks of
+ * 256 of them (or of 4, 8 and 16 up to 4, 8 and 64 columns), sequences heads blocks
+ * is at most 2^23 - 1 (2^24 - 1 up to 64 columns); up to 64 columns and past 1024
+ * tokens sequences heads blocks (max_kv / 64 + 12) is below 2^30, and there are less
+ * than 2^24 rows of max_q queries.  The workspace size of what is refused is 0.
  * The result does not depend on the order in which anything runs.
  */
 size_t mq_attention_kv4_workspace_size(int sequences, int tokens, int heads, int group,

@@ -997,6 +997,13 @@ struct Plan4 {
     int splits, split_steps;            // 256 columns
 };
 
+// Columns of a workgroup.
+static int columns4(int max_q, int group) {
+    const int64_t cols = (int64_t)max_q * group;
+    return cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 256;
+}
+constexpr int kWholeSteps = 16;         // few columns: sequences of up to as many steps are taken whole
+
 // Workgroups of a launch.  Few columns: short sequences (up to 1024 tokens: 16
 // steps, four for each wave) are taken whole; the others are cut into as many
 // equal shares as workgroups fit on the chip, or shares of four steps if those are
@@ -1005,7 +1012,7 @@ struct Plan4 {
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;
-    p.columns = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 256;
+    p.columns = columns4(max_q, group);
     const int64_t units = (int64_t)sequences * heads * ((cols + p.columns - 1) / p.columns), steps = (max_kv + kStep - 1) / kStep;
     p.splits = 1;
     p.split_steps = (int)std::max<int64_t>(steps, 1);
@@ -1019,7 +1026,7 @@ static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_k
         p.groups = units * p.splits;
         return p;
     }
-    p.whole = steps <= 16;
+    p.whole = steps <= kWholeSteps;
     const int64_t shares = (units * steps + kLeastSteps - 1) / kLeastSteps, resident = p.columns > 8 ? 512 : 768;
     p.groups = p.whole ? units : std::min(shares, resident);
     return p;
@@ -1031,11 +1038,18 @@ static size_t workspace4(const Plan4& p, int sequences, int head_dim) {
     return (floats * sizeof(float) + 15) / 16 * 16;
 }
 
+// Sizes that the plan, the kernels' indexes and the launches hold: a grid has less than 2^32 threads, and where
+// workgroups share out all steps, these are counted in 32 bits.
 static bool shape4_ok(int sequences, int heads, int group, int max_q, int64_t max_kv) {
-    return sequences >= 0 && heads >= 1 && group >= 1 && max_q >= 0 && max_kv >= 0 && sequences <= (1 << 24) && heads <= 65535 &&
-           group <= 1024 && (int64_t)max_q * group < (1 << 30) && max_kv < (1ll << 31) - 65536 &&
-           // steps of all units, counted in 32 bits
-           (double)sequences * heads * (((double)max_q * group + 15) / 4) * ((double)max_kv / kStep + 1 + kUnitSteps) < (1 << 30) * 1.0;
+    if (sequences < 0 || heads < 1 || group < 1 || max_q < 0 || max_kv < 0 || sequences > (1 << 24) || heads > 65535 || group > 1024 ||
+        (int64_t)max_q * group >= (1 << 30) || max_kv >= (1ll << 31) - 65536)
+        return false;
+    const int columns = columns4(max_q, group);
+    const double units = (double)sequences * heads * (double)(((int64_t)max_q * group + columns - 1) / columns);
+    const double rows = (double)sequences * max_q * heads * group;
+    if (units > (double)(UINT32_MAX / (columns == 256 ? 512 : 256))) return false;
+    if (columns == 256 || (max_kv + kStep - 1) / kStep <= kWholeSteps) return true;
+    return units * (double)((max_kv + kStep - 1) / kStep + kUnitSteps) < 0x1p30 && rows <= (double)(UINT32_MAX / 256);
 }
 
 }  // namespace mq
@@ -1075,8 +1089,7 @@ extern "C" mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, 
                       sequences, tokens, group, max_q, scale, causal != 0, part, part ? part + rows * cache->head_dim : nullptr,
                       part ? part + rows * (cache->head_dim + 1) : nullptr,
                       part ? reinterpret_cast<int32_t*>(part + rows * (cache->head_dim + 2)) : nullptr, p.splits, p.split_steps};
-    const int64_t joins = (int64_t)sequences * max_q * cache->heads * group;
-    if (p.groups > INT32_MAX || joins > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const int64_t joins = (int64_t)sequences * max_q * cache->heads * group;            // rows, where the launch is followed by a join
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto with_dim = [&](auto d) {

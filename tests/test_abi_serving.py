@@ -143,3 +143,32 @@ def test_gemm_w8a8_rows_far_apart(lib):
         assert f(M, ldx) == MISALIGNED, (M, ldx)
     for M, ldx in ((3, top), (16, 286331152), (33, 69273664), (1 << 24, 1 << 27)):
         assert f(M, ldx) == SHAPE, (M, ldx)
+
+
+def test_attention_kv4_limits(lib):
+    """Both sides of the limits that the launches have; what is within them is refused for its queries' address only."""
+    def f(B=1, heads=8, group=4, max_q=1, max_kv=64):
+        c = cache(heads=heads, page_size=65536)
+        T = B * max_q
+        return lib.mq_attention_kv4(C.addressof(c), B, T, group, max_q, max_kv, 0, A + 8, 512, 64, A, 1 << 15, A, A, 0.125, 1, A, 512, 64,
+                                    None, 0, None)
+    # long prompts: whatever the context's length
+    for sizes in (dict(group=8, max_q=32768, max_kv=131072), dict(max_q=131072, max_kv=131072), dict(group=8, max_q=131072, max_kv=1 << 20),
+                  dict(B=64, max_q=32768 // 64, max_kv=131072), dict(B=16, heads=64, group=1, max_q=8192, max_kv=1 << 17),
+                  dict(heads=65535, group=1, max_q=32768, max_kv=4096)):
+        assert f(**sizes) == MISALIGNED, sizes
+    assert f(heads=65535, group=1, max_q=32769, max_kv=4096) == SHAPE
+    # few columns, shared out step by step
+    most = (1 << 31) - 65537
+    assert f(heads=32, group=1, max_kv=most) == MISALIGNED and f(heads=33, group=1, max_kv=most) == SHAPE
+    assert f(B=255, heads=65535, group=1, max_kv=64) == MISALIGNED and f(B=257, heads=65535, group=1, max_kv=64) == SHAPE
+    assert f(B=1 << 24, heads=65535, group=1024, max_q=1 << 19, max_kv=most) == SHAPE
+    assert lib.mq_attention_kv4_workspace_size(1 << 24, 1, 65535, 1, 64, 1, most) == 0
+
+
+def test_attention_kv4_defaults_are_within_the_limits(lib):
+    """The binding's own bounds, all rows of Q and the whole table: 64 prompts of 512 tokens, tables of 8192."""
+    c = cache(heads=8, page_size=64)
+    status = lib.mq_attention_kv4(C.addressof(c), 64, 64 * 512, 4, 64 * 512, 8192, 0, A + 8, 512, 64, A, 128, A, A, 0.125, 1, A, 512, 64,
+                                  None, 0, None)
+    assert status == MISALIGNED

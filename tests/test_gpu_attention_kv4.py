@@ -331,3 +331,24 @@ def test_values_past_fp16s_range(nqs, dim):
         k, v = so.values4(seqs.k[0])[:70], so.values4(seqs.v[0])[:70]
         want = so.attention(q[:70], k, v, 1 / math.sqrt(dim), True)
         assert ((o[:70].double() - want).abs() <= so.attention_error(q[:70], k, v, 1 / math.sqrt(dim), torch.bfloat16, want)).all()
+
+
+def test_prompts_with_the_bounds_left_to_their_defaults():
+    """All rows of Q and the whole of a long table as bounds: launches of many workgroups that have nothing to do."""
+    m = mq()
+    lens, nqs = [600 + b for b in range(16)], [512 if b % 2 else 300 + b for b in range(16)]
+    seqs = so.Sequences(lens, 8, 64, 64, torch.float16, 31, most=1024 * 2)
+    cache = filled(seqs, 8, 64)
+    q = torch.randn(sum(nqs), 32, 64, generator=so.generator(32)).half().cuda()
+    cu = torch.tensor([0] + list(torch.tensor(nqs).cumsum(0)), dtype=torch.int32).cuda()
+    o = m.attention_kv4(q, cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu)
+    again = m.attention_kv4(q, cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu, max_q=512, max_kv=615)
+    assert (o.double() - again.double()).abs().max() <= 2e-3 * again.abs().max()
+    b, at = 3, int(cu[3])
+    i = [0, 1, 255, 511]
+    k, v = so.values4(seqs.k[b]), so.values4(seqs.v[b])
+    for j in i:
+        seen = lens[b] - nqs[b] + j + 1
+        want = so.attention(q[at + j:at + j + 1].cpu(), k[:seen], v[:seen], 0.125, True)
+        tol = so.attention_error(q[at + j:at + j + 1].cpu(), k[:seen], v[:seen], 0.125, torch.float16, want)
+        assert ((o[at + j:at + j + 1].cpu().double() - want).abs() <= tol).all()
