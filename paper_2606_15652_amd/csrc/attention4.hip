@@ -573,6 +573,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
   } while (true);
 }
 
+constexpr float kLift = 8.0f, kMost = 15.0f;    // log2 of the weight at the running maximum, and above which that moves
 constexpr uint16_t kMostPower = 0x7000;     // 2^13 in fp16: the largest power of two by which codes are staged
 
 // what a scheduling group holds
@@ -601,7 +602,8 @@ constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
 // The vector unit bounds it (an exponential takes it four times as long as
 // another operation): a score is brought under its column's running maximum by
 // the two multiply-adds that scale it, score - m = acc sk + (zk sum(q) - m), and
-// the sums are rows of the second product.
+// the sums are rows of the second product.  Weights are held as multiples of 2^-kLift of
+// the running maximum's, up to 2^15: a weight counts down to 2^-33 of the largest.
 template <typename T, int D>
 __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     constexpr int KK = D / 32, VT = D / 16, C = 2, WaveCols = 16 * C, NW = 8, Cols = WaveCols * NW;
@@ -775,7 +777,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
     f32x4 acc[C][VT] = {}, sums[C] = {};
     float m[C] = {}, most[C];                               // scores are taken less m; above `most` of that m moves
 #pragma unroll
-    for (int j = 0; j < C; ++j) most[j] = -INFINITY;        // to the first score that there is, then by more than kSlack
+    for (int j = 0; j < C; ++j) most[j] = -INFINITY;        // to the first score that there is, then above kMost
 
     int now[4];                                             // pages of the stage in use
     auto turn = [&](int t) {                                // the stage at t from registers to LDS, the one after into registers
@@ -844,9 +846,9 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
             if (__any(moves)) {
 #pragma unroll
                 for (int j = 0; j < C; ++j) {
-                    const float to = quads_max(top[j]), by = to > most[j] ? to : 0.0f;
-                    const float down = most[j] == kSlack ? __builtin_amdgcn_exp2f(-by) : 1.0f;  // (before: sums of nothing)
-                    most[j] = to > most[j] ? kSlack : most[j];
+                    const float to = quads_max(top[j]), by = to > most[j] ? to - kLift : 0.0f;
+                    const float down = most[j] == kMost ? __builtin_amdgcn_exp2f(-by) : 1.0f;   // (before: sums of nothing)
+                    most[j] = to > most[j] ? kMost : most[j];
                     m[j] += by;
 #pragma unroll
                     for (int h = 0; h < 4; ++h) x[j][h] -= by;
@@ -903,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void attention4_wide_kernel(Attn4Args a) {
                 else *reinterpret_cast<f32x4*>(a.part_o + place * D + g * (D / 4) + c) = o;
             }
             if (a.splits > 1 && g == 0) {
-                a.part_m[place] = most[j] == kSlack ? m[j] : kLowest;
+                a.part_m[place] = most[j] == kMost ? m[j] : kLowest;
                 a.part_l[place] = sum;
             }
         }

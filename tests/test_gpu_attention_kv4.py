@@ -352,3 +352,36 @@ def test_prompts_with_the_bounds_left_to_their_defaults():
         want = so.attention(q[at + j:at + j + 1].cpu(), k[:seen], v[:seen], 0.125, True)
         tol = so.attention_error(q[at + j:at + j + 1].cpu(), k[:seen], v[:seen], 0.125, torch.float16, want)
         assert ((o[at + j:at + j + 1].cpu().double() - want).abs() <= tol).all()
+
+
+def sink(nq, nats, step):
+    """One token `nats` above all others, which together have a share: their weights count in both sums alike.  Each is
+    off by 2^-11 of itself, or by `step` of the largest."""
+    m = mq()
+    n, heads, dim = 4096, 256, 64                           # as many heads as CUs: contexts are not split
+    g = so.generator(nq, 41)
+    k, v = torch.zeros(n, 1, dim), torch.rand(n, 1, dim, generator=g)
+    v[..., 0], v[..., 1] = 0.0, 1.0
+    v = (v * 15).round() / 16                               # values and keys that the cache holds as they are
+    k[0, :, 0], v[0] = 15.0, 0.0
+    cache = m.kv4_cache(n // 64, 64, heads, dim)
+    m.kv4_append(cache, k.half().cuda().expand(-1, heads, -1), v.half().cuda().expand(-1, heads, -1), torch.arange(n).cuda())
+    table = torch.arange(n // 64, dtype=torch.int32)[None].cuda()
+    q = torch.zeros(nq, heads, dim)
+    q[..., 0] = nats / 15 * 8
+    q = q.half()
+    kd, vd = so.values4(k.half())[:, 0], so.values4(v.half())[:, 0]
+    assert kd[0, 0] == 15 and torch.equal(vd, v[:, 0].double())
+    o = m.attention_kv4(q.cuda(), cache, table, torch.tensor([n], dtype=torch.int32).cuda(),
+                        cu_q=torch.tensor([0, nq], dtype=torch.int32).cuda()).cpu().double()
+    w = torch.exp(0.125 * (kd @ q[0, 0].double() - 15 * q[0, 0, 0].double()))
+    for i in range(nq):
+        seen = n - nq + i + 1
+        want = (w[:seen] @ vd[:seen]) / w[:seen].sum()
+        tol = want * (2.0 ** -11 + 2.0 ** -18) + n * step * vd.max() + so.UNIT[torch.float16] * want + so.TINY[torch.float16]
+        assert ((o[i] - want).abs() <= tol).all(), ((o[i] - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("nats", [14.0, 17.0, 18.5, 20.0])
+def test_a_sink_beside_a_long_context_many_queries(nats):
+    sink(65, nats, 2.0 ** -33)                              # fp16's smallest step, halved, of weights held up to 2^8 at the maximum
