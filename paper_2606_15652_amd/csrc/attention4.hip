@@ -185,10 +185,10 @@ __device__ __forceinline__ Work4 work4(const Attn4Args& a, const Sequence& s) {
 // the kernel: a batch of 64 contexts of up to 8191 tokens 70 us, 65).
 // The weights cross to the lanes of the second product, O^T = V^T P^T, through LDS.
 //
-// Weights are held as multiples of `scale` (at least every sv), w = p sv / scale,
-// rounded to fp16; of the products 7.5 sum(w) is taken off again and made up for in
-// fp32: codes about their middle, so that the rounding of w counts against values
-// about their middle.
+// Weights are held as multiples of `unit` (every sv is at most 2^7 of them), w = p sv /
+// unit up to 2^15, rounded to fp16, whose smallest step is then 2^-31 of the largest sv;
+// of the products 7.5 sum(w) is taken off again and made up for in fp32: codes about
+// their middle, so that the rounding of w counts against values about their middle.
 //
 // What a wave loads for 64 tokens: lane (r, g), tile i: token r's key channels
 // (D / 4) g .., the tokens 4 g .. + 3's value channels (D / 16) r ..; and the
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
 
     f32x4 acc[VT] = {};
     float m[R], l[R] = {}, rest[R] = {};                    // rest: what the codes about their middle leave out
-    float scale = 0.0f, per_scale = 0.0f;                   // weights are held as multiples of `scale`
+    float unit = 0.0f, per_unit = 0.0f;                     // weights are held as multiples of `unit`
 #pragma unroll
     for (int e = 0; e < R; ++e) m[e] = kLowest;
     // over the lanes that keep the same columns
@@ -434,13 +434,13 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             top[e] *= to_score;
             moves = moves || top[e] > m[e] + kSlack;
         }
-        moves = moves || most > scale;
+        moves = moves || most > 0x1p7f * unit;
         if (__any(moves)) {
-            const float old = scale;
+            const float old = unit;
 #pragma unroll
             for (int i = 1; i < 64; i <<= 1) most = fmaxf(most, __shfl_xor(most, i));
-            scale = fmaxf(scale, 2.0f * most);
-            per_scale = scale > 0.0f ? 1.0f / scale : 0.0f;
+            unit = fmaxf(unit, 0x1p-6f * most);
+            per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
             float down[R];
 #pragma unroll
             for (int e = 0; e < R; ++e) {
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
                 m[e] = to;
                 l[e] *= down[e];
                 rest[e] *= down[e];
-                down[e] *= old * per_scale;
+                down[e] *= old * per_unit;
             }
             // the factor of the second product's column r: register r % 4 of a lane that keeps it
             float by = 1.0f;
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             const int tile = i * Shape4<RP>::kTiles + base;
             // tokens of 32 in the order of the second product's operand: 4 g .. + 3 of one tile, then of the other
             const int at = tile / 2 * 32 + r / 4 * 8 + tile % 2 * 4 + r % 4;
-            const float by = sv[i] * per_scale, off = -7.5f * scale;
+            const float by = sv[i] * per_unit, off = -7.5f * unit;
 #pragma unroll
             for (int e = 0; e < R; ++e) {
                 const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], to_score, -m[e]));
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             shared_l[wave][mine + e] = l[e];
         }
     }
-    const float of_scale = scale * 0x1p24f;
+    const float of_unit = unit * 0x1p24f;
     __syncthreads();                                        // every wave has read its last weights
     if (r < RP && col0 + r < cols) {
 #pragma unroll
@@ -530,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int i = (c + k) % VT, e = (c + k) / VT;
-                out[k] = __builtin_fmaf(acc[i][e], of_scale * (i % 2 ? 0.0625f : 1.0f), add);
+                out[k] = __builtin_fmaf(acc[i][e], of_unit * (i % 2 ? 0.0625f : 1.0f), add);
             }
             *reinterpret_cast<f32x4*>(&shared.o[wave][r][g * (D / 4) + c]) = out;
         }

@@ -385,3 +385,37 @@ def sink(nq, nats, step):
 @pytest.mark.parametrize("nats", [14.0, 17.0, 18.5, 20.0])
 def test_a_sink_beside_a_long_context_many_queries(nats):
     sink(65, nats, 2.0 ** -33)                              # fp16's smallest step, halved, of weights held up to 2^8 at the maximum
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq", [1, 3, 40])
+def test_small_values_beside_a_hidden_large_row(nq, dtype):
+    """A token without weight whose values are ten million times the others': its scale does not cost theirs.  The
+    weight of a code's part is held to fp16's smallest step at 2^-6 of the largest scale, 7.5 codes of it at most."""
+    m = mq()
+    n, dim, group = 64 + nq, 64, 4
+    g = so.generator(nq, 43)
+    k, v = torch.zeros(n, 1, dim), torch.rand(n, 1, dim, generator=g) * 2e-3
+    k[..., 0], k[9, 0, 0], k[5, 0, 0] = 15.0, 30.0, 0.0     # scores: the first far above the second, that above the third
+    v[5] = (torch.rand(dim, generator=g) - 0.5) * 50000
+    k, v = k.to(dtype), v.to(dtype)
+    cache = m.kv4_cache(-(-n // 16), 16, 1, dim)
+    m.kv4_append(cache, k.cuda(), v.cuda(), torch.arange(n).cuda())
+    table = torch.arange(-(-n // 16), dtype=torch.int32)[None].cuda()
+    q = torch.zeros(nq, group, dim)
+    q[..., 0] = 16.0
+    q = q.to(dtype)
+    kd, vd = so.values4(k), so.values4(v)
+    o = m.attention_kv4(q.cuda(), cache, table, torch.tensor([n], dtype=torch.int32).cuda(),
+                        cu_q=torch.tensor([0, nq], dtype=torch.int32).cuda()).cpu().double()
+    want = so.attention(q, kd, vd, 0.125, True)
+    large = so.quantise4(v)[1].max().item()
+    rest = torch.cat((vd[:5], vd[6:]))
+    tol = 2.0 ** -11 * (rest.max() - rest.min()) * 1.01 + 7.5 * 2.0 ** -25 * large * 2.0 ** -6 + math.exp(-60 * 0.99) * 3e4 \
+        + 2.0 ** -22 * rest.max() + so.UNIT[dtype] * want.abs() * 1.01 + so.TINY[dtype]
+    assert ((o - want).abs() <= tol).all(), ((o - want).abs() / tol).max()
+
+
+@pytest.mark.parametrize("nats", [14.0, 17.0, 18.5, 20.0])
+def test_a_sink_beside_a_long_context_one_query(nats):
+    sink(1, nats, 2.0 ** -32)                               # half of fp16's smallest step at 2^-6 of the scale, 7.5 codes of it
