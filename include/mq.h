@@ -523,8 +523,11 @@ mq_status mq_kv4_read(const mq_kv4_cache* cache, int T, mq_dtype type, const int
  * its nq queries, query i sees the tokens 0 .. kv_lens[b] - nq + i (causal: the
  * last query sees all), or all of them.  Query head h reads key head h / group.
  *     O = sum_t p_t v_t / sum_t p_t,   p_t = exp(scale q.k_t)
- * Queries and weights enter the products in fp16 (queries scaled by a power of
- * two each); sums, maxima and the running results are fp32.
+ * Queries and weights enter the products in fp16 (queries scaled by a power of two,
+ * one for up to 256 columns max_q group of a sequence and key head: a query value
+ * counts down to 2^-28 of the largest finite one beside it); sums, maxima and the
+ * running results are fp32.  Values of queries that are not finite change no other
+ * query's result.
  * A query that sees nothing gives 0.  A row of the cache that is not finite makes
  * the queries that see it NaN, and no others.  Tokens of a page outside [0, pages)
  * are seen by none.

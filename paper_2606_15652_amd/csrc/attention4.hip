@@ -110,7 +110,7 @@ __device__ __forceinline__ f16x8 value_operand(uint32_t a0, uint32_t a1, uint32_
 }
 
 // Operands and scales of 16 columns of queries: fp16, scaled by a power of two that brings the largest
-// value near 2^8, so that neither type's range matters; channels of the codes that come 16 times too large
+// finite value of the workgroup's columns near 2^8, so that neither type's range matters; channels of the codes that come 16 times too large
 // divided by 16.  A lane has the channels (D / 4) g .. of its column.
 template <int D>
 struct Queries {
@@ -120,7 +120,7 @@ struct Queries {
     f32x8 x[D / 32];
 
     template <typename T>
-    __device__ __forceinline__ void load(const T* q) {      // amax: of the 16 columns
+    __device__ __forceinline__ void load(const T* q) {      // amax: of the 16 columns; a column that is not finite spoils no other
         of_minimum = amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -128,14 +128,14 @@ struct Queries {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 of_minimum += x[i][e];
-                amax = fmaxf(amax, fabsf(x[i][e]));
+                amax = fmaxf(amax, fabsf(x[i][e]) < INFINITY ? fabsf(x[i][e]) : 0.0f);
             }
         }
         of_minimum = quads_sum(of_minimum);
 #pragma unroll
         for (int i = 1; i < 64; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
     }
-    static __device__ __forceinline__ int exponent(float amax) { return amax > 0.0f && amax < INFINITY ? 8 - ilogbf(amax) : 0; }
+    static __device__ __forceinline__ int exponent(float amax) { return amax > 0.0f ? 8 - ilogbf(amax) : 0; }
     __device__ __forceinline__ void finish(int up) {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {

@@ -419,3 +419,29 @@ def test_small_values_beside_a_hidden_large_row(nq, dtype):
 @pytest.mark.parametrize("nats", [14.0, 17.0, 18.5, 20.0])
 def test_a_sink_beside_a_long_context_one_query(nats):
     sink(1, nats, 2.0 ** -32)                               # half of fp16's smallest step at 2^-6 of the scale, 7.5 codes of it
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("q_spread", [1e6, 1e-6])
+@pytest.mark.parametrize("nqs", [[1, 1], [3, 2], [40, 17]])
+def test_queries_that_are_not_finite_change_no_others(nqs, q_spread, bad):
+    m = mq()
+    lens, heads, group, dim = [100, 60], 1, 4, 64
+    seqs = so.Sequences(lens, heads, dim, 16, torch.bfloat16, 51)
+    cache = filled(seqs, heads, dim)
+    q = (torch.randn(sum(nqs), heads * group, dim, generator=so.generator(52)) * q_spread).bfloat16()
+    hit = q.clone()
+    hit[0, 1, 5] = bad
+    cu = torch.tensor([0] + list(torch.tensor(nqs).cumsum(0)), dtype=torch.int32)
+    scale = 1.0 / (2 * q_spread)
+    o = m.attention_kv4(hit.cuda(), cache, seqs.table.cuda(), seqs.kv_lens.cuda(), cu_q=cu.cuda(), scale=scale).cpu()
+    assert torch.isnan(o[0, 1]).any()
+    for b in range(2):
+        part = slice(int(cu[b]), int(cu[b + 1]))
+        k, v = so.values4(seqs.k[b]), so.values4(seqs.v[b])
+        want = so.attention(q[part], k, v, scale, True)
+        off = (o[part].double() - want).abs()
+        fine = off <= so.attention_error(q[part], k, v, scale, torch.bfloat16, want)
+        if b == 0:
+            fine[0, 1] = True
+        assert fine.all()
