@@ -43,7 +43,8 @@ def _empty(shape, dtype, device, stream):
 
 
 def _need_rows(t, name, cols=None):
-    """A matrix with contiguous rows (any row stride): its row stride."""
+    """A matrix with contiguous rows (any row stride): its row stride; of a single row, which says nothing, its
+    columns rounded up to 8."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     shape = t.shape
@@ -52,7 +53,7 @@ def _need_rows(t, name, cols=None):
     row, col = t.stride()
     if col != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return row if shape[0] > 1 else max(row, shape[1])
+    return row if shape[0] > 1 else -(-shape[1] // 8) * 8
 
 
 def _same_device(first, name, **others):
@@ -79,8 +80,8 @@ def _need_codes(Xq8, K=None):
         raise TypeError(f"Xq8 must be torch.int8, got {Xq8.dtype}")
     M, K = Xq8.shape
     padded = -(-K // 16) * 16
-    if M == 1:
-        ld = max(padded, ld - ld % 16)          # one row: its stride says nothing
+    if M <= 1:
+        ld = padded                             # one row: its stride says nothing
     if ld < padded or ld % 16:
         raise ValueError(f"Xq8's rows must start every multiple of 16 bytes, at least {padded}; got a row stride of {ld}")
     if padded != K and M and Xq8.storage_offset() + (M - 1) * ld + padded > Xq8.untyped_storage().nbytes():

@@ -179,3 +179,10 @@ def test_rows_far_apart(M, N, K, ld):
     far = torch.empty((M - 1) * ld + pad, dtype=torch.int8, device="cuda").as_strided((M, K), (ld, 1))
     far.copy_(x)
     assert torch.equal(m.gemm_w8a8(far, sx, pw), m.gemm_w8a8(near, sx, pw))
+
+
+def test_no_rows_of_an_odd_width():
+    m = mq()
+    _, _, w, sw = operands(1, 32, 100)
+    pw = m.repack_weight8(w.cuda(), sw.cuda())
+    assert m.gemm_w8a8(torch.empty(0, 100, dtype=torch.int8).cuda(), torch.empty(0).cuda(), pw).shape == (0, 32)

@@ -227,3 +227,21 @@ def test_zeros_without_eps(layout):
     codes, s = m.rms_norm_quantize8(x.cuda(), torch.ones(256).half().cuda(), 0.0, layout=layout)
     codes = m.unpack_act8(codes) if layout == "a8" else codes
     assert torch.isnan(s[1]) and not codes[1].any() and torch.isfinite(s[[0, 2]]).all() and codes[[0, 2]].abs().amax() == 127
+
+
+def test_the_stride_of_a_single_row():
+    """One row (or none) is never stepped along: whatever stride the view has."""
+    m = mq()
+    x, w = so.acts(1, 516, torch.float16, 21).cuda(), torch.ones(512).half().cuda()
+    one = torch.zeros(3, 516).half().cuda()
+    one[0, :512] = x[0, :512]
+    view = one[:1, :512]                                    # its rows 516 apart, if there were more
+    want = m.rms_norm_quantize8(x[:, :512].contiguous(), w, EPS, residual=x[:, :512].contiguous())
+    got = m.rms_norm_quantize8(view, w, EPS, residual=view)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(m.quantize_rows8(view)[0], m.quantize_rows8(x[:, :512].contiguous())[0])
+    out = torch.zeros(2, 516).half().cuda()
+    m.dequantize_act8(want[0], want[1], out=out[:1, :512])
+    assert torch.equal(out[:1, :512], m.dequantize_act8(want[0], want[1])) and not out[1].any() and not out[0, 512:].any()
+    none = torch.zeros(0, 516).half().cuda()[:, :512]
+    assert m.rms_norm_quantize8(none, w, EPS)[0].shape == (0, 512)
