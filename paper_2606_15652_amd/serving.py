@@ -190,6 +190,20 @@ class PackedWeight8:
     K: int
     Wq: "object"          # uint8 [mq_weight8_bytes(N, K)]
     s_w: "object"         # fp32 [N]
+    _of: tuple = field(default=(), repr=False, init=False, compare=False)     # what _operands found to go together
+
+    def _operands(self):
+        """Addresses of the codes and scales, which have to be those of N and K: kernels read as much of them."""
+        of, Wq, s_w = self._of, self.Wq, self.s_w
+        if not (of and of[0] is Wq and of[1] is s_w and of[2] == (self.N, self.K, Wq.numel(), s_w.numel())):
+            torch, need = _torch(), load().mq_weight8_bytes(self.N, self.K)
+            if need == 0:
+                raise ValueError(f"no INT8 weight of {self.N} channels and {self.K} codes")
+            _need_out(Wq, (need,), torch.uint8, "Wq")
+            _need_out(s_w, (self.N,), torch.float32, "s_w")
+            _same_device(Wq, "Wq", s_w=s_w)
+            self._of = (Wq, s_w, (self.N, self.K, need, self.N))
+        return Wq.data_ptr(), s_w.data_ptr()
 
     @property
     def nbytes(self) -> int:
@@ -229,8 +243,9 @@ def repack_weight8(Wc, s_w, stream=None) -> PackedWeight8:
 def unpack_weight8(pw: PackedWeight8, stream=None):
     """Library layout -> canonical int8 codes [N, K]."""
     torch = _torch()
+    Wq, _ = pw._operands()
     Wc = _empty((pw.N, pw.K), torch.int8, pw.Wq.device, stream)
-    _check("mq_unpack_weight8", load().mq_unpack_weight8(pw.N, pw.K, pw.Wq.data_ptr(), Wc.data_ptr(), pw.K, _stream(stream)))
+    _check("mq_unpack_weight8", load().mq_unpack_weight8(pw.N, pw.K, Wq, Wc.data_ptr(), pw.K, _stream(stream)))
     return Wc
 
 
@@ -243,6 +258,7 @@ def gemm_w8a8(Xq8, s_x, pw: PackedWeight8, bias=None, out=None, out_dtype=None, 
     torch = _torch()
     ldx = _need_codes(Xq8, pw.K)
     M = Xq8.shape[0]
+    Wq, s_w = pw._operands()
     _need_out(s_x, (M,), torch.float32, "s_x")
     Y = out if out is not None else _empty((M, pw.N), out_dtype or torch.float16, Xq8.device, stream)
     code, ldy = _dtype_code(Y.dtype, "out", fp32=True), _need_rows(Y, "out", pw.N)
@@ -255,7 +271,7 @@ def gemm_w8a8(Xq8, s_x, pw: PackedWeight8, bias=None, out=None, out_dtype=None, 
     ws = lib.mq_gemm_w8a8_workspace_size(M, pw.N, pw.K)
     wbuf = _scratch(ws, Xq8.device, stream, workspace)
     _check("mq_gemm_w8a8", lib.mq_gemm_w8a8(
-        M, pw.N, pw.K, Xq8.data_ptr(), ldx, s_x.data_ptr(), pw.Wq.data_ptr(), pw.s_w.data_ptr(), code, _ptr(bias),
+        M, pw.N, pw.K, Xq8.data_ptr(), ldx, s_x.data_ptr(), Wq, s_w, code, _ptr(bias),
         Y.data_ptr(), ldy, _ptr(wbuf), ws, _stream(stream)))
     return Y
 

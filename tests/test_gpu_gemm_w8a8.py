@@ -186,3 +186,30 @@ def test_no_rows_of_an_odd_width():
     _, _, w, sw = operands(1, 32, 100)
     pw = m.repack_weight8(w.cuda(), sw.cuda())
     assert m.gemm_w8a8(torch.empty(0, 100, dtype=torch.int8).cuda(), torch.empty(0).cuda(), pw).shape == (0, 32)
+
+
+def test_weights_that_do_not_go_together():
+    """Codes and scales of another size than N and K say are refused before a kernel reads past them."""
+    m = mq()
+    x, sx, w, sw = operands(4, 64, 128)
+    x, sx = x.contiguous().cuda(), sx.cuda()
+    good = m.repack_weight8(w.cuda(), sw.cuda())
+    y = m.gemm_w8a8(x, sx, good)
+    short, cpu = good.Wq[:4096], good.Wq.cpu()
+    for error, pw in [
+        (ValueError, m.PackedWeight8(64, 128, short, good.s_w)),
+        (ValueError, m.PackedWeight8(65, 128, good.Wq, good.s_w)),
+        (ValueError, m.PackedWeight8(64, 128, good.Wq, good.s_w[:63])),
+        (TypeError, m.PackedWeight8(64, 128, good.Wq, good.s_w.half())),
+        (TypeError, m.PackedWeight8(64, 128, good.Wq.view(torch.int8), good.s_w)),
+        (TypeError, m.PackedWeight8(64, 128, cpu, good.s_w)),
+        (ValueError, m.PackedWeight8(0, 128, good.Wq, good.s_w)),
+    ]:
+        with pytest.raises(error):
+            m.gemm_w8a8(x, sx, pw)
+        with pytest.raises(error):
+            m.unpack_weight8(pw)
+    good.Wq = short                                         # replaced after it was used
+    with pytest.raises(ValueError):
+        m.gemm_w8a8(x, sx, good)
+    assert torch.equal(m.gemm_w8a8(x, sx, m.repack_weight8(w.cuda(), sw.cuda())), y)
