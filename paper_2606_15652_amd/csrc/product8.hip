@@ -473,7 +473,7 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
     if (!Xq8 || !s_x || !Wq8 || !s_w || !Y) return MQ_ERR_INVALID_ARG;
     const size_t size = type == MQ_FP32 ? 4 : 2;
     if (!mq_host::aligned(Xq8, 16) || !mq_host::aligned(Wq8, 16) || !mq_host::aligned(s_x, 4) || !mq_host::aligned(s_w, 4) ||
-        !mq_host::aligned(bias, size) || !mq_host::aligned(Y, size))
+        !mq_host::aligned(bias, size) || !mq_host::aligned(Y, size) || !mq_host::aligned(workspace, 16))
         return MQ_ERR_MISALIGNED;
     const size_t need = mq_gemm_w8a8_workspace_size(M, N, K);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;

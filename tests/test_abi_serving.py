@@ -172,3 +172,11 @@ def test_attention_kv4_defaults_are_within_the_limits(lib):
     status = lib.mq_attention_kv4(C.addressof(c), 64, 64 * 512, 4, 64 * 512, 8192, 0, A + 8, 512, 64, A, 128, A, A, 0.125, 1, A, 512, 64,
                                   None, 0, None)
     assert status == MISALIGNED
+
+
+def test_gemm_w8a8_workspace_alignment(lib):
+    M, N, K = 64, 4096, 14336                               # splits of K
+    need = lib.mq_gemm_w8a8_workspace_size(M, N, K)
+    assert need > 0
+    for off in (1, 4, 8):
+        assert lib.mq_gemm_w8a8(M, N, K, A, K, A, A, A, 0, None, A, N, A + off, need, None) == MISALIGNED
