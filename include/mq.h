@@ -470,6 +470,8 @@ mq_status mq_unpack_weight8(int N, int K, const uint8_t* Wq8, int8_t* Wc, int ld
  *               (may be NULL when that is 0).
  */
 size_t mq_gemm_w8a8_workspace_size(int M, int N, int K);
+/* Output tile of one workgroup of that launch, and the splits of K. */
+mq_status mq_gemm_w8a8_tile(int M, int N, int K, int* rows, int* cols, int* splits);
 mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ldx, const float* s_x,
                        const uint8_t* Wq8, const float* s_w, mq_dtype type, const void* bias,
                        void* Y, int ldy, void* workspace, size_t ws_bytes, hipStream_t stream);

@@ -69,6 +69,7 @@ _SIG = {
     "mq_repack_weight8": (_I, [_I, _I, _P, _I, _P, _P]),
     "mq_unpack_weight8": (_I, [_I, _I, _P, _P, _I, _P]),
     "mq_gemm_w8a8_workspace_size": (C.c_size_t, [_I, _I, _I]),
+    "mq_gemm_w8a8_tile": (_I, [_I, _I, _I, _P, _P, _P]),
     "mq_gemm_w8a8": (_I, [_I, _I, _I, _P, _I, _P, _P, _P, _I, _P, _P, _I, _P, C.c_size_t, _P]),
     "mq_kv4_code_bytes": (C.c_size_t, [_I, _I, _I, _I]),
     "mq_kv4_append": (_I, [_P, _I, _I, _P, _L, _L, _P, _L, _L, _P, _P]),
@@ -550,5 +551,5 @@ def prepare_weight(W, nnzb: int, criterion: str = "frob", X_calib=None, stream=N
 
 from .serving import (  # noqa: E402  (needs the names above)
     KVCache4, PackedWeight8, attention_kv4, attention_kv4_workspace_bytes, dequantize_act8, gemm_w8a8,
-    gemm_w8a8_workspace_bytes, kv4_append, kv4_cache, kv4_read, quantize_rows8, quantize_weight8, repack_weight8,
+    gemm_w8a8_tile, gemm_w8a8_workspace_bytes, kv4_append, kv4_cache, kv4_read, quantize_rows8, quantize_weight8, repack_weight8,
     rms_norm_quantize8, unpack_weight8)

@@ -460,6 +460,16 @@ extern "C" size_t mq_gemm_w8a8_workspace_size(int M, int N, int K) {
     return p.splits == 1 ? 0 : (size_t)p.splits * M * padded_n8(N) * sizeof(int);
 }
 
+extern "C" mq_status mq_gemm_w8a8_tile(int M, int N, int K, int* rows, int* cols, int* splits) {
+    if (!rows || !cols || !splits || M < 1 || M > (1 << 24)) return MQ_ERR_INVALID_ARG;
+    if (!shape8_ok(N, K)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const Plan8 p = plan8(M, N, K);
+    *rows = p.rows;
+    *cols = p.cols;
+    *splits = p.splits;
+    return MQ_OK;
+}
+
 extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ldx, const float* s_x, const uint8_t* Wq8,
                                   const float* s_w, mq_dtype type, const void* bias, void* Y, int ldy, void* workspace,
                                   size_t ws_bytes, hipStream_t stream) {

@@ -253,6 +253,13 @@ def gemm_w8a8_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(load().mq_gemm_w8a8_workspace_size(M, N, K))
 
 
+def gemm_w8a8_tile(M: int, N: int, K: int):
+    """(rows, columns) of the output tile one workgroup takes, and the splits of K (host logic only)."""
+    r, c, s = C.c_int(0), C.c_int(0), C.c_int(0)
+    _check("mq_gemm_w8a8_tile", load().mq_gemm_w8a8_tile(M, N, K, C.byref(r), C.byref(c), C.byref(s)))
+    return r.value, c.value, s.value
+
+
 def gemm_w8a8(Xq8, s_x, pw: PackedWeight8, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
     """Y [M, N] = s_x s_w (Xq8 Wq^T) + bias, in fp16 (or ``out_dtype`` bf16, fp32); bias in Y's type."""
     torch = _torch()

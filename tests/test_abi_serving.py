@@ -180,3 +180,29 @@ def test_gemm_w8a8_workspace_alignment(lib):
     assert need > 0
     for off in (1, 4, 8):
         assert lib.mq_gemm_w8a8(M, N, K, A, K, A, A, A, 0, None, A, N, A + off, need, None) == MISALIGNED
+
+
+# (M, N, K): output tile and splits of K, one at least for every kernel that the W8A8 product has
+W8A8_TILES = [
+    ((1, 14336, 4096), (16, 64, 1)), ((4, 8192, 8192), (16, 32, 1)), ((16, 1000, 512), (16, 16, 1)),
+    ((32, 4096, 4096), (32, 32, 1)), ((19, 4099, 1000), (32, 32, 1)), ((17, 255, 64), (32, 16, 1)),
+    ((130, 129, 14335), (64, 64, 4)), ((257, 1500, 8192), (64, 64, 2)), ((33, 512, 64), (64, 64, 1)),
+    ((300, 1024, 28672), (128, 64, 4)), ((65, 3001, 8192), (128, 64, 4)), ((257, 4099, 14336), (128, 64, 2)), ((77, 25599, 640), (128, 64, 1)),
+    ((700, 8201, 1000), (128, 128, 1)), ((2050, 4099, 513), (256, 256, 1)),
+]
+
+
+@pytest.mark.parametrize("shape,expect", W8A8_TILES, ids=[f"M{m}_N{n}_K{k}" for (m, n, k), _ in W8A8_TILES])
+def test_gemm_w8a8_tile(lib, shape, expect):
+    import paper_2606_15652_amd as mq
+    assert mq.gemm_w8a8_tile(*shape) == expect
+    M, N, _ = shape
+    splits = expect[2]
+    assert mq.gemm_w8a8_workspace_bytes(*shape) == (0 if splits == 1 else splits * M * -(-N // 64) * 64 * 4)
+
+
+def test_gemm_w8a8_tile_validation(lib):
+    r = C.byref(C.c_int(0))
+    f = lib.mq_gemm_w8a8_tile
+    assert f(0, 64, 64, r, r, r) == INVALID and f(1, 64, 64, r, r, None) == INVALID and f(1, 64, 64, None, r, r) == INVALID
+    assert f(1, 0, 64, r, r, r) == SHAPE and f(1, 64, 131057, r, r, r) == SHAPE

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import serving_oracle as so
+from test_abi_serving import W8A8_TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -213,3 +214,10 @@ def test_weights_that_do_not_go_together():
     with pytest.raises(ValueError):
         m.gemm_w8a8(x, sx, good)
     assert torch.equal(m.gemm_w8a8(x, sx, m.repack_weight8(w.cuda(), sw.cuda())), y)
+
+
+@pytest.mark.parametrize("shape,expect", W8A8_TILES, ids=[f"M{m}_N{n}_K{k}" for (m, n, k), _ in W8A8_TILES])
+def test_every_kernel(shape, expect):
+    assert mq().gemm_w8a8_tile(*shape) == expect
+    for dtype in (torch.float16, torch.bfloat16, torch.float32):
+        check(*shape, dtype, bias=dtype != torch.float32, seed=4)
