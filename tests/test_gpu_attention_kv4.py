@@ -445,3 +445,11 @@ def test_queries_that_are_not_finite_change_no_others(nqs, q_spread, bad):
         if b == 0:
             fine[0, 1] = True
         assert fine.all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group,nqs", [(1, None), (2, None), (3, None), (5, None), (8, None), (9, None), (16, None), (40, None),
+                                       (1, [2, 1, 0, 2]), (1, [4, 3, 4, 1]), (4, [2, 2, 1, 2]), (3, [5, 1, 5, 4]), (8, [8, 8, 2, 8])])
+def test_long_contexts_of_every_number_of_columns(group, nqs, dim):
+    """Contexts cut into shares, by blocks of 4 (one, two or more queries in use), 8 and 16 columns, one block or several."""
+    check([4999, 1100, 0, 70], nqs, 2, group, dim, 32, DTYPES[group % 2], seed=group)
