@@ -40,7 +40,7 @@ constexpr int kLeastSteps = 4;          // of a workgroup
 // What beginning and ending a unit takes, in steps of a workgroup (64 ragged contexts of up to 8191 tokens:
 // none counted 82.7 us, 4 68.6, 12 66.7, 24 69.0).
 constexpr int kUnitSteps = 12;
-constexpr float kLowest = -1e30f;       // below every score: running maximum of none
+constexpr float kLowest = -FLT_MAX;     // no score is lower: running maximum of none
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;          // weights up to 2^kSlack before the running maximum moves
 
@@ -145,7 +145,7 @@ struct Queries {
         }
         of_minimum = ldexpf(of_minimum, up - 24);
     }
-    // never zero or infinite, so that a hidden token's -infinity stays that
+    // never zero or infinite: a scale or minimum of zero times it stays zero
     static __device__ __forceinline__ float to_score(float scale, int up) {
         return fminf(fmaxf(ldexpf(scale * kLog2e, 24 - up), FLT_MIN), FLT_MAX);
     }
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             if (wave == 0) shared_q[i][lane] = mq.op[i];
 #pragma unroll
         for (int e = 0; e < R; ++e) {
-            of_minimum[e] = __shfl(mq.of_minimum, mine + e);
+            of_minimum[e] = __shfl(mq.of_minimum, mine + e) * to_score;
         }
         __syncthreads();
     }
@@ -398,8 +398,10 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             // queries that see it, and its weight 0 stays 0
             const float bad = __builtin_fmaf((float)v[0], 0.0f, 0.0f);
             vps[i] = v[0] == v[0] ? vp[i] : 0u;
+            // in powers of 2 from here on: less their maximum, itself one of them, scores of any size are exact
+            const float sk = (float)k[0] * to_score;
 #pragma unroll
-            for (int e = 0; e < R; ++e) x[i][e] = __builtin_fmaf(x[i][e], (float)k[0], __builtin_fmaf((float)k[1], of_minimum[e], bad));
+            for (int e = 0; e < R; ++e) x[i][e] = __builtin_fmaf(x[i][e], sk, __builtin_fmaf((float)k[1], of_minimum[e], bad));
         }
         __builtin_amdgcn_sched_barrier(0);
         load_keys(pages, then);
@@ -431,7 +433,6 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             top[e] = x[0][e];
 #pragma unroll
             for (int i = 1; i < NT; ++i) top[e] = fmaxf(top[e], x[i][e]);
-            top[e] *= to_score;
             moves = moves || top[e] > m[e] + kSlack;
         }
         moves = moves || most > 0x1p7f * unit;
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(256, 2) void attention4_kernel(Attn4Args a) {
             const float by = sv[i] * per_unit, off = -7.5f * unit;
 #pragma unroll
             for (int e = 0; e < R; ++e) {
-                const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][e], to_score, -m[e]));
+                const float pe = __builtin_amdgcn_exp2f(x[i][e] - m[e]);
                 l[e] += pe;
                 const _Float16 w = (_Float16)(pe * by);
                 rest[e] = __builtin_fmaf((float)w, off, __builtin_fmaf(pe, middle[i], rest[e]));

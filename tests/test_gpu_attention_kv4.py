@@ -453,3 +453,24 @@ def test_queries_that_are_not_finite_change_no_others(nqs, q_spread, bad):
 def test_long_contexts_of_every_number_of_columns(group, nqs, dim):
     """Contexts cut into shares, by blocks of 4 (one, two or more queries in use), 8 and 16 columns, one block or several."""
     check([4999, 1100, 0, 70], nqs, 2, group, dim, 32, DTYPES[group % 2], seed=group)
+
+
+@pytest.mark.parametrize("n,nq", [(300, 1), (5000, 1), (300, 3), (5000, 70)])
+def test_scores_far_below_zero(n, nq):
+    """Every score below -1e30: the highest takes all the weight all the same."""
+    m = mq()
+    g = so.generator(n, 61)
+    k, v = torch.zeros(n, 1, 64), torch.randn(n, 1, 64, generator=g).bfloat16()
+    k[:, 0, 0] = 2.0 + torch.randperm(n, generator=g) % 60 / 16
+    k[n // 3, 0, 0] = 1.0                                   # seen by all
+    k = k.bfloat16()
+    cache = m.kv4_cache(-(-n // 16), 16, 1, 64)
+    m.kv4_append(cache, k.cuda(), v.cuda(), torch.arange(n).cuda())
+    q = torch.zeros(nq, 1, 64).bfloat16()
+    q[..., 0] = -1e32
+    o = m.attention_kv4(q.cuda(), cache, torch.arange(-(-n // 16), dtype=torch.int32)[None].cuda(), torch.tensor([n], dtype=torch.int32).cuda(),
+                        cu_q=torch.tensor([0, nq], dtype=torch.int32).cuda(), scale=1.0).cpu().double()
+    want = so.values4(v)[n // 3, 0]
+    spread = (v.float().amax() - v.float().amin()).item()
+    tol = (2.0 ** -11 + 2.0 ** -25) * spread * 1.01 + 2.0 ** -22 * want.abs().max() + so.UNIT[torch.bfloat16] * want.abs() * 1.01
+    assert ((o[:, 0] - want).abs() <= tol).all()
