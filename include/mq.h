@@ -388,6 +388,9 @@ mq_status mq_linear_noalloc(int M, int N, int K, const void* X, int ldx,
 /* Around the layers: norm, 8-bit product, 4-bit cache and its attention     */
 /* ======================================================================== */
 
+/* A launch has less than 2^32 threads: calls of this part that would need more
+ * (upwards of 3 10^10 values) return MQ_ERR_UNSUPPORTED_SHAPE. */
+
 /* Types of values that are not codes. */
 typedef enum mq_dtype { MQ_FP16 = 0, MQ_BF16 = 1, MQ_FP32 = 2 } mq_dtype;
 

@@ -155,12 +155,19 @@ Cache4 device_cache4(const mq_kv4_cache* c) {
                   static_cast<uint32_t*>(c->v_params), c->pages, c->heads, __builtin_ctz((unsigned)c->page_size)};
 }
 
+// workgroups of four waves, of 512 / head_dim rows each
+static int64_t row_blocks(const mq_kv4_cache* c, int T) {
+    const int rows = 512 / c->head_dim;
+    return (((int64_t)T + rows - 1) / rows * c->heads + 3) / 4;
+}
+
 static mq_status check_rows(const mq_kv4_cache* c, int T, const void* K, int64_t kt, int64_t kh, const void* V, int64_t vt,
                             int64_t vh, const int64_t* slots, mq_dtype type) {
     if (T < 0 || !mq_host::is_half_type(type)) return MQ_ERR_INVALID_ARG;
     if (mq_status st = check_cache4(c); st != MQ_OK) return st;
     for (int64_t s : {kt, kh, vt, vh})
         if (s < 0 || s % 8 != 0) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (!mq_host::launch_holds(row_blocks(c, T), 256)) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (T == 0) return MQ_OK;
     if (!K || !V || !slots) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(K, 16) || !mq_host::aligned(V, 16) || !mq_host::aligned(slots, 8)) return MQ_ERR_MISALIGNED;
@@ -170,9 +177,7 @@ static mq_status check_rows(const mq_kv4_cache* c, int T, const void* K, int64_t
 template <typename F>
 static mq_status launch_rows(const mq_kv4_cache* c, int T, mq_dtype type, F&& run) {
     if (T == 0) return MQ_OK;
-    const int rows = 512 / c->head_dim;
-    const int64_t units = ((int64_t)T + rows - 1) / rows * c->heads, blocks = (units + 3) / 4;
-    if (blocks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const int64_t blocks = row_blocks(c, T);
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         if (c->head_dim == 64) run(T{}, std::integral_constant<int, 64>{}, dim3((unsigned)blocks));

@@ -324,6 +324,9 @@ inline bool shape_ok(int N, int K) {
            K <= (1 << 20) && N <= (1 << 24);
 }
 
+// Whether a launch holds that many workgroups: its threads are counted in 32 bits, and more are cut, without an error.
+inline bool launch_holds(int64_t blocks, int threads) { return blocks * threads <= (int64_t)UINT32_MAX; }
+
 inline mq_status launch_status() {
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? MQ_OK : MQ_ERR_HIP;

@@ -204,18 +204,21 @@ struct NormArgs {
     void* s_x;
 };
 
+// threads of a row: one for 16 values, a wave at least
+static int norm_threads(int K) { return std::min(((K + 15) / 16 + 63) / 64 * 64, kNormMaxThreads); }
+
 template <typename T, bool NORM, bool A8>
 static mq_status launch_norm(const NormArgs& a, hipStream_t stream) {
-    auto run = [&](auto kernel, int threads) {
-        hipLaunchKernelGGL(kernel, dim3(a.M), dim3(threads), 0, stream, static_cast<const T*>(a.X),
+    auto run = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(a.M), dim3(norm_threads(a.K)), 0, stream, static_cast<const T*>(a.X),
                            static_cast<const T*>(a.R), static_cast<const T*>(a.gamma), static_cast<T*>(a.H), a.M, a.K,
                            a.ldx, a.ldr, a.ldh, a.eps, static_cast<uint8_t*>(a.Xq), a.ldq, a.s_x);
         return mq_host::launch_status();
     };
-    const int pieces = (a.K + 15) / 16, threads = (pieces + 63) / 64 * 64;
-    if (pieces <= kNormMaxThreads) return run(norm_quant_kernel<T, NORM, A8, 1>, threads);
-    if (pieces <= 2 * kNormMaxThreads) return run(norm_quant_kernel<T, NORM, A8, 2>, kNormMaxThreads);
-    return run(norm_quant_kernel<T, NORM, A8, 4>, kNormMaxThreads);
+    const int pieces = (a.K + 15) / 16;
+    if (pieces <= kNormMaxThreads) return run(norm_quant_kernel<T, NORM, A8, 1>);
+    if (pieces <= 2 * kNormMaxThreads) return run(norm_quant_kernel<T, NORM, A8, 2>);
+    return run(norm_quant_kernel<T, NORM, A8, 4>);
 }
 
 // K and leading dimensions that the row kernels take.
@@ -239,7 +242,8 @@ extern "C" mq_status mq_rms_norm_quantize8(int M, int K, mq_dtype type, const vo
                                            void* Xq8, int ldq, void* s_x, hipStream_t stream) {
     if (!mq_host::is_half_type(type) || !(eps >= 0.0f)) return MQ_ERR_INVALID_ARG;
     if (mq_status st = check_codes(M, K, layout, Xq8, ldq, s_x); st != MQ_OK) return st;
-    if (!rows_ok(K, ldx) || (R && (!rows_ok(K, ldr) || !rows_ok(K, ldh)))) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (!rows_ok(K, ldx) || (R && (!rows_ok(K, ldr) || !rows_ok(K, ldh))) || !mq_host::launch_holds(M, norm_threads(K)))
+        return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
     if (!X || !gamma || (R != nullptr) != (H != nullptr)) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(X, 16) || !mq_host::aligned(R, 16) || !mq_host::aligned(gamma, 16) || !mq_host::aligned(H, 16))
@@ -255,7 +259,7 @@ extern "C" mq_status mq_quantize_rows8(int M, int K, mq_dtype type, const void* 
                                        void* s_x, hipStream_t stream) {
     if (!mq_host::is_half_type(type)) return MQ_ERR_INVALID_ARG;
     if (mq_status st = check_codes(M, K, MQ_ACT8_ROWS, Xq8, ldq, s_x); st != MQ_OK) return st;
-    if (!rows_ok(K, ldx)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (!rows_ok(K, ldx) || !mq_host::launch_holds(M, norm_threads(K))) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
     if (!X) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(X, 16)) return MQ_ERR_MISALIGNED;
@@ -267,12 +271,11 @@ extern "C" mq_status mq_dequantize_act8(int M, int K, mq_act8_layout layout, con
                                         mq_dtype type, void* Y, int ldy, hipStream_t stream) {
     if (!mq_host::is_half_type(type)) return MQ_ERR_INVALID_ARG;
     if (mq_status st = check_codes(M, K, layout, Xq8, ldq, s_x); st != MQ_OK) return st;
-    if (!rows_ok(K, ldy)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const int threads = std::min((K / 8 + 63) / 64 * 64, 256), chunks = (K / 8 + threads - 1) / threads;
+    if (!rows_ok(K, ldy) || !mq_host::launch_holds((int64_t)M * chunks, threads)) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
     if (!Y) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(Y, 16)) return MQ_ERR_MISALIGNED;
-    const int threads = std::min((K / 8 + 63) / 64 * 64, 256), chunks = (K / 8 + threads - 1) / threads;
-    if ((int64_t)M * chunks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto kernel) {

@@ -350,12 +350,12 @@ __global__ __launch_bounds__(1024) void pack_weight8_kernel(From from, int N, in
 
 __global__ __launch_bounds__(256) void unpack_weight8_kernel(const uint8_t* __restrict__ Wq, int N, int K,
                                                              int8_t* __restrict__ Wc, int64_t ldw) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)N * K) return;
-    const int n = (int)(i / K), k = (int)(i % K), c = n % kBlock8;
-    const int row = c / 16 * 4 + c % 4, piece = c % 16 / 4;     // channel8's inverse
-    const int64_t at = ((int64_t)(n / kBlock8) * (padded_k8(K) / kPieceK) + k / kPieceK) * 4 + piece;
-    Wc[n * ldw + k] = (int8_t)Wq[at * kPieceBytes + 16 * (row + 16 * (k % kPieceK / 16)) + k % 16];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)N * K; i += (int64_t)gridDim.x * 256) {
+        const int n = (int)(i / K), k = (int)(i % K), c = n % kBlock8;
+        const int row = c / 16 * 4 + c % 4, piece = c % 16 / 4;     // channel8's inverse
+        const int64_t at = ((int64_t)(n / kBlock8) * (padded_k8(K) / kPieceK) + k / kPieceK) * 4 + piece;
+        Wc[n * ldw + k] = (int8_t)Wq[at * kPieceBytes + 16 * (row + 16 * (k % kPieceK / 16)) + k % 16];
+    }
 }
 
 static bool shape8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
@@ -448,8 +448,8 @@ extern "C" mq_status mq_unpack_weight8(int N, int K, const uint8_t* Wq8, int8_t*
     if (!shape8_ok(N, K) || ldw < K) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (!Wc || !Wq8) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(Wq8, 16)) return MQ_ERR_MISALIGNED;
-    const int64_t blocks = ((int64_t)N * K + 255) / 256;
-    if (blocks > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
+    // a launch has less than 2^32 threads; the rest of the codes come in further turns
+    const int64_t blocks = std::min<int64_t>(((int64_t)N * K + 255) / 256, 1 << 22);
     hipLaunchKernelGGL(unpack_weight8_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, Wq8, N, K, Wc, ldw);
     return mq_host::launch_status();
 }
@@ -477,6 +477,10 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
     if (M > (1 << 24) || !shape8_ok(N, K) || ldx < (K + 15) / 16 * 16 || ldx % 16 != 0 || ldy < N) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
     const Plan8 p = plan8(M, N, K);
+    const int64_t groups = p.streams ? (int64_t)((N + kBlock8 - 1) / kBlock8) * (kBlock8 / p.cols)
+                                     : (int64_t)((M + p.rows - 1) / p.rows) * ((N + p.cols - 1) / p.cols);
+    const int64_t joins = p.splits > 1 ? ((int64_t)M * (padded_n8(N) / 16) + 255) / 256 : 0;
+    if (!mq_host::launch_holds(groups, 512) || !mq_host::launch_holds(joins, 256)) return MQ_ERR_UNSUPPORTED_SHAPE;
     // offsets within a wave's rows: 32 bits, of which the tiled kernels' loads past the end take the upper half
     if ((int64_t)(std::min(M, kWaveRows) - 1) * ldx + (K + 15) / 16 * 16 > (p.streams ? (int64_t)UINT32_MAX : INT32_MAX))
         return MQ_ERR_UNSUPPORTED_SHAPE;
@@ -491,9 +495,6 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
                          mq_host::aligned(Y, 16) && ldy * size % 16 == 0};
     auto run = [&](auto z) {
         using T = decltype(z);
-        const int64_t groups = p.streams ? (int64_t)((N + kBlock8 - 1) / kBlock8) * (kBlock8 / p.cols)
-                                         : (int64_t)((M + p.rows - 1) / p.rows) * ((N + p.cols - 1) / p.cols);
-        if (groups > INT32_MAX) return MQ_ERR_UNSUPPORTED_SHAPE;
         int* part = static_cast<int*>(workspace);
         auto stream_rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * kStreamWaves), 0, stream, a); };
         auto tile = [&](auto kernel, int threads) {
@@ -518,7 +519,6 @@ extern "C" mq_status mq_gemm_w8a8(int M, int N, int K, const int8_t* Xq8, int ld
             else tile(product8_tiled_kernel<T, 4, 1, 1, 4, false>, 256);
         }
         if (p.splits > 1) {
-            const int64_t joins = ((int64_t)M * (padded_n8(N) / 16) + 255) / 256;
             hipLaunchKernelGGL(product8_join_kernel<T>, dim3((unsigned)joins), dim3(256), 0, stream, a, p.splits, part);
         }
         return mq_host::launch_status();

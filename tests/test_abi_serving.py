@@ -206,3 +206,25 @@ def test_gemm_w8a8_tile_validation(lib):
     f = lib.mq_gemm_w8a8_tile
     assert f(0, 64, 64, r, r, r) == INVALID and f(1, 64, 64, r, r, None) == INVALID and f(1, 64, 64, None, r, r) == INVALID
     assert f(1, 0, 64, r, r, r) == SHAPE and f(1, 64, 131057, r, r, r) == SHAPE
+
+
+def test_launches_past_32_bits_of_threads(lib):
+    """Such launches are cut by the runtime without an error; what fits is refused for an address only."""
+    norm = lambda M, K: lib.mq_rms_norm_quantize8(M, K, 0, A + 2, K, None, 0, A, 1e-5, None, 0, 0, A, K, A, None)      # noqa: E731
+    rows = lambda M, K: lib.mq_quantize_rows8(M, K, 0, A + 2, K, A, K, A, None)                                        # noqa: E731
+    values = lambda M, K: lib.mq_dequantize_act8(M, K, 0, A, K, A, 0, A + 2, K, None)                                  # noqa: E731
+    for f in (norm, rows):
+        assert f((1 << 22) - 1, 16384) == MISALIGNED and f(1 << 22, 16384) == SHAPE and f(1 << 24, 2048) == MISALIGNED
+    assert values((1 << 24) - 1, 2048) == MISALIGNED and values(1 << 24, 2048) == SHAPE and values(1 << 22, 16384) == SHAPE
+    c = cache(heads=64, head_dim=128)
+
+    def append(T):
+        return lib.mq_kv4_append(C.addressof(c), T, 0, A + 2, 0, 0, A, 0, 0, A, None)
+
+    def read(T):
+        return lib.mq_kv4_read(C.addressof(c), T, 0, A, A + 2, 0, 0, A, 0, 0, None)
+    most = ((1 << 24) - 1) * 4 // 64 * 4                    # workgroups of four waves of four rows
+    for f in (append, read):
+        assert f(most) == MISALIGNED and f(most + 1) == SHAPE
+    gemm = lambda M, N, K: lib.mq_gemm_w8a8(M, N, K, A, 16, A, A, A, 0, None, A + 1, N, A, 1 << 62, None)              # noqa: E731
+    assert gemm(1 << 20, 65536, 16) == MISALIGNED and gemm(1 << 24, 1 << 24, 16) == SHAPE

@@ -221,3 +221,19 @@ def test_every_kernel(shape, expect):
     assert mq().gemm_w8a8_tile(*shape) == expect
     for dtype in (torch.float16, torch.bfloat16, torch.float32):
         check(*shape, dtype, bias=dtype != torch.float32, seed=4)
+
+
+def test_a_weight_past_32_bits():
+    """More than 2^32 codes: laid out, read back, and multiplied."""
+    m = mq()
+    N, K = 1 << 20, 4112
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    w = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    pw = m.repack_weight8(w, torch.ones(N, device="cuda"))
+    assert pw.Wq.numel() > 1 << 32 and torch.equal(m.unpack_weight8(pw), w)
+    x = torch.randint(-128, 128, (40, K), generator=g, device="cuda", dtype=torch.int8)
+    for rows in (3, 40):
+        y = m.gemm_w8a8(x[:rows], torch.ones(rows, device="cuda"), pw, out_dtype=torch.float32)
+        for n in (0, N // 2 + 77, N - 1):
+            assert torch.equal(y[:, n].double(), (x[:rows].double() * w[n].double()).sum(1).float().double())
