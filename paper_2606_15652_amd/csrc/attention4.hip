@@ -120,20 +120,29 @@ struct Queries {
     f32x8 x[D / 32];
 
     template <typename T>
-    __device__ __forceinline__ void load(const T* q) {      // amax: of the 16 columns; a column that is not finite spoils no other
-        of_minimum = amax = 0.0f;
+    __device__ __forceinline__ void load(const T* q) {
+        of_minimum = 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
             x[i] = load8(q + 8 * i);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                of_minimum += x[i][e];
-                amax = fmaxf(amax, fabsf(x[i][e]) < INFINITY ? fabsf(x[i][e]) : 0.0f);
-            }
+            for (int e = 0; e < 8; ++e) of_minimum += x[i][e];
         }
         of_minimum = quads_sum(of_minimum);
+        amax = largest([](float v) { return v; });
+        // a column that is not finite spoils no other
+        if (amax == INFINITY) amax = largest([](float v) { return v < INFINITY ? v : 0.0f; });
+    }
+    template <typename F>
+    __device__ __forceinline__ float largest(F of) const {  // of the 16 columns' values without their signs; NaN is none
+        float v = 0.0f;
 #pragma unroll
-        for (int i = 1; i < 64; i <<= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v = fmaxf(v, of(fabsf(x[i][e])));
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) v = fmaxf(v, __shfl_xor(v, i));
+        return v;
     }
     static __device__ __forceinline__ int exponent(float amax) { return amax > 0.0f ? 8 - ilogbf(amax) : 0; }
     __device__ __forceinline__ void finish(int up) {
