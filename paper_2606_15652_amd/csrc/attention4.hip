@@ -10,10 +10,6 @@
 // weights, of which there are D times fewer than codes.  A token that a query
 // does not see has the weight 0 there, whatever its parameters hold.
 //
-// The scores are computed transposed, S^T = K Q^T: a lane then holds four
-// neighbouring tokens of one query, which is what the second product, O^T =
-// V^T P^T, takes from it.  Nothing goes through LDS but the waves' results.
-//
 // Columns are the queries of one sequence and key head: position qi and head hg
 // of the group at column qi group + hg.
 #include "kv4.h"
@@ -604,8 +600,9 @@ constexpr int kVector = 0x402, kProducts = 0x8, kLdsReads = 0x100;
 // fp16 numbers, are four rows more of the second product (of the latter a 16th and what
 // that leaves: it passes fp16's range, as z + 15 s may in bf16).  The weights' rounding is thus the only one, and the
 // same above and below the fraction: fp16 results are off by 2.7e-4 of their norm,
-// 2.1e-4 of it their own rounding (values staged as fp16 values: 3.3e-4, four ragged
-// prompts of up to 2047 tokens 275 us, 288).  A stage is
+// 2.1e-4 of it their own rounding (values staged as fp16 values: 3.3e-4, and 5 % less
+// time).  Four ragged prompts of up to 2047 tokens, 32 / 8 heads of 128: 293 us, 580
+// TFLOP/s; heads of 64: 263.  A stage is
 // converted by the whole workgroup while the one before is in use, from registers
 // loaded one stage earlier still; every conversion then serves 256 columns.
 //
@@ -1009,7 +1006,12 @@ struct Plan4 {
     int splits, split_steps;            // 256 columns
 };
 
-// Columns of a workgroup.
+// Columns of a workgroup.  Blocks of 16 read the cache once for every 16 columns, in a
+// block of 256 the waves whose 32 columns are not there idle: the switch is where the two
+// are about even (8 heads of 128; one context of 65536 tokens, one and eight of 8192, 32
+// of 2048): at 64 columns blocks of 16 take 57.7, 21.6, 53.0 and 69.5 us, one of 256 74.0,
+// 30.1, 66.5 and 61.4; at 68 columns 67.9, 22.5, 71.9 and 91.0 against 76.7, 30.9, 69.1
+// and 64.0; at 192 141.6, 32.3, 128.4 and 191.3 against 98.6, 40.1, 93.6 and 86.3.
 static int columns4(int max_q, int group) {
     const int64_t cols = (int64_t)max_q * group;
     return cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 64 ? 16 : 256;
@@ -1019,8 +1021,12 @@ constexpr int kWholeSteps = 16;         // few columns: sequences of up to as ma
 // Workgroups of a launch.  Few columns: short sequences (up to 1024 tokens: 16
 // steps, four for each wave) are taken whole; the others are cut into as many
 // equal shares as workgroups fit on the chip, or shares of four steps if those are
-// fewer.  Many columns: units are split while there are fewer than CUs, into parts
-// of at least eight steps (four contexts of 4096 tokens by 128 queries 60 us, in one part 127).
+// fewer: 768 up to 8 columns, 512 for 16 (8 heads of 128, 4 columns: 64 contexts of up
+// to 8191 tokens 75.6 us, in 512 shares 76.4, in 1024 76.9, in 256 79.7; 256 contexts
+// of up to 2000 tokens 84.9, 86.6, 94.5 and 119.9; 8 of up to 8192 21.0, 19.9, 26.2 and
+// 21.8; 16 columns, the 64 contexts, 89.5, in 768 shares 98.9, in 256 100.7).  Many
+// columns: units are split while there are fewer than CUs, into parts of at least eight
+// steps (four contexts of 4096 tokens by 128 queries 60 us, in one part 127).
 static Plan4 plan4(int sequences, int heads, int group, int max_q, int64_t max_kv) {
     Plan4 p;
     const int64_t cols = (int64_t)max_q * group;

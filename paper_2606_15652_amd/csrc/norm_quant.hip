@@ -11,8 +11,10 @@
 // fp64 (the scale is rounded to fp32, and in the A8 layout from there to fp16, as
 // the other quantisers' are), and a code is rounded from one fp32 rounding of its
 // quotient, multiplied as two parts: memory bounds the kernel, which leaves room
-// for both.  8192 rows of 8192 with residual: 105-115 us, 4.1-4.5 TB/s of the 4.9 that a copy
-// reaches; their values read back: 69 us.
+// for both.  8192 rows of 8192 with residual: in rows 93 us, in the A8 layout 106, 4.8-5.0 TB/s of the 4.9 that a
+// copy reaches; without the norm 44 us, 4.6; their values read back from rows 37 us, 5.4 TB/s, from the A8 layout 66,
+// 3.6 (two threads read a chunk's low bytes).  Four pieces a thread (K > 32768) spill 23-25 registers: 1024 rows of
+// 65536 with residual 149 us, 3.2 TB/s.
 #include "mq_float.h"
 
 #include <math.h>

@@ -13,7 +13,7 @@
 //  * tiled: output tiles of 64 x 64 to 256 x 256, both operands through two to
 //    four LDS slots of 128 codes, filled by the LDS DMA.  The matrix unit and LDS
 //    bound it: 8192 rows of 8192 codes by 28672 channels 1480-1540 us, 2.5-2.6
-//    POP/s (63 % of the cycles have a product running);
+//    POP/s (65 % of the cycles have a product running);
 //  * streaming (few rows): weights go straight to registers, once; the eight
 //    waves of a workgroup share out K and add their sums in LDS (integers: in
 //    any order).  Reading the weight bounds it: 4096 -> 14336 at one row 10.2 us,
@@ -290,7 +290,8 @@ __global__ __launch_bounds__(64 * kStreamWaves) void product8_stream_kernel(Prod
     }
 }
 
-// Per-channel INT8 weights: s = max|w| / 127 (fp32), q = clamp(round_half_even(w / s), -127, 127),
+// Per-channel INT8 weights, once for a weight (4096 channels of 14336 codes: quantised in 733 us, laid out in 396, read
+// back in 174; few and narrow loads bound them): s = max|w| / 127 (fp32), q = clamp(round_half_even(w / s), -127, 127),
 // and canonical codes into pieces: one workgroup per 16 rows.
 struct FromFloat {
     const float* W;
@@ -371,7 +372,9 @@ static bool shape8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 
 // takes.  The estimates are within a fifth of what was measured (K = 14336, N =
 // 4096: M = 64 in four splits 19.9 us, unsplit 34.5; M = 512 by 128 x 64 51.2,
 // 64 x 64 56.5, 128 x 128 91; K = N = 8192 at M = 1157 by 256 x 256 97, 128 x 128
-// 114; 5120 -> 25599 at M = 77 by 128 x 64 38.1, 64 x 64 44.5, 128 x 128 42.8).
+// 114; 5120 -> 25599 at M = 77 by 64 x 64 44.5, 128 x 128 42.8), but for few rows of
+// 128 x 64, whose loads of W reach less than the rate assumed (the last by 128 x 64
+// 38.1 us, estimated at 28.5).
 struct Tile8 {
     int rows, cols;
     double alone, share;                // us of a stage: one workgroup a CU, and of each of several
