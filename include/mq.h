@@ -563,6 +563,79 @@ mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, int tokens,
                            void* O, int64_t o_token, int64_t o_head,
                            void* workspace, size_t ws_bytes, hipStream_t stream);
 
+/*
+ * Paged cache of keys and values in 8 bits (OCP e4m3).  Pages hold page_size tokens (a
+ * power of two, 32 .. 65536) of every key head; head_dim is 64 or 128.  A slot is
+ * page * page_size + the place in the page.  Each block of 32 tokens of a page and
+ * head has a scale 2^e for its keys and one for its values:
+ *     e = least integer >= -127 with max |x| <= 448 2^e over the block's tokens,
+ *     n = e4m3(x 2^-e)  (ties to even);  the value is n 2^e.
+ * A token of a head whose key or value holds infinity or NaN has the key NaN and
+ * the value 0, and does not count in e.
+ *   k, v               : mq_kv8_code_bytes() bytes each, 16-byte aligned,
+ *     [pages][heads][page_size / 32] blocks of 32 head_dim bytes.  Byte of channel c of
+ *     the block's token t:
+ *     keys   16 head_dim (t / 16) + 1024 (c / 64) + 16 (16 (c % 64 / 16) + t % 16) + c % 16,
+ *     values 1024 (c / 32) + 16 (16 (t % 16 / 4) + c % 16) + 8 (c % 32 / 16) + 4 (t / 16) + t % 4.
+ *   k_scales, v_scales : uint8 [pages][heads][page_size / 32], e + 127.
+ * The caller clears all four once (zeros are valid blocks).  Values' codes are never
+ * NaN (0x7F, 0xFF): the attention multiplies those of tokens that it does not see by 0.
+ */
+typedef struct mq_kv8_cache {
+    void *k, *v, *k_scales, *v_scales;
+    int pages, page_size, heads, head_dim;
+} mq_kv8_cache;
+
+size_t mq_kv8_code_bytes(int pages, int page_size, int heads, int head_dim);
+
+/*
+ * Adds tokens to the ends of sequences.  Sequence b has kv_lens[b] tokens, the new
+ * ones among them: rows cu_new[b] .. cu_new[b + 1] - 1 of the T rows of K and V
+ * (cu_new NULL: row b, T == sequences); token t is in place t % page_size of page
+ * page_table[b][t / page_size].  Where new tokens raise a block's e, the codes of the
+ * block's earlier tokens are divided by that power of two (ties to even; exact unless
+ * they fall below 2^-6).  What lies in a block behind kv_lens[b] counts for
+ * nothing and may change.  A block belongs to one sequence of the call.
+ *   K, V       : `type` (MQ_FP16 or MQ_BF16), token t's head h at t k_token + h k_head
+ *                (elements, multiples of 8), head_dim contiguous values, 16-byte aligned.
+ *   page_table : int32 [sequences, table_pages]; tokens past it, or of a page outside
+ *                [0, pages), are skipped.
+ *   kv_lens    : int32 [sequences];  cu_new : int32 [sequences + 1], ascending from 0 to T.
+ */
+mq_status mq_kv8_append(const mq_kv8_cache* cache, int sequences, int T, mq_dtype type,
+                        const void* K, int64_t k_token, int64_t k_head,
+                        const void* V, int64_t v_token, int64_t v_head,
+                        const int32_t* page_table, int table_pages, const int32_t* kv_lens,
+                        const int32_t* cu_new, hipStream_t stream);
+
+/* The values of T slots (int64), rounded to `type`; 0 for slots outside the cache. */
+mq_status mq_kv8_read(const mq_kv8_cache* cache, int T, mq_dtype type, const int64_t* slots,
+                      void* K, int64_t k_token, int64_t k_head,
+                      void* V, int64_t v_token, int64_t v_head, hipStream_t stream);
+
+/*
+ * Attention over the 8-bit cache: arguments and result as mq_attention_kv4.
+ * Scores, maxima, sums and the running results are fp32; queries enter the products
+ * in fp16 (bf16 ones scaled by a power of two for each query and head, which
+ * keeps what is 2^-39 of the largest value and more), weights in fp16, up to 2^15
+ * and down to 2^-24 for the largest product of a weight and its block's scale.
+ * Weights below 2^-126 of the largest are 0.
+ * A query with a value that is not finite gives NaN, and changes no other's
+ * result.  A token whose key is NaN makes the queries that see it NaN, and no others.
+ * Sizes past the launch's indexes are refused, and have the workspace size 0: 2^24
+ * workgroups of 128 columns max_q group (of 16 or 32 up to 32 columns) or more for the
+ * sequences and key heads, or 2^24 sequences, key heads and columns where contexts are split.
+ */
+size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group,
+                                       int head_dim, int max_q, int64_t max_kv);
+mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens, int group,
+                           int max_q, int64_t max_kv, mq_dtype type,
+                           const void* Q, int64_t q_token, int64_t q_head,
+                           const int32_t* page_table, int table_pages, const int32_t* kv_lens,
+                           const int32_t* cu_q, float scale, int causal,
+                           void* O, int64_t o_token, int64_t o_head,
+                           void* workspace, size_t ws_bytes, hipStream_t stream);
+
 /* ======================================================================== */
 /* Offline weight preparation (not on the timed path)                        */
 /* ======================================================================== */

@@ -1,0 +1,464 @@
+// Attention over the paged 8-bit cache.
+//
+//   o = sum_t p_t v_t / sum_t p_t,   p_t = exp(scale q.k_t),
+//   k_t = 2^ek nk_t,  v_t = 2^ev nv_t   (n: e4m3 codes; ek, ev: of the token's block of 32 and head)
+//
+// Columns are the queries of one sequence and key head: position qi and head hg
+// of the group at column qi group + hg.  A wave takes blocks of 32 tokens for 16
+// NT columns: codes go from memory to registers in operand order, become fp16
+// there (exactly), and the matrix instruction's two products of a block are
+//   scores  S = K Q^T  (tokens x columns),   O += V^T W  (channels x columns),
+// the lanes' scores being, in place, the operand W of the second.  Scales act on
+// scores and weights, D times fewer than codes.
+//
+// With s = log2(e) scale q.k and, for each column, whole numbers m (running
+// maximum of s, by up to 2^kSlack too low) and J (the same of s - m + ev):
+//   p = 2^(s - m),  l = sum p,   w = p 2^(ev - J + kLift) in fp16,  O = sum w nv,
+//   o = 2^(J - kLift) O / l.
+// Only differences of s enter, so scores may be of any size, and a block of large
+// values that a column gives no weight takes nothing from the others.  Moving m or
+// J multiplies by powers of two.
+#include "kv8.h"
+
+#include <float.h>
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+namespace mq {
+
+mq_status check_cache8(const mq_kv8_cache* c);
+Cache8 device_cache8(const mq_kv8_cache* c);
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;          // weights up to 2^kSlack before a maximum moves
+constexpr float kLift = 7.0f;           // and as operands up to 2^(kSlack + kLift) < 65504, down to 2^-24
+constexpr float kLowest = -FLT_MAX;     // m of a column that has seen nothing
+constexpr float kNone = -1e30f;         // and its J: below any that a token gives
+
+struct Attn8Args {
+    Cache8 c;
+    const void* q;
+    void* o;
+    int64_t q_token, q_head, o_token, o_head;
+    const int32_t *table, *lens, *starts;
+    int table_pages, tokens, group, max_q, causal;
+    float scale;                        // times log2(e)
+    int64_t max_kv;
+    int chunk, chunks;                  // tokens that a workgroup takes, and chunks of the longest sequence
+    float* part;                        // of each sequence, key head, chunk and column: O[D], then m, J, l in `stats`
+    float* stats;
+};
+
+// One sequence's lengths, as the arguments bound them.
+struct Sequence8 {
+    int64_t len;                        // tokens
+    int first, queries;                 // rows of Q; queries that are computed
+    int64_t shift;                      // query i is at token i + shift
+    __device__ __forceinline__ Sequence8(const Attn8Args& a, int b) {
+        const int64_t n = a.lens[b];
+        len = n < 0 ? 0 : n < a.max_kv ? n : a.max_kv;
+        first = a.starts ? a.starts[b] : b;
+        const int count = a.starts ? a.starts[b + 1] - first : 1;
+        shift = n - count;
+        queries = min(count, a.max_q);
+    }
+    // tokens that query i sees: those before this
+    __device__ __forceinline__ int64_t seen(const Attn8Args& a, int i) const {
+        if (!a.causal) return len;
+        const int64_t n = shift + i + 1;
+        return n < 0 ? 0 : n < len ? n : len;
+    }
+};
+
+__device__ __forceinline__ f16x8 operand8(uint32_t a, uint32_t b) {
+    struct {
+        f16x2 v[4];
+    } r = {{__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
+            __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)}};
+    return __builtin_bit_cast(f16x8, r);
+}
+
+// s c - m, the product rounded before it meets m: m is one of these products, and where they pass 2^24 an exact product
+// would differ from it by more than any weight allows.
+__device__ __forceinline__ float score8(float s, float c, float m) {
+#pragma clang fp contract(off)
+    return s * c - m;
+}
+
+// The largest of v over the lanes l, l ^ 16, l ^ 32, l ^ 48 (a column's).
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+
+// WT waves of a workgroup share out the tokens of its columns (blocks in turn), 4 / WT take columns of their own.
+template <typename T, int D, int NT, int WT>
+__global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
+    constexpr int COLS = 16 * NT, WC = 4 / WT, STEPS = D / 32, PIECES = D / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wt = wave % WT, wc = wave / WT, col = lane & 15, quarter = lane >> 4;
+    const int b = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads;
+    const int group_block = gridDim.y - 1 - blockIdx.y;     // the longest first
+    const Sequence8 seq(a, b);
+    const int columns = seq.queries * a.group;
+    const int first_col = group_block * WC * COLS;          // of the workgroup
+    if (first_col >= columns) return;
+    const int64_t seen = seq.seen(a, (min(first_col + WC * COLS, columns) - 1) / a.group);
+    const int chunks = max(1, (int)((seen + a.chunk - 1) / a.chunk));
+    if ((int)blockIdx.z >= chunks) return;
+    const int64_t from = (int64_t)blockIdx.z * a.chunk;
+
+    // this wave's columns
+    const int col0 = first_col + wc * COLS;
+    f16x8 q[NT][STEPS];
+    float slope[NT];                                        // of the scores, in log2
+    int64_t sees[NT], least = seen, most = 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int c = col0 + 16 * n + col;
+        const bool there = c < columns;
+        const int qi = there ? c / a.group : 0, hg = there ? c % a.group : 0;
+        const int64_t row = (int64_t)seq.first + qi;
+        const bool has = there && row >= 0 && row < a.tokens;
+        sees[n] = has ? seq.seen(a, qi) : 0;
+        const T* p = static_cast<const T*>(a.q) + (has ? row * a.q_token + (int64_t)(head * a.group + hg) * a.q_head : 0) + 16 * quarter;
+        f32x8 x[STEPS];
+        uint32_t big = 0;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            x[s] = has ? load8(p + s / 2 * 64 + s % 2 * 8) : f32x8{};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
+        }
+        big = max(big, (uint32_t)__shfl_xor((int)big, 16));
+        big = max(big, (uint32_t)__shfl_xor((int)big, 32));
+        // bf16: by a power of two so that the largest is in [2^14, 2^15).  A query that is not finite is NaN throughout.
+        const int by = sizeof(T) == 2 && __is_same(T, __bf16) && big ? 141 - (int)(big >> 23) : 0;
+        const bool bad = big >= kFloatInf;
+        slope[n] = fminf(ldexpf(a.scale, -by), FLT_MAX);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[n][s][j] = bad ? (_Float16)__builtin_nanf("") : (_Float16)ldexpf(x[s][j], by);
+        least = has && sees[n] < least ? sees[n] : least;
+        most = sees[n] > most ? sees[n] : most;
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        least = min(least, (int64_t)__shfl_xor((long long)least, m));
+        most = max(most, (int64_t)__shfl_xor((long long)most, m));
+    }
+    const int64_t until = min(from + a.chunk, most);
+    const int first_block = (int)(from / kBlockTokens) + wt, end_block = (int)((until + kBlockTokens - 1) / kBlockTokens);
+    const int whole_end = (int)(least / kBlockTokens);      // blocks before this are seen by every column
+
+    f32x4 o[2 * PIECES][NT] = {};
+    float m[NT], jj[NT], l[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = kLowest;
+        jj[n] = kNone;
+        l[n] = 0.0f;
+    }
+    const int32_t* table = a.table + (int64_t)b * a.table_pages;
+    struct Block {
+        uint4 k[PIECES], v[PIECES];
+        int ke, ve;                                         // ve < 0: no page holds it
+    };
+    auto load = [&](Block& x, int block) {
+        const int64_t row = block_row8(a.c, table, a.table_pages, block, head);
+        const int64_t at = row < 0 ? 0 : row;
+        const uint8_t *k = a.c.k + at * D + lane * 16, *v = a.c.v + at * D + lane * 16;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x.k[i] = ldg16(k + i * 1024);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x.v[i] = ldg16(v + i * 1024);
+        x.ke = a.c.ke[at / kBlockTokens];
+        x.ve = row < 0 ? -1 : a.c.ve[at / kBlockTokens];
+    };
+    auto take = [&](const Block& x, int block) {
+        if (__builtin_amdgcn_readfirstlane(x.ve) < 0) return;
+        f32x4 s[NT][2] = {};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < PIECES / 2; ++i) {
+                const uint4 p = x.k[t * (PIECES / 2) + i];
+                const f16x8 k0 = operand8(p.x, p.y), k1 = operand8(p.z, p.w);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * i], s[n][t], 0, 0, 0);
+                    s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * i + 1], s[n][t], 0, 0, 0);
+                }
+            }
+        const float ev = (float)(x.ve - 127);
+        f16x8 w[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float c = fminf(ldexpf(slope[n], x.ke - 127), FLT_MAX);
+            if (block >= whole_end) {
+                const int64_t left = sees[n] - (int64_t)block * kBlockTokens - 4 * quarter;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * t + r >= left) s[n][t][r] = -INFINITY;
+            }
+            float y[8], high = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = score8(s[n][j / 4][j % 4], c, m[n]);
+                high = fmaxf(high, y[j]);
+            }
+            if (__ballot(high > fminf(kSlack, jj[n] + kSlack - ev))) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, s[n][j / 4][j % 4] * c);
+                top = column_max(top);
+                const float was = m[n];
+                m[n] = fmaxf(was, ceilf(top));
+                const float old = jj[n] + (was - m[n]);     // J of what O holds, by the new m
+                jj[n] = fmaxf(fmaxf(old, ceilf(top - m[n]) + ev), kNone);
+                l[n] *= __builtin_amdgcn_exp2f(was - m[n]);
+                const float by = __builtin_amdgcn_exp2f(old - jj[n]);
+#pragma unroll
+                for (int i = 0; i < 2 * PIECES; ++i) o[i][n] *= by;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = score8(s[n][j / 4][j % 4], c, m[n]);
+            }
+            const int e = (int)fminf(ev - jj[n] + kLift, 1000.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(y[j]);
+                l[n] += p;
+                w[n][j] = (_Float16)ldexpf(p, e);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const f16x8 v0 = operand8(x.v[i].x, x.v[i].y), v1 = operand8(x.v[i].z, x.v[i].w);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                o[2 * i][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[n], o[2 * i][n], 0, 0, 0);
+                o[2 * i + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n], o[2 * i + 1][n], 0, 0, 0);
+            }
+        }
+    };
+    Block x0, x1;
+    if (first_block < end_block) load(x0, first_block);
+    for (int block = first_block; block < end_block; block += 2 * WT) {
+        if (block + WT < end_block) load(x1, block + WT);
+        take(x0, block);
+        if (block + WT >= end_block) break;
+        if (block + 2 * WT < end_block) load(x0, block + 2 * WT);
+        take(x1, block + WT);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        l[n] += __shfl_xor(l[n], 16);
+        l[n] += __shfl_xor(l[n], 32);
+    }
+
+    // four channels 16 i + 4 quarter .. of a column's result, as sums or as values
+    const bool direct = chunks == 1;
+    auto store = [&](int c, int ch, f32x4 sum, float mm, float j, float ll) {
+        if (direct) {
+            const int64_t row = (int64_t)seq.first + c / a.group;
+            if (row < 0 || row >= a.tokens) return;
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            f32x4 y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = ll == 0.0f ? 0.0f : ldexpf(sum[r] / ll, (int)fmaxf(j - kLift, -1000.0f));
+            *reinterpret_cast<t4*>(static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head + ch) =
+                __builtin_convertvector(y, t4);
+        } else {
+            const int64_t at = ((int64_t)blockIdx.x * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
+            *reinterpret_cast<f32x4*>(a.part + at * D + ch) = sum;
+            if (ch == 0) {
+                a.stats[3 * at] = mm;
+                a.stats[3 * at + 1] = j;
+                a.stats[3 * at + 2] = ll;
+            }
+        }
+    };
+    if constexpr (WT == 1) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int c = col0 + 16 * n + col;
+            if (c < columns)
+#pragma unroll
+                for (int i = 0; i < 2 * PIECES; ++i) store(c, 16 * i + 4 * quarter, o[i][n], m[n], jj[n], l[n]);
+        }
+    } else {
+        __shared__ float sums[4][COLS][D + 4], stat[4][COLS][3];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2 * PIECES; ++i)
+                *reinterpret_cast<f32x4*>(&sums[wave][16 * n + col][16 * i + 4 * quarter]) = o[i][n];
+            if (quarter == 0) {
+                stat[wave][16 * n + col][0] = m[n];
+                stat[wave][16 * n + col][1] = jj[n];
+                stat[wave][16 * n + col][2] = l[n];
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < WC * COLS * (D / 4); e += 256) {
+            const int c = e / (D / 4), ch = e % (D / 4) * 4, w0 = c / COLS * WT, cc = c % COLS;
+            if (first_col + c >= columns) continue;
+            float mm = kLowest, j = kNone, ll = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WT; ++w) mm = fmaxf(mm, stat[w0 + w][cc][0]);
+#pragma unroll
+            for (int w = 0; w < WT; ++w) j = fmaxf(j, stat[w0 + w][cc][1] + (stat[w0 + w][cc][0] - mm));
+            f32x4 sum = {};
+#pragma unroll
+            for (int w = 0; w < WT; ++w) {
+                const float by = stat[w0 + w][cc][0] - mm;
+                ll += stat[w0 + w][cc][2] * __builtin_amdgcn_exp2f(by);
+                sum += *reinterpret_cast<const f32x4*>(&sums[w0 + w][cc][ch]) * __builtin_amdgcn_exp2f(stat[w0 + w][cc][1] + by - j);
+            }
+            store(first_col + c, ch, sum, mm, j, ll);
+        }
+    }
+}
+
+// The chunks of one column to its result: one workgroup, D / 4 threads for four channels each, the rest share the chunks.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention8_join_kernel(Attn8Args a, int block_cols) {
+    constexpr int LANES = D / 4, PARTS = 256 / LANES;
+    __shared__ float sums[PARTS][D + 4], heads[PARTS][2], ls[PARTS];
+    const int most = a.max_q * a.group, unit = blockIdx.x / most, c = blockIdx.x % most;
+    const int b = unit / a.c.heads, head = unit % a.c.heads;
+    const Sequence8 seq(a, b);
+    const int columns = seq.queries * a.group;
+    if (c >= columns) return;
+    const int64_t seen = seq.seen(a, (min(c / block_cols * block_cols + block_cols, columns) - 1) / a.group);
+    const int chunks = max(1, (int)((seen + a.chunk - 1) / a.chunk));
+    const int64_t row = (int64_t)seq.first + c / a.group;
+    if (chunks == 1 || row < 0 || row >= a.tokens) return;
+    const int64_t stride = most, first = (int64_t)unit * a.chunks * stride + c;
+    const int part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
+    float m = kLowest, j = kNone;
+    for (int i = 0; i < chunks; ++i) m = fmaxf(m, a.stats[3 * (first + i * stride)]);
+    for (int i = 0; i < chunks; ++i) {
+        const float* s = a.stats + 3 * (first + i * stride);
+        j = fmaxf(j, s[1] + (s[0] - m));
+    }
+    f32x4 sum = {};
+    float l = 0.0f;
+    for (int i = part; i < chunks; i += PARTS) {
+        const int64_t at = first + i * stride;
+        const float by = a.stats[3 * at] - m;
+        l += a.stats[3 * at + 2] * __builtin_amdgcn_exp2f(by);
+        sum += *reinterpret_cast<const f32x4*>(a.part + at * D + ch) * __builtin_amdgcn_exp2f(a.stats[3 * at + 1] + by - j);
+    }
+    *reinterpret_cast<f32x4*>(&sums[part][ch]) = sum;
+    if (ch == 0) ls[part] = l;
+    __syncthreads();
+    if (part != 0) return;
+    sum = f32x4{};
+    l = 0.0f;
+    for (int p = 0; p < PARTS; ++p) {
+        sum += *reinterpret_cast<const f32x4*>(&sums[p][ch]);
+        l += ls[p];
+    }
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    f32x4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = l == 0.0f ? 0.0f : ldexpf(sum[r] / l, (int)fmaxf(j - kLift, -1000.0f));
+    *reinterpret_cast<t4*>(static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head + ch) =
+        __builtin_convertvector(y, t4);
+}
+
+// ---------------------------------------------------------------- host side --
+struct Plan8a {
+    int nt, wt;                         // 16 nt columns a wave, wt waves share out the tokens
+    int blocks;                         // of columns
+    int chunk, chunks;                  // tokens of a workgroup, and the most of them of a sequence
+};
+static bool plan_attention8(int sequences, int heads, int group, int head_dim, int max_q, int64_t max_kv, Plan8a& p) {
+    if (sequences < 0 || heads < 1 || heads > 65535 || group < 1 || group > 1024 || max_q < 0 || max_kv < 0 || max_kv > INT32_MAX - 65536 ||
+        (head_dim != 64 && head_dim != 128))
+        return false;
+    const int64_t columns = (int64_t)max_q * group;
+    if (columns > INT32_MAX / 2) return false;
+    p.nt = columns <= 16 ? 1 : 2;
+    p.wt = columns <= 32 ? 4 : 1;
+    const int cols = 16 * p.nt * (4 / p.wt);
+    const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols), units = (int64_t)sequences * heads * blocks;
+    // chunks: about eight workgroups for each CU, of 128 tokens at least for each wave
+    const int64_t least = 128 * p.wt, want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, units));
+    int64_t chunk = std::max<int64_t>(least, ((max_kv + want - 1) / want + 31) / 32 * 32);
+    p.chunk = (int)chunk;
+    const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
+    if (blocks > 65535 || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256) ||
+        (chunks > 1 && !mq_host::launch_holds((int64_t)sequences * heads * columns, 256)))
+        return false;
+    p.blocks = (int)blocks;
+    p.chunks = (int)chunks;
+    return true;
+}
+
+}  // namespace mq
+
+using namespace mq;
+
+static size_t workspace_of(const Plan8a& p, int sequences, int heads, int group, int head_dim, int max_q) {
+    return p.chunks == 1 ? 0 : (size_t)sequences * heads * p.chunks * ((size_t)max_q * group) * (head_dim + 3) * sizeof(float) + 16;
+}
+
+extern "C" size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group, int head_dim, int max_q,
+                                                  int64_t max_kv) {
+    Plan8a p;
+    if (tokens < 0 || !plan_attention8(sequences, heads, group, head_dim, max_q, max_kv, p)) return 0;
+    return workspace_of(p, sequences, heads, group, head_dim, max_q);
+}
+
+extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens, int group, int max_q, int64_t max_kv,
+                                      mq_dtype type, const void* Q, int64_t q_token, int64_t q_head, const int32_t* page_table,
+                                      int table_pages, const int32_t* kv_lens, const int32_t* cu_q, float scale, int causal, void* O,
+                                      int64_t o_token, int64_t o_head, void* workspace, size_t ws_bytes, hipStream_t stream) {
+    if (sequences < 0 || tokens < 0 || group < 1 || max_q < 0 || max_kv < 0 || table_pages < 0 || !mq_host::is_half_type(type) ||
+        !(scale > 0.0f) || !(scale <= FLT_MAX) || (!cu_q && tokens != sequences))
+        return MQ_ERR_INVALID_ARG;
+    if (mq_status st = check_cache8(cache); st != MQ_OK) return st;
+    for (int64_t s : {q_token, q_head, o_token, o_head})
+        if (s < 0 || s % 8 != 0) return MQ_ERR_UNSUPPORTED_SHAPE;
+    Plan8a p;
+    if (max_kv > (int64_t)table_pages * cache->page_size ||
+        !plan_attention8(sequences, cache->heads, group, cache->head_dim, cu_q ? max_q : std::min(max_q, 1), max_kv, p))
+        return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (tokens == 0 || sequences == 0 || max_q == 0) return MQ_OK;
+    if (!Q || !O || !kv_lens || (!page_table && max_kv > 0)) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(Q, 16) || !mq_host::aligned(O, 16) || !mq_host::aligned(page_table, 4) || !mq_host::aligned(kv_lens, 4) ||
+        !mq_host::aligned(cu_q, 4) || !mq_host::aligned(workspace, 16))
+        return MQ_ERR_MISALIGNED;
+    if (!cu_q) max_q = 1;
+    const size_t need = workspace_of(p, sequences, cache->heads, group, cache->head_dim, max_q);
+    if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
+    Attn8Args a{device_cache8(cache), Q, O, q_token, q_head, o_token, o_head, page_table, kv_lens, cu_q, table_pages, tokens, group, max_q,
+                causal != 0, scale * kLog2e, max_kv, p.chunk, p.chunks, static_cast<float*>(workspace), nullptr};
+    a.stats = a.part + (size_t)sequences * cache->heads * p.chunks * ((size_t)max_q * group) * cache->head_dim;
+    const dim3 grid(sequences * cache->heads, p.blocks, p.chunks);
+    return mq_host::with_half_type(type, [&](auto z) {
+        using T = decltype(z);
+        auto run = [&](auto d) {
+            constexpr int D = decltype(d)::value;
+            if (p.wt == 4 && p.nt == 1) hipLaunchKernelGGL((attention8_kernel<T, D, 1, 4>), grid, dim3(256), 0, stream, a);
+            else if (p.wt == 4) hipLaunchKernelGGL((attention8_kernel<T, D, 2, 4>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((attention8_kernel<T, D, 2, 1>), grid, dim3(256), 0, stream, a);
+            if (p.chunks > 1)
+                hipLaunchKernelGGL((attention8_join_kernel<T, D>), dim3((unsigned)(sequences * cache->heads) * (unsigned)(max_q * group)),
+                                   dim3(256), 0, stream, a, 16 * p.nt * (4 / p.wt));
+        };
+        if (cache->head_dim == 64) run(std::integral_constant<int, 64>{});
+        else run(std::integral_constant<int, 128>{});
+        return mq_host::launch_status();
+    });
+}

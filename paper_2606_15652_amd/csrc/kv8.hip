@@ -1,0 +1,264 @@
+// Keys and values of new tokens into the paged 8-bit cache, and back.
+//
+// A block of 32 tokens of a sequence and head has one scale 2^e for its keys and
+// one for its values, e the least with |x| <= 448 2^e; codes are e4m3(x 2^-e).
+// Later tokens of the block may raise e: the codes that are there are then
+// divided by the power of two, exactly but where they pass below 2^-6.
+//
+// One wave takes one block and head: what the block holds comes to LDS, new codes
+// go there, and it goes back in whole lines.  Nobody else writes the block, so
+// nothing depends on order.
+#include "kv8.h"
+
+#include <type_traits>
+
+namespace mq {
+
+struct Append8Args {
+    Cache8 c;
+    const void *k, *v;
+    int64_t k_token, k_head, v_token, v_head;   // strides, in elements
+    const int32_t *table, *lens, *starts;       // starts may be null: one token a sequence
+    int sequences, tokens, table_pages;
+};
+
+// Blocks that the tokens of sequences before b can reach, and two for each: a bound that ascends and needs no pass over
+// the sequences (n tokens reach at most n / 32 + 2 blocks).
+__device__ __forceinline__ int64_t first_unit(const int32_t* starts, int b) { return starts[b] / kBlockTokens + 2 * (int64_t)b; }
+
+// The last sequence with first_unit <= unit (the wave looks at 64 of them at a time), -1 for none.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int sequences, int64_t unit) {
+    const int lane = threadIdx.x & 63;
+    int first = 0, n = sequences;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = lane * step;
+        const int count = __popcll(__ballot(i < n && first_unit(starts, first + i) <= unit));
+        if (count == 0) return -1;
+        first += (count - 1) * step;
+        n = min(step, n - (count - 1) * step);
+    }
+    return first;
+}
+
+// Least e with amax <= 448 2^e = 1.75 2^(e + 8), for the exponent's byte: e + 127 in 0 .. 254.
+__device__ __forceinline__ int exponent_byte(uint32_t amax_bits) {
+    const int x = (int)(amax_bits >> 23) + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return max(x - 8, 0);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, TURNS = kBlockTokens / ROWS, BYTES = kBlockTokens * D;
+    __shared__ __attribute__((aligned(16))) uint8_t image[4][2][BYTES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+    const int head = (int)(unit % a.c.heads), ch = 8 * (lane % LANES), sub = lane / LANES;
+    const int64_t which = unit / a.c.heads;
+    const int b = a.starts ? sequence_of(a.starts, a.sequences, which) : (int)min(which, (int64_t)a.sequences);
+    if (b < 0 || b >= a.sequences) return;                  // (waves do not meet)
+    const int first_new = a.starts ? a.starts[b] : b, count = a.starts ? a.starts[b + 1] - first_new : 1;
+    const int64_t len = a.lens[b], had = len - count;       // had < 0: the first -had tokens have no place
+    const int64_t block = (had > 0 ? had : 0) / kBlockTokens + (a.starts ? which - first_unit(a.starts, b) : 0);
+    const int64_t at = block * kBlockTokens;
+    if (count <= 0 || at >= len) return;
+    const int64_t row = block_row8(a.c, a.table + (int64_t)b * a.table_pages, a.table_pages, block, head);
+    if (row < 0) return;
+    const int64_t base = row * D, blk = row / kBlockTokens;
+
+    // the block's new tokens, and which of them are finite in key and value
+    f32x8 x[2][TURNS];
+    uint32_t fresh = 0, fine = 0;                           // bit i: this lane's token of turn i
+    uint32_t amax[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int64_t t = at + i * ROWS + sub, from = first_new + t - had;
+        const bool there = t >= had && t < len && from >= 0 && from < a.tokens;
+        x[0][i] = x[1][i] = f32x8{};
+        if (there) {
+            x[0][i] = load8(static_cast<const T*>(a.k) + from * a.k_token + head * a.k_head + ch);
+            x[1][i] = load8(static_cast<const T*>(a.v) + from * a.v_token + head * a.v_head + ch);
+        }
+        uint32_t most[2] = {0, 0};
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most[w] = max(most[w], __float_as_uint(x[w][i][j]) & 0x7FFFFFFFu);
+        const uint64_t bad = __ballot(max(most[0], most[1]) >= kFloatInf);
+        const bool finite = ((bad >> (lane & ~(LANES - 1))) & ((1u << LANES) - 1)) == 0;
+        fresh |= (uint32_t)there << i;
+        fine |= (uint32_t)finite << i;
+        if (finite) {
+            amax[0] = max(amax[0], most[0]);
+            amax[1] = max(amax[1], most[1]);
+        }
+    }
+    const bool whole = __ballot(fresh != (1u << TURNS) - 1) == 0;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        uint8_t *codes = (w ? a.c.v : a.c.k) + base, *held = (w ? a.c.ve : a.c.ke) + blk;
+        uint8_t* im = image[wave][w];
+        int e = exponent_byte(wave_max_dpp(amax[w]));
+        if (!whole) {
+            const int e_old = *held;
+            const bool moves = at < had && e > e_old;       // only tokens from before hold a block's scale up
+            if (at < had) e = max(e, e_old);
+#pragma unroll
+            for (int i = 0; i < BYTES / 1024; ++i) {
+                uint4 p = ldg16(codes + i * 1024 + lane * 16);
+                if (moves) {
+                    auto moved = [&](uint32_t d) {
+                        const f32x2 lo = from_e4m3<false>(d), hi = from_e4m3<true>(d);
+                        const int by = e_old - e;
+                        const uint32_t to = to_e4m3x4(ldexpf(lo[0], by), ldexpf(lo[1], by), ldexpf(hi[0], by), ldexpf(hi[1], by));
+                        // a NaN stays the one it was (the conversion may change its sign)
+                        const uint32_t nan = ((d & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) / 0x80u * 0xFFu;
+                        return (to & ~nan) | (d & nan);
+                    };
+                    p = make_uint4(moved(p.x), moved(p.y), moved(p.z), moved(p.w));
+                }
+                *reinterpret_cast<uint4*>(im + i * 1024 + lane * 16) = p;
+            }
+            wave_sync();
+        }
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            if (!(fresh >> i & 1)) continue;
+            const int t = i * ROWS + sub;
+            uint32_t q[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[j] = ldexpf(x[w][i][4 * h + j], 127 - e);
+                // a token that is not finite: NaN throughout its key, and a value of zeros
+                q[h] = fine >> i & 1 ? to_e4m3x4(f[0], f[1], f[2], f[3]) : w ? 0u : 0x7F7F7F7Fu;
+            }
+            if (w == 0) {
+                *reinterpret_cast<uint2*>(im + key_offset8<D>(t, ch)) = make_uint2(q[0], q[1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) im[value_offset8(t, ch + j)] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+            }
+        }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < BYTES / 1024; ++i)
+            *reinterpret_cast<uint4*>(codes + i * 1024 + lane * 16) = *reinterpret_cast<const uint4*>(im + i * 1024 + lane * 16);
+        if (lane == 0) *held = (uint8_t)e;
+    }
+}
+
+struct Read8Args {
+    Cache8 c;
+    void *k, *v;
+    int64_t k_token, k_head, v_token, v_head;
+    const int64_t* slots;
+    int tokens;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_read_kernel(Read8Args a) {
+    constexpr int LANES = D / 8, ROWS = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int head = (int)(unit % a.c.heads), ch = 8 * (lane % LANES);
+    const int64_t token = unit / a.c.heads * ROWS + lane / LANES;
+    if (token >= a.tokens) return;
+    const int64_t slot = a.slots[token];
+    f32x8 kx{}, vx{};
+    if (slot >= 0 && slot < (int64_t)a.c.pages << a.c.page_bits) {
+        const int64_t page = slot >> a.c.page_bits, in = slot & ((1 << a.c.page_bits) - 1);
+        const int64_t row = ((page * a.c.heads + head) << a.c.page_bits) + in / kBlockTokens * kBlockTokens;
+        const int t = (int)(in % kBlockTokens), ke = a.c.ke[row / kBlockTokens] - 127, ve = a.c.ve[row / kBlockTokens] - 127;
+        const uint2 kw = *reinterpret_cast<const uint2*>(a.c.k + row * D + key_offset8<D>(t, ch));
+        uint32_t vw[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vw[j / 4] |= (uint32_t)a.c.v[row * D + value_offset8(t, ch + j)] << (8 * (j % 4));
+        auto values = [](uint32_t a, uint32_t b, int e) {
+            const f32x2 p[4] = {from_e4m3<false>(a), from_e4m3<true>(a), from_e4m3<false>(b), from_e4m3<true>(b)};
+            f32x8 y;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = ldexpf(p[j / 2][j % 2], e);
+            return y;
+        };
+        kx = values(kw.x, kw.y, ke);
+        vx = values(vw[0], vw[1], ve);
+    }
+    store8(static_cast<T*>(a.k) + token * a.k_token + head * a.k_head + ch, kx);
+    store8(static_cast<T*>(a.v) + token * a.v_token + head * a.v_head + ch, vx);
+}
+
+// What a cache has to be, for every call that takes one.
+mq_status check_cache8(const mq_kv8_cache* c) {
+    if (!c || c->pages < 0 || c->heads < 0 || c->page_size < 0 || c->head_dim < 0) return MQ_ERR_INVALID_ARG;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->page_size < kBlockTokens || c->page_size > 65536 ||
+        (c->page_size & (c->page_size - 1)) != 0 || c->heads < 1 || c->heads > 65535 || c->pages < 1)
+        return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (!c->k || !c->v || !c->k_scales || !c->v_scales) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(c->k, 16) || !mq_host::aligned(c->v, 16)) return MQ_ERR_MISALIGNED;
+    return MQ_OK;
+}
+Cache8 device_cache8(const mq_kv8_cache* c) {
+    return Cache8{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), static_cast<uint8_t*>(c->k_scales),
+                  static_cast<uint8_t*>(c->v_scales), c->pages, c->heads, __builtin_ctz((unsigned)c->page_size)};
+}
+
+static bool strides_ok(int64_t kt, int64_t kh, int64_t vt, int64_t vh) {
+    for (int64_t s : {kt, kh, vt, vh})
+        if (s < 0 || s % 8 != 0) return false;
+    return true;
+}
+
+}  // namespace mq
+
+using namespace mq;
+
+extern "C" size_t mq_kv8_code_bytes(int pages, int page_size, int heads, int head_dim) {
+    if (pages < 1 || page_size < 1 || heads < 1 || head_dim < 1) return 0;
+    return (size_t)pages * page_size * heads * head_dim;
+}
+
+extern "C" mq_status mq_kv8_append(const mq_kv8_cache* cache, int sequences, int T, mq_dtype type, const void* K,
+                                   int64_t k_token, int64_t k_head, const void* V, int64_t v_token, int64_t v_head,
+                                   const int32_t* page_table, int table_pages, const int32_t* kv_lens, const int32_t* cu_new,
+                                   hipStream_t stream) {
+    if (T < 0 || sequences < 0 || table_pages < 0 || !mq_host::is_half_type(type) || (!cu_new && T != sequences))
+        return MQ_ERR_INVALID_ARG;
+    if (mq_status st = check_cache8(cache); st != MQ_OK) return st;
+    if (!strides_ok(k_token, k_head, v_token, v_head)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    const int64_t units = cu_new ? (int64_t)T / kBlockTokens + 2 * (int64_t)sequences : sequences;
+    const int64_t groups = (units * cache->heads + 3) / 4;
+    if (!mq_host::launch_holds(groups, 256)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0 || sequences == 0) return MQ_OK;
+    if (!K || !V || !page_table || !kv_lens) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(K, 16) || !mq_host::aligned(V, 16) || !mq_host::aligned(page_table, 4) ||
+        !mq_host::aligned(kv_lens, 4) || !mq_host::aligned(cu_new, 4))
+        return MQ_ERR_MISALIGNED;
+    const Append8Args a{device_cache8(cache), K, V, k_token, k_head, v_token, v_head, page_table, kv_lens, cu_new,
+                        sequences, T, table_pages};
+    return mq_host::with_half_type(type, [&](auto z) {
+        using E = decltype(z);
+        if (cache->head_dim == 64) hipLaunchKernelGGL((kv8_append_kernel<E, 64>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((kv8_append_kernel<E, 128>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+        return mq_host::launch_status();
+    });
+}
+
+extern "C" mq_status mq_kv8_read(const mq_kv8_cache* cache, int T, mq_dtype type, const int64_t* slots, void* K,
+                                 int64_t k_token, int64_t k_head, void* V, int64_t v_token, int64_t v_head, hipStream_t stream) {
+    if (T < 0 || !mq_host::is_half_type(type)) return MQ_ERR_INVALID_ARG;
+    if (mq_status st = check_cache8(cache); st != MQ_OK) return st;
+    const int rows = 512 / cache->head_dim;
+    const int64_t groups = (((int64_t)T + rows - 1) / rows * cache->heads + 3) / 4;
+    if (!strides_ok(k_token, k_head, v_token, v_head) || !mq_host::launch_holds(groups, 256)) return MQ_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MQ_OK;
+    if (!K || !V || !slots) return MQ_ERR_INVALID_ARG;
+    if (!mq_host::aligned(K, 16) || !mq_host::aligned(V, 16) || !mq_host::aligned(slots, 8)) return MQ_ERR_MISALIGNED;
+    const Read8Args a{device_cache8(cache), K, V, k_token, k_head, v_token, v_head, slots, T};
+    return mq_host::with_half_type(type, [&](auto z) {
+        using E = decltype(z);
+        if (cache->head_dim == 64) hipLaunchKernelGGL((kv8_read_kernel<E, 64>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((kv8_read_kernel<E, 128>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+        return mq_host::launch_status();
+    });
+}
