@@ -636,6 +636,41 @@ mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens,
                            void* O, int64_t o_token, int64_t o_head,
                            void* workspace, size_t ws_bytes, hipStream_t stream);
 
+#define MQ_SAMPLE_MAX_VOCAB 1048576
+
+/*
+ * A token drawn from the logits x of each row.  In the order of descending logits, the
+ * lower index first among equals, with w_i = exp((x_i - max x) / temperature):
+ *   1. top_k (if positive): the first top_k tokens;
+ *   2. top_p (below 1): of these the shortest beginning whose sum of w is top_p times
+ *      theirs, one token at least;
+ *   3. min_p (above 0): of these the tokens with w >= min_p (which min_p above 1 is taken as 1);
+ * the token is the first at which the running sum of w passes u times the sum of all
+ * that is left; its probability is w over that sum.  Weights are held as whole
+ * multiples of 2^-43, sums and comparisons of them are exact: a token whose weight is below 2^-44
+ * is never drawn, and the result does not depend on the order in which anything runs.
+ * temperature 0 (and any in the array that is not positive) gives the first token
+ * with the largest logit, and the probability 1.
+ * Tokens at -infinity have no weight; where one is at +infinity, only those have.  A row of
+ * -infinity only gives the token -1 and the probability 0, one with a NaN -1 and NaN.
+ *   logits : `type` (MQ_FP16, MQ_BF16, MQ_FP32) [rows, ldx], ldx >= vocab, aligned to it;
+ *            vocab 1 .. MQ_SAMPLE_MAX_VOCAB.
+ *   u      : fp32 [rows], in [0, 1) (below: 0; 1 and above, and NaN: the last token kept).
+ *   temperature, top_p, min_p (fp32 [rows]) and top_k (int32 [rows]): each may be NULL; then
+ *            the value beside it is every row's, temperature_all, top_p_all, min_p_all
+ *            >= 0.  In arrays, NaN and what is out of range filter nothing (top_p
+ *            below 0 is 0).
+ *   tokens, probs : out, int64 [rows], fp32 [rows].
+ *   workspace : >= mq_sample_workspace_size(rows, vocab) bytes, 16-byte aligned (may
+ *               be NULL when that is 0).
+ */
+size_t mq_sample_workspace_size(int rows, int vocab);
+mq_status mq_sample(int rows, int vocab, mq_dtype type, const void* logits, int64_t ldx,
+                    const float* u, const float* temperature, float temperature_all,
+                    const int32_t* top_k, int top_k_all, const float* top_p, float top_p_all,
+                    const float* min_p, float min_p_all, int64_t* tokens, float* probs,
+                    void* workspace, size_t ws_bytes, hipStream_t stream);
+
 /* ======================================================================== */
 /* Offline weight preparation (not on the timed path)                        */
 /* ======================================================================== */

@@ -83,6 +83,8 @@ _SIG = {
     "mq_attention_kv8_workspace_size": (C.c_size_t, [_I, _I, _I, _I, _I, _I, _L]),
     "mq_attention_kv8": (_I, [_P, _I, _I, _I, _I, _L, _I, _P, _L, _L, _P, _I, _P, _P, _F, _I, _P, _L, _L, _P,
                               C.c_size_t, _P]),
+    "mq_sample_workspace_size": (C.c_size_t, [_I, _I]),
+    "mq_sample": (_I, [_I, _I, _I, _P, _L, _P, _P, _F, _P, _I, _P, _F, _P, _F, _P, _P, _P, C.c_size_t, _P]),
 }
 
 _lib: Optional[C.CDLL] = None
@@ -560,4 +562,4 @@ from .serving import (  # noqa: E402  (needs the names above)
     gemm_w8a8_tile, gemm_w8a8_workspace_bytes, kv4_append, kv4_cache, kv4_read, quantize_rows8, quantize_weight8, repack_weight8,
     rms_norm_quantize8, unpack_weight8)
 from .fp8 import (  # noqa: E402
-    KVCache8, attention_kv8, attention_kv8_workspace_bytes, kv8_append, kv8_cache, kv8_read)
+    KVCache8, attention_kv8, attention_kv8_workspace_bytes, kv8_append, kv8_cache, kv8_read, sample)

@@ -1,4 +1,5 @@
-"""Binding of the operators in 8-bit floating point (OCP e4m3): the paged 8-bit cache and the attention over it.
+"""Binding of the operators in 8-bit floating point (OCP e4m3), the paged 8-bit cache and the attention over it, and of
+sampling.
 
 As in the package's other calls only arguments are checked and marshalled here; ``include/mq.h`` documents each
 operator.  Values are fp16 or bf16.  A call runs on the device of its tensors, which need not be the current one,
@@ -180,3 +181,54 @@ def attention_kv8(Q, cache: KVCache8, page_table, kv_lens, cu_q=None, max_q=None
             _ptr(cu_q), 1.0 / math.sqrt(D) if scale is None else scale, causal, O.data_ptr(), ot, oh, _ptr(wbuf), ws,
             _stream(stream)))
     return O
+
+
+# ----------------------------------------------------------- sampling --
+def _of_rows(value, rows, dtype, name, none, device):
+    """A parameter for each row (a tensor) or for all: (tensor or None, number)."""
+    if value is None:
+        return None, none
+    if isinstance(value, _torch().Tensor):
+        _need_out(value, (rows,), dtype, name)
+        if value.get_device() != device:
+            raise ValueError(f"{name} is on {value.device}, logits on cuda:{device}")
+        return value, none
+    return None, value
+
+
+def sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=None, workspace=None, stream=None):
+    """(tokens int64 [rows], probabilities fp32 [rows]): a token drawn from each row of logits [rows, vocab] (fp16, bf16 or
+    fp32, contiguous rows) by the uniform numbers ``u`` (fp32 [rows], in [0, 1)).  ``temperature``, ``top_k``, ``top_p`` and
+    ``min_p`` filter in this order (include/mq.h); each is a number for all rows or a tensor [rows] (fp32, top_k
+    int32), None for none.  Temperature 0 takes the largest logit."""
+    torch = _torch()
+    code = _dtype_code(getattr(logits, "dtype", None), "logits", fp32=True)
+    if not logits.is_cuda or logits.dim() != 2:
+        raise ValueError("logits must be a CUDA (HIP) tensor [rows, vocab]")
+    rows, vocab = logits.shape
+    ldx, col = logits.stride()
+    if col != 1 and vocab > 1:
+        raise ValueError("logits must have contiguous rows")
+    device = logits.get_device()
+    _need_out(u, (rows,), torch.float32, "u")
+    t, t1 = _of_rows(temperature, rows, torch.float32, "temperature", 1.0, device)
+    k, k1 = _of_rows(top_k, rows, torch.int32, "top_k", 0, device)
+    p, p1 = _of_rows(top_p, rows, torch.float32, "top_p", 1.0, device)
+    m, m1 = _of_rows(min_p, rows, torch.float32, "min_p", 0.0, device)
+    if not -(1 << 31) <= k1 < 1 << 31:
+        raise ValueError(f"top_k {k1} is out of range")
+    if out is None:
+        tokens, probs = _empty((rows,), torch.int64, logits.device, stream), _empty((rows,), torch.float32, logits.device, stream)
+    else:
+        tokens, probs = out
+        _need_out(tokens, (rows,), torch.int64, "out[0] (tokens)")
+        _need_out(probs, (rows,), torch.float32, "out[1] (probs)")
+    _same_device(logits, "logits", u=u, tokens=tokens, probs=probs, workspace=workspace)
+    lib = load()
+    ws = lib.mq_sample_workspace_size(rows, vocab)
+    with _on(logits, stream):
+        wbuf = _scratch(ws, logits.device, stream, workspace)
+        _check("mq_sample", lib.mq_sample(rows, vocab, code, logits.data_ptr(), ldx if rows > 1 else vocab, u.data_ptr(), _ptr(t), t1,
+                                          _ptr(k), k1, _ptr(p), p1, _ptr(m), m1, tokens.data_ptr(), probs.data_ptr(), _ptr(wbuf), ws,
+                                          _stream(stream)))
+    return tokens, probs
