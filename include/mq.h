@@ -564,6 +564,58 @@ mq_status mq_attention_kv4(const mq_kv4_cache* cache, int sequences, int tokens,
                            void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Activations in 8-bit floating point (OCP e4m3: largest 448), a scale for each token
+ * and group of 128 channels:
+ *     s_x[m,g] = max_{k in g} |X| / 448  (fp32),   q = e4m3(X / s_x)  (0 if s_x == 0):
+ * the quotient is rounded to fp32, kept in [-448, 448], and from there to e4m3, ties to
+ * even.  A group that is not finite has the scale NaN and codes 0.
+ *   X        : `type` MQ_FP16 or MQ_BF16, [M, ldx], ldx >= K, ldx % 8 == 0, 16-byte
+ *              aligned; K a multiple of 8, at most MQ_W8A8_MAX_K.
+ *   Xq       : out, bytes [M, ldq], ldq >= K rounded up to 16, ldq % 16 == 0, 16-byte
+ *              aligned; codes between K and that are 0.
+ *   s_x      : out, fp32 [ceil(K / 128)][lds], lds >= M: s_x[m,g] at g lds + m.
+ */
+mq_status mq_quantize_rows_fp8(int M, int K, mq_dtype type, const void* X, int ldx,
+                               void* Xq, int ldq, float* s_x, int lds, hipStream_t stream);
+
+/*
+ * e4m3 weights, one fp32 scale for each block of 128 output channels and 128 codes:
+ * s_w fp32 [ceil(N / 128)][ceil(K / 128)].  Library layout of the codes: that of the INT8
+ * weights (mq_weight8_bytes).  Any N in [1, 2^24] and K in [1, MQ_W8A8_MAX_K].
+ */
+size_t mq_weight_fp8_bytes(int N, int K);
+/* s_w = max |W| / 448 over the block, q = e4m3(W / s_w) as above, from fp32 W [N, ldw],
+ * ldw >= K.  Wq: out, mq_weight_fp8_bytes(N, K) bytes, 16-byte aligned. */
+mq_status mq_quantize_weight_fp8(const float* W, int N, int K, int ldw, uint8_t* Wq, float* s_w,
+                                 hipStream_t stream);
+/* Canonical e4m3 rows Wc [N, ldw] (ldw >= K, any alignment) <-> that layout. */
+mq_status mq_repack_weight_fp8(int N, int K, const uint8_t* Wc, int ldw, uint8_t* Wq,
+                               hipStream_t stream);
+mq_status mq_unpack_weight_fp8(int N, int K, const uint8_t* Wq, uint8_t* Wc, int ldw,
+                               hipStream_t stream);
+
+/*
+ * Product of both:
+ *     Y[m,n] = rn( sum_g s_x[m,g] s_w[n/128,g] sum_{k in g} Xq[m,k] Wq[n,k] + bias[n] )
+ * in fp32: the sum of a group, the product of its scales, the sum of the groups (in an
+ * order that the sizes alone choose) and the bias; rounded once to `type`.
+ *   Xq, s_x   : as mq_quantize_rows_fp8 writes them, any K; ldx, lds as there.  A row's
+ *               bytes between K and the next multiple of 16 are read: they must not be NaN
+ *               codes.  Beyond 32 rows, (31 ldx + K) below 2^31 (fewer: (M - 1) ldx + K).
+ *   Wq, s_w   : library layout, fp32 [ceil(N / 128)][ceil(K / 128)].
+ *   type      : of bias (may be NULL) and Y: MQ_FP16, MQ_BF16 or MQ_FP32.
+ *   Y         : out, [M, ldy], ldy >= N, aligned to its type.
+ *   workspace : >= mq_gemm_fp8_workspace_size(M, N, K) bytes, 16-byte aligned
+ *               (may be NULL when that is 0).
+ */
+size_t mq_gemm_fp8_workspace_size(int M, int N, int K);
+/* Output tile of one workgroup of that launch, and the splits of K. */
+mq_status mq_gemm_fp8_tile(int M, int N, int K, int* rows, int* cols, int* splits);
+mq_status mq_gemm_fp8(int M, int N, int K, const void* Xq, int ldx, const float* s_x, int lds,
+                      const uint8_t* Wq, const float* s_w, mq_dtype type, const void* bias,
+                      void* Y, int ldy, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Paged cache of keys and values in 8 bits (OCP e4m3).  Pages hold page_size tokens (a
  * power of two, 32 .. 65536) of every key head; head_dim is 64 or 128.  A slot is
  * page * page_size + the place in the page.  Each block of 32 tokens of a page and

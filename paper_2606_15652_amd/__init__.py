@@ -77,6 +77,14 @@ _SIG = {
     "mq_attention_kv4_workspace_size": (C.c_size_t, [_I, _I, _I, _I, _I, _I, _L]),
     "mq_attention_kv4": (_I, [_P, _I, _I, _I, _I, _L, _I, _P, _L, _L, _P, _I, _P, _P, _F, _I, _P, _L, _L, _P,
                               C.c_size_t, _P]),
+    "mq_quantize_rows_fp8": (_I, [_I, _I, _I, _P, _I, _P, _I, _P, _I, _P]),
+    "mq_weight_fp8_bytes": (C.c_size_t, [_I, _I]),
+    "mq_quantize_weight_fp8": (_I, [_P, _I, _I, _I, _P, _P, _P]),
+    "mq_repack_weight_fp8": (_I, [_I, _I, _P, _I, _P, _P]),
+    "mq_unpack_weight_fp8": (_I, [_I, _I, _P, _P, _I, _P]),
+    "mq_gemm_fp8_workspace_size": (C.c_size_t, [_I, _I, _I]),
+    "mq_gemm_fp8_tile": (_I, [_I, _I, _I, _P, _P, _P]),
+    "mq_gemm_fp8": (_I, [_I, _I, _I, _P, _I, _P, _I, _P, _P, _I, _P, _P, _I, _P, C.c_size_t, _P]),
     "mq_kv8_code_bytes": (C.c_size_t, [_I, _I, _I, _I]),
     "mq_kv8_append": (_I, [_P, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
     "mq_kv8_read": (_I, [_P, _I, _I, _P, _P, _L, _L, _P, _L, _L, _P]),
@@ -562,4 +570,5 @@ from .serving import (  # noqa: E402  (needs the names above)
     gemm_w8a8_tile, gemm_w8a8_workspace_bytes, kv4_append, kv4_cache, kv4_read, quantize_rows8, quantize_weight8, repack_weight8,
     rms_norm_quantize8, unpack_weight8)
 from .fp8 import (  # noqa: E402
-    KVCache8, attention_kv8, attention_kv8_workspace_bytes, kv8_append, kv8_cache, kv8_read, sample)
+    KVCache8, PackedWeightFP8, attention_kv8, attention_kv8_workspace_bytes, gemm_fp8, gemm_fp8_tile, gemm_fp8_workspace_bytes,
+    kv8_append, kv8_cache, kv8_read, quantize_rows_fp8, quantize_weight_fp8, repack_weight_fp8, sample, unpack_weight_fp8)

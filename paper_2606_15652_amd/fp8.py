@@ -1,5 +1,5 @@
-"""Binding of the operators in 8-bit floating point (OCP e4m3), the paged 8-bit cache and the attention over it, and of
-sampling.
+"""Binding of the operators in 8-bit floating point (OCP e4m3): the product with scales for blocks of 128, the paged
+8-bit cache and the attention over it; and of sampling.
 
 As in the package's other calls only arguments are checked and marshalled here; ``include/mq.h`` documents each
 operator.  Values are fp16 or bf16.  A call runs on the device of its tensors, which need not be the current one,
@@ -13,7 +13,7 @@ from contextlib import nullcontext
 from dataclasses import dataclass, field
 
 from . import _check, _need, _need_out, _ptr, _scratch, _stream, _torch, load
-from .serving import _dtype_code, _empty, _need_heads, _same_device
+from .serving import _dtype_code, _empty, _need_heads, _need_rows, _same_device
 
 _no_guard = nullcontext()
 
@@ -25,6 +25,170 @@ def _on(t, stream):
     if stream is not None and stream.device_index != device:
         raise ValueError(f"the stream is of cuda:{stream.device_index}, the tensors are on cuda:{device}")
     return _no_guard if torch._C._cuda_getDevice() == device else torch.cuda.device(device)
+
+
+# ----------------------------------------------------- block-scaled product --
+def _groups(K):
+    return -(-K // 128)
+
+
+def _need_codes_fp8(Xq, K=None):
+    """e4m3 rows as the kernels take them: their stride in bytes.  The bytes up to the next multiple of 16 after a row's
+    last code have to be there too."""
+    torch = _torch()
+    ld = _need_rows(Xq, "Xq", K)
+    if Xq.dtype != torch.float8_e4m3fn:
+        raise TypeError(f"Xq must be torch.float8_e4m3fn, got {Xq.dtype}")
+    M, K = Xq.shape
+    padded = -(-K // 16) * 16
+    if M <= 1:
+        ld = padded                             # one row: its stride says nothing
+    if ld < padded or ld % 16:
+        raise ValueError(f"Xq's rows must start every multiple of 16 bytes, at least {padded}; got a row stride of {ld}")
+    if padded != K and M and Xq.storage_offset() + (M - 1) * ld + padded > Xq.untyped_storage().nbytes():
+        raise ValueError("Xq's last row must be followed by its padding to 16 bytes")
+    return ld
+
+
+def _need_scales(s_x, M, K):
+    """fp32 [M, groups] with the tokens next to each other: the stride of the groups."""
+    torch = _torch()
+    if not isinstance(s_x, torch.Tensor) or not s_x.is_cuda or s_x.dtype != torch.float32:
+        raise TypeError("s_x must be an fp32 CUDA (HIP) tensor")
+    if tuple(s_x.shape) != (M, _groups(K)):
+        raise ValueError(f"s_x must be [{M}, {_groups(K)}], got {tuple(s_x.shape)}")
+    token, group = s_x.stride()
+    if (token != 1 and M > 1) or (group < M and s_x.shape[1] > 1):
+        raise ValueError("s_x must have the tokens of a group next to each other (strides 1, at least the tokens)")
+    return group if s_x.shape[1] > 1 else M
+
+
+def quantize_rows_fp8(X, out=None, stream=None):
+    """Quantisation of fp16 / bf16 X [M, K] to e4m3 with a scale for each token and 128 channels: (Xq float8_e4m3fn [M, K]
+    with padded rows, s_x fp32 [M, ceil(K / 128)], the tokens of a group next to each other)."""
+    torch = _torch()
+    code = _dtype_code(getattr(X, "dtype", None), "X")
+    ldx = _need_rows(X, "X")
+    M, K = X.shape
+    if out is None:
+        ldq = -(-K // 16) * 16
+        rows = _empty((M, ldq), torch.float8_e4m3fn, X.device, stream)
+        Xq, s_x = (rows if ldq == K else rows[:, :K]), _empty((_groups(K), M), torch.float32, X.device, stream).t()
+        lds = M
+    else:
+        Xq, s_x = out
+        ldq, lds = _need_codes_fp8(Xq, K), _need_scales(s_x, M, K)
+        if Xq.shape[0] != M:
+            raise ValueError(f"out[0] (Xq) must have {M} rows, got {Xq.shape[0]}")
+        _same_device(X, "X", Xq=Xq, s_x=s_x)
+    with _on(X, stream):
+        _check("mq_quantize_rows_fp8", load().mq_quantize_rows_fp8(M, K, code, X.data_ptr(), ldx, Xq.data_ptr(), ldq, s_x.data_ptr(), lds,
+                                                                   _stream(stream)))
+    return Xq, s_x
+
+
+@dataclass
+class PackedWeightFP8:
+    """e4m3 weight of N channels of K codes in the library layout (include/mq.h), a scale for each block of 128 x 128."""
+    N: int
+    K: int
+    Wq: "object"          # uint8 [mq_weight_fp8_bytes(N, K)]
+    s_w: "object"         # fp32 [ceil(N / 128), ceil(K / 128)]
+    _of: tuple = field(default=(), repr=False, init=False, compare=False)     # what _operands found to go together
+
+    def _operands(self):
+        """Addresses of the codes and scales, which have to be those of N and K: kernels read as much of them."""
+        of, Wq, s_w = self._of, self.Wq, self.s_w
+        if not (of and of[0] is Wq and of[1] is s_w and of[2] == (self.N, self.K, Wq.numel(), s_w.numel())):
+            torch, need = _torch(), load().mq_weight_fp8_bytes(self.N, self.K)
+            if need == 0:
+                raise ValueError(f"no e4m3 weight of {self.N} channels and {self.K} codes")
+            _need_out(Wq, (need,), torch.uint8, "Wq")
+            _need_out(s_w, (_groups(self.N), _groups(self.K)), torch.float32, "s_w")
+            _same_device(Wq, "Wq", s_w=s_w)
+            self._of = (Wq, s_w, (self.N, self.K, need, s_w.numel()))
+        return Wq.data_ptr(), s_w.data_ptr()
+
+    @property
+    def nbytes(self) -> int:
+        return self.Wq.numel() + 4 * self.s_w.numel()
+
+
+def _weight_fp8(N, K, device, stream):
+    nbytes = load().mq_weight_fp8_bytes(N, K)
+    if nbytes == 0:
+        raise ValueError(f"no e4m3 weight of {N} channels and {K} codes")
+    return _empty((nbytes,), _torch().uint8, device, stream)
+
+
+def quantize_weight_fp8(W, stream=None) -> PackedWeightFP8:
+    """fp32 W [N, K] -> e4m3 codes with a scale for each block of 128 x 128."""
+    torch = _torch()
+    _need(W, torch.float32, "W", 2)
+    N, K = W.shape
+    Wq = _weight_fp8(N, K, W.device, stream)
+    s_w = _empty((_groups(N), _groups(K)), torch.float32, W.device, stream)
+    with _on(W, stream):
+        _check("mq_quantize_weight_fp8", load().mq_quantize_weight_fp8(W.data_ptr(), N, K, W.stride(0), Wq.data_ptr(), s_w.data_ptr(),
+                                                                       _stream(stream)))
+    return PackedWeightFP8(N, K, Wq, s_w)
+
+
+def repack_weight_fp8(Wc, s_w, stream=None) -> PackedWeightFP8:
+    """Canonical codes float8_e4m3fn [N, K] and their scales fp32 [ceil(N / 128), ceil(K / 128)] -> the library layout."""
+    torch = _torch()
+    _need(Wc, torch.float8_e4m3fn, "Wc", 2)
+    N, K = Wc.shape
+    _need_out(s_w, (_groups(N), _groups(K)), torch.float32, "s_w")
+    _same_device(Wc, "Wc", s_w=s_w)
+    Wq = _weight_fp8(N, K, Wc.device, stream)
+    with _on(Wc, stream):
+        _check("mq_repack_weight_fp8", load().mq_repack_weight_fp8(N, K, Wc.data_ptr(), Wc.stride(0), Wq.data_ptr(), _stream(stream)))
+    return PackedWeightFP8(N, K, Wq, s_w)
+
+
+def unpack_weight_fp8(pw: PackedWeightFP8, stream=None):
+    """Library layout -> canonical codes float8_e4m3fn [N, K]."""
+    torch = _torch()
+    Wq, _ = pw._operands()
+    Wc = _empty((pw.N, pw.K), torch.float8_e4m3fn, pw.Wq.device, stream)
+    with _on(Wc, stream):
+        _check("mq_unpack_weight_fp8", load().mq_unpack_weight_fp8(pw.N, pw.K, Wq, Wc.data_ptr(), pw.K, _stream(stream)))
+    return Wc
+
+
+def gemm_fp8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().mq_gemm_fp8_workspace_size(M, N, K))
+
+
+def gemm_fp8_tile(M: int, N: int, K: int):
+    """(rows, columns) of the output tile one workgroup takes, and the splits of K (host logic only)."""
+    r, c, s = C.c_int(0), C.c_int(0), C.c_int(0)
+    _check("mq_gemm_fp8_tile", load().mq_gemm_fp8_tile(M, N, K, C.byref(r), C.byref(c), C.byref(s)))
+    return r.value, c.value, s.value
+
+
+def gemm_fp8(Xq, s_x, pw: PackedWeightFP8, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
+    """Y [M, N] = sum over groups of s_x s_w (Xq Wq^T) + bias, in fp16 (or ``out_dtype`` bf16, fp32); bias in Y's type."""
+    torch = _torch()
+    ldx = _need_codes_fp8(Xq, pw.K)
+    M = Xq.shape[0]
+    Wq, s_w = pw._operands()
+    lds = _need_scales(s_x, M, pw.K)
+    Y = out if out is not None else _empty((M, pw.N), out_dtype or torch.float16, Xq.device, stream)
+    code, ldy = _dtype_code(Y.dtype, "out", fp32=True), _need_rows(Y, "out", pw.N)
+    if Y.shape[0] != M:
+        raise ValueError(f"out must have {M} rows, got {Y.shape[0]}")
+    if bias is not None:
+        _need_out(bias, (pw.N,), Y.dtype, "bias")
+    _same_device(Xq, "Xq", s_x=s_x, weight=pw.Wq, bias=bias, out=Y, workspace=workspace)
+    lib = load()
+    ws = lib.mq_gemm_fp8_workspace_size(M, pw.N, pw.K)
+    with _on(Xq, stream):
+        wbuf = _scratch(ws, Xq.device, stream, workspace)
+        _check("mq_gemm_fp8", lib.mq_gemm_fp8(M, pw.N, pw.K, Xq.data_ptr(), ldx, s_x.data_ptr(), lds, Wq, s_w, code, _ptr(bias),
+                                              Y.data_ptr(), ldy, _ptr(wbuf), ws, _stream(stream)))
+    return Y
 
 
 # -------------------------------------------------------- 8-bit cache --
