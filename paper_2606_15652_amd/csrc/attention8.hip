@@ -83,11 +83,10 @@ __device__ __forceinline__ f16x8 operand8(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(f16x8, r);
 }
 
-// s c - m, the product rounded before it meets m: m is one of these products, and where they pass 2^24 an exact product
-// would differ from it by more than any weight allows.
-__device__ __forceinline__ float score8(float s, float c, float m) {
+// A product that is rounded before anything is taken from it.
+__device__ __forceinline__ float rounded_product(float a, float b) {
 #pragma clang fp contract(off)
-    return s * c - m;
+    return a * b;
 }
 
 // The largest of v over the lanes l, l ^ 16, l ^ 32, l ^ 48 (a column's).
@@ -96,82 +95,218 @@ __device__ __forceinline__ float column_max(float v) {
     return fmaxf(v, __shfl_xor(v, 32));
 }
 
-// WT waves of a workgroup share out the tokens of its columns (blocks in turn), 4 / WT take columns of their own.
-template <typename T, int D, int NT, int WT>
-__global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
-    constexpr int COLS = 16 * NT, WC = 4 / WT, STEPS = D / 32, PIECES = D / 32;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wt = wave % WT, wc = wave / WT, col = lane & 15, quarter = lane >> 4;
-    const int b = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads;
-    const int group_block = gridDim.y - 1 - blockIdx.y;     // the longest first
-    const Sequence8 seq(a, b);
-    const int columns = seq.queries * a.group;
-    const int first_col = group_block * WC * COLS;          // of the workgroup
-    if (first_col >= columns) return;
-    const int64_t seen = seq.seen(a, (min(first_col + WC * COLS, columns) - 1) / a.group);
-    const int chunks = max(1, (int)((seen + a.chunk - 1) / a.chunk));
-    if ((int)blockIdx.z >= chunks) return;
-    const int64_t from = (int64_t)blockIdx.z * a.chunk;
-
-    // this wave's columns
-    const int col0 = first_col + wc * COLS;
+// The columns of one wave: their queries as operands, and what has been summed up for them.
+template <typename T, int D, int NT>
+struct Columns8 {
+    static constexpr int STEPS = D / 32, TILES = D / 16;    // of 32 channels of keys, of 16 channels of values
     f16x8 q[NT][STEPS];
     float slope[NT];                                        // of the scores, in log2
-    int64_t sees[NT], least = seen, most = 0;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int c = col0 + 16 * n + col;
-        const bool there = c < columns;
-        const int qi = there ? c / a.group : 0, hg = there ? c % a.group : 0;
-        const int64_t row = (int64_t)seq.first + qi;
-        const bool has = there && row >= 0 && row < a.tokens;
-        sees[n] = has ? seq.seen(a, qi) : 0;
-        const T* p = static_cast<const T*>(a.q) + (has ? row * a.q_token + (int64_t)(head * a.group + hg) * a.q_head : 0) + 16 * quarter;
-        f32x8 x[STEPS];
-        uint32_t big = 0;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            x[s] = has ? load8(p + s / 2 * 64 + s % 2 * 8) : f32x8{};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
-        }
-        big = max(big, (uint32_t)__shfl_xor((int)big, 16));
-        big = max(big, (uint32_t)__shfl_xor((int)big, 32));
-        // bf16: by a power of two so that the largest is in [2^14, 2^15).  A query that is not finite is NaN throughout.
-        const int by = sizeof(T) == 2 && __is_same(T, __bf16) && big ? 141 - (int)(big >> 23) : 0;
-        const bool bad = big >= kFloatInf;
-        slope[n] = fminf(ldexpf(a.scale, -by), FLT_MAX);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[n][s][j] = bad ? (_Float16)__builtin_nanf("") : (_Float16)ldexpf(x[s][j], by);
-        least = has && sees[n] < least ? sees[n] : least;
-        most = sees[n] > most ? sees[n] : most;
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        least = min(least, (int64_t)__shfl_xor((long long)least, m));
-        most = max(most, (int64_t)__shfl_xor((long long)most, m));
-    }
-    const int64_t until = min(from + a.chunk, most);
-    const int first_block = (int)(from / kBlockTokens) + wt, end_block = (int)((until + kBlockTokens - 1) / kBlockTokens);
-    const int whole_end = (int)(least / kBlockTokens);      // blocks before this are seen by every column
-
-    f32x4 o[2 * PIECES][NT] = {};
+    int sees[NT];                                           // tokens that the column sees
+    int least, most;                                        // over the columns that are there
+    f32x4 o[TILES][NT];
     float m[NT], jj[NT], l[NT];
+
+    __device__ __forceinline__ Columns8(const Attn8Args& a, const Sequence8& seq, int head, int col0) {
+        const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, columns = seq.queries * a.group;
+        least = (int)seq.len;
+        most = 0;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n] = kLowest;
-        jj[n] = kNone;
-        l[n] = 0.0f;
+        for (int n = 0; n < NT; ++n) {
+            const int c = col0 + 16 * n + col;
+            const bool there = c < columns;
+            const int qi = there ? c / a.group : 0, hg = there ? c % a.group : 0;
+            const int64_t row = (int64_t)seq.first + qi;
+            const bool has = there && row >= 0 && row < a.tokens;
+            sees[n] = has ? (int)seq.seen(a, qi) : 0;
+            const T* p = static_cast<const T*>(a.q) + (has ? row * a.q_token + (int64_t)(head * a.group + hg) * a.q_head : 0) + 16 * quarter;
+            f32x8 x[STEPS];
+            uint32_t big = 0;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                x[s] = has ? load8(p + s / 2 * 64 + s % 2 * 8) : f32x8{};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) big = max(big, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
+            }
+            big = max(big, (uint32_t)__shfl_xor((int)big, 16));
+            big = max(big, (uint32_t)__shfl_xor((int)big, 32));
+            // bf16: by a power of two so that the largest is in [2^14, 2^15).  A query that is not finite is NaN throughout.
+            const int by = __is_same(T, __bf16) && big ? 141 - (int)(big >> 23) : 0;
+            const bool bad = big >= kFloatInf;
+            slope[n] = fminf(ldexpf(a.scale, -by), FLT_MAX);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[n][s][j] = bad ? (_Float16)__builtin_nanf("") : (_Float16)ldexpf(x[s][j], by);
+            least = has && sees[n] < least ? sees[n] : least;
+            most = max(most, sees[n]);
+            m[n] = kLowest;
+            jj[n] = kNone;
+            l[n] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) o[i][n] = f32x4{};
+        }
+#pragma unroll
+        for (int k = 32; k >= 1; k >>= 1) {
+            least = min(least, __shfl_xor(least, k));
+            most = max(most, __shfl_xor(most, k));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
     }
-    const int32_t* table = a.table + (int64_t)b * a.table_pages;
+
+    // One block of 32 tokens: key(t, s) and value(i) give the operands of its two tiles of tokens, and of its channels.
+    template <typename K, typename V>
+    __device__ __forceinline__ void take(int block, int ke, int ve, K&& key, V&& value) {
+        const int quarter = (threadIdx.x & 63) >> 4;
+        f32x4 s[NT][2] = {};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const f16x8 k = key(t, i);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][i], s[n][t], 0, 0, 0);
+            }
+        const float ev = (float)(ve - 127);
+        f16x8 w[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float c = fminf(fmaxf(ldexpf(slope[n], ke - 127), FLT_MIN), FLT_MAX);   // not 0: hidden scores stay -infinity
+            if ((block + 1) * kBlockTokens > least) {
+                const int left = sees[n] - block * kBlockTokens - 4 * quarter;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * t + r >= left) s[n][t][r] = -INFINITY;
+            }
+            // Scores as they are usual: the product less m and the weights' exponent in one operation, and p from w.  Not so where
+            // a maximum moves, where m passes 2^20 (m is a rounded product: an exact one may differ from it by more than any
+            // weight allows), and where w may lose what p still has.
+            float e = ev - jj[n] + kLift, from_m = e - m[n];
+            float y[8], high = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = __builtin_fmaf(s[n][j / 4][j % 4], c, from_m);
+                high = fmaxf(high, y[j]);
+            }
+            // p <= 2^kSlack, w <= 2^(kSlack + kLift)
+            if (__ballot(high > kSlack + fminf(e, kLift) || !(fabsf(m[n]) < 0x1p20f) || e < -60.0f)) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    y[j] = rounded_product(s[n][j / 4][j % 4], c);
+                    top = fmaxf(top, y[j]);
+                }
+                top = column_max(top);
+                const float was = m[n];
+                if (top > was + kSlack || ceilf(top - was) + ev > jj[n] + kSlack) {
+                    m[n] = fmaxf(was, ceilf(top));
+                    const float old = jj[n] + (was - m[n]);     // J of what O holds, by the new m
+                    jj[n] = fmaxf(fmaxf(old, ceilf(top - m[n]) + ev), kNone);
+                    l[n] *= __builtin_amdgcn_exp2f(was - m[n]);
+                    const float by = __builtin_amdgcn_exp2f(old - jj[n]);
+#pragma unroll
+                    for (int i = 0; i < TILES; ++i) o[i][n] *= by;
+                }
+                const int by = (int)fminf(ev - jj[n] + kLift, 1000.0f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(y[j] - m[n]);
+                    l[n] += p;
+                    w[n][j] = (_Float16)ldexpf(p, by);
+                }
+            } else {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(y[j]);
+                    sum += p;
+                    w[n][j] = (_Float16)p;
+                }
+                l[n] = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-e), l[n]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const f16x8 v = value(i);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[n], o[i][n], 0, 0, 0);
+        }
+    }
+
+    __device__ __forceinline__ void sum_up() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+        }
+    }
+};
+
+// Four channels ch .. of column c's result, as values, or where chunks share the column as sums.
+template <typename T, int D>
+__device__ __forceinline__ void store_column8(const Attn8Args& a, const Sequence8& seq, int head, int c, int ch, f32x4 sum, float m, float j,
+                                              float l, bool direct) {
+    if (direct) {
+        const int64_t row = (int64_t)seq.first + c / a.group;
+        if (row < 0 || row >= a.tokens) return;
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        f32x4 y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = l == 0.0f ? 0.0f : ldexpf(sum[r] / l, (int)fmaxf(j - kLift, -1000.0f));
+        *reinterpret_cast<t4*>(static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head + ch) =
+            __builtin_convertvector(y, t4);
+    } else {
+        const int64_t at = ((int64_t)blockIdx.x * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
+        *reinterpret_cast<f32x4*>(a.part + at * D + ch) = sum;
+        if (ch == 0) {
+            a.stats[3 * at] = m;
+            a.stats[3 * at + 1] = j;
+            a.stats[3 * at + 2] = l;
+        }
+    }
+}
+
+// What a workgroup takes: `cols` columns of a sequence and key head, and a chunk of the tokens that they see.
+struct Part8 {
+    int b, head, first_col, columns, chunks, from, until;
+    bool empty;
+    __device__ __forceinline__ Part8(const Attn8Args& a, int cols) {
+        b = blockIdx.x / a.c.heads;
+        head = blockIdx.x % a.c.heads;
+        const Sequence8 seq(a, b);
+        columns = seq.queries * a.group;
+        first_col = (int)(gridDim.y - 1 - blockIdx.y) * cols;               // the longest first
+        empty = first_col >= columns;
+        if (empty) return;
+        const int seen = (int)seq.seen(a, (min(first_col + cols, columns) - 1) / a.group);
+        chunks = max(1, (seen + a.chunk - 1) / a.chunk);
+        empty = (int)blockIdx.z >= chunks;
+        from = (int)blockIdx.z * a.chunk;
+        until = min(from + a.chunk, seen);
+    }
+};
+
+// Few columns: the waves share out the tokens (WT of them; blocks in turn), 4 / WT take 16 NT columns of their own.  Codes go
+// from memory to registers, a block ahead.
+template <typename T, int D, int NT, int WT>
+__global__ __launch_bounds__(256, 2) void attention8_kernel(Attn8Args a) {
+    constexpr int COLS = 16 * NT, WC = 4 / WT, PIECES = D / 32, TILES = D / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wt = wave % WT, wc = wave / WT, col = lane & 15, quarter = lane >> 4;
+    const Part8 part(a, WC * COLS);
+    if (part.empty) return;
+    const Sequence8 seq(a, part.b);
+    Columns8<T, D, NT> cols(a, seq, part.head, part.first_col + wc * COLS);
+
+    const int32_t* table = a.table + (int64_t)part.b * a.table_pages;
     struct Block {
         uint4 k[PIECES], v[PIECES];
         int ke, ve;                                         // ve < 0: no page holds it
     };
     auto load = [&](Block& x, int block) {
-        const int64_t row = block_row8(a.c, table, a.table_pages, block, head);
+        const int64_t row = block_row8(a.c, table, a.table_pages, block, part.head);
         const int64_t at = row < 0 ? 0 : row;
         const uint8_t *k = a.c.k + at * D + lane * 16, *v = a.c.v + at * D + lane * 16;
 #pragma unroll
@@ -183,72 +318,12 @@ __global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
     };
     auto take = [&](const Block& x, int block) {
         if (__builtin_amdgcn_readfirstlane(x.ve) < 0) return;
-        f32x4 s[NT][2] = {};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < PIECES / 2; ++i) {
-                const uint4 p = x.k[t * (PIECES / 2) + i];
-                const f16x8 k0 = operand8(p.x, p.y), k1 = operand8(p.z, p.w);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * i], s[n][t], 0, 0, 0);
-                    s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * i + 1], s[n][t], 0, 0, 0);
-                }
-            }
-        const float ev = (float)(x.ve - 127);
-        f16x8 w[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float c = fminf(ldexpf(slope[n], x.ke - 127), FLT_MAX);
-            if (block >= whole_end) {
-                const int64_t left = sees[n] - (int64_t)block * kBlockTokens - 4 * quarter;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (16 * t + r >= left) s[n][t][r] = -INFINITY;
-            }
-            float y[8], high = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                y[j] = score8(s[n][j / 4][j % 4], c, m[n]);
-                high = fmaxf(high, y[j]);
-            }
-            if (__ballot(high > fminf(kSlack, jj[n] + kSlack - ev))) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, s[n][j / 4][j % 4] * c);
-                top = column_max(top);
-                const float was = m[n];
-                m[n] = fmaxf(was, ceilf(top));
-                const float old = jj[n] + (was - m[n]);     // J of what O holds, by the new m
-                jj[n] = fmaxf(fmaxf(old, ceilf(top - m[n]) + ev), kNone);
-                l[n] *= __builtin_amdgcn_exp2f(was - m[n]);
-                const float by = __builtin_amdgcn_exp2f(old - jj[n]);
-#pragma unroll
-                for (int i = 0; i < 2 * PIECES; ++i) o[i][n] *= by;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = score8(s[n][j / 4][j % 4], c, m[n]);
-            }
-            const int e = (int)fminf(ev - jj[n] + kLift, 1000.0f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float p = __builtin_amdgcn_exp2f(y[j]);
-                l[n] += p;
-                w[n][j] = (_Float16)ldexpf(p, e);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const f16x8 v0 = operand8(x.v[i].x, x.v[i].y), v1 = operand8(x.v[i].z, x.v[i].w);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                o[2 * i][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[n], o[2 * i][n], 0, 0, 0);
-                o[2 * i + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n], o[2 * i + 1][n], 0, 0, 0);
-            }
-        }
+        auto half = [](const uint4 p, int h) { return h ? operand8(p.z, p.w) : operand8(p.x, p.y); };
+        cols.take(block, x.ke, x.ve, [&](int t, int s) { return half(x.k[t * (PIECES / 2) + s / 2], s % 2); },
+                  [&](int i) { return half(x.v[i / 2], i % 2); });
     };
+    const int first_block = part.from / kBlockTokens + wt;
+    const int end_block = (min(part.until, cols.most) + kBlockTokens - 1) / kBlockTokens;
     Block x0, x1;
     if (first_block < end_block) load(x0, first_block);
     for (int block = first_block; block < end_block; block += 2 * WT) {
@@ -258,73 +333,124 @@ __global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
         if (block + 2 * WT < end_block) load(x0, block + 2 * WT);
         take(x1, block + WT);
     }
+    cols.sum_up();
+
+    // the waves' sums of a column, in LDS
+    __shared__ float sums[4][COLS][D + 4], stat[4][COLS][3];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        l[n] += __shfl_xor(l[n], 16);
-        l[n] += __shfl_xor(l[n], 32);
-    }
-
-    // four channels 16 i + 4 quarter .. of a column's result, as sums or as values
-    const bool direct = chunks == 1;
-    auto store = [&](int c, int ch, f32x4 sum, float mm, float j, float ll) {
-        if (direct) {
-            const int64_t row = (int64_t)seq.first + c / a.group;
-            if (row < 0 || row >= a.tokens) return;
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            f32x4 y;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = ll == 0.0f ? 0.0f : ldexpf(sum[r] / ll, (int)fmaxf(j - kLift, -1000.0f));
-            *reinterpret_cast<t4*>(static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head + ch) =
-                __builtin_convertvector(y, t4);
-        } else {
-            const int64_t at = ((int64_t)blockIdx.x * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
-            *reinterpret_cast<f32x4*>(a.part + at * D + ch) = sum;
-            if (ch == 0) {
-                a.stats[3 * at] = mm;
-                a.stats[3 * at + 1] = j;
-                a.stats[3 * at + 2] = ll;
-            }
+        for (int i = 0; i < TILES; ++i)
+            *reinterpret_cast<f32x4*>(&sums[wave][16 * n + col][16 * i + 4 * quarter]) = cols.o[i][n];
+        if (quarter == 0) {
+            stat[wave][16 * n + col][0] = cols.m[n];
+            stat[wave][16 * n + col][1] = cols.jj[n];
+            stat[wave][16 * n + col][2] = cols.l[n];
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < WC * COLS * (D / 4); e += 256) {
+        const int c = e / (D / 4), ch = e % (D / 4) * 4, w0 = c / COLS * WT, cc = c % COLS;
+        if (part.first_col + c >= part.columns) continue;
+        float mm = kLowest, j = kNone, ll = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WT; ++w) mm = fmaxf(mm, stat[w0 + w][cc][0]);
+#pragma unroll
+        for (int w = 0; w < WT; ++w) j = fmaxf(j, stat[w0 + w][cc][1] + (stat[w0 + w][cc][0] - mm));
+        f32x4 sum = {};
+#pragma unroll
+        for (int w = 0; w < WT; ++w) {
+            const float by = stat[w0 + w][cc][0] - mm;
+            ll += stat[w0 + w][cc][2] * __builtin_amdgcn_exp2f(by);
+            sum += *reinterpret_cast<const f32x4*>(&sums[w0 + w][cc][ch]) * __builtin_amdgcn_exp2f(stat[w0 + w][cc][1] + by - j);
+        }
+        store_column8<T, D>(a, seq, part.head, part.first_col + c, ch, sum, mm, j, ll, part.chunks == 1);
+    }
+}
+
+// Many columns: each wave takes 16 NT of them and all tokens.  A stage of 4096 / D tokens is turned to fp16 once, a share by each
+// wave, and lies in LDS in operand order, in two slots: while one is used the next is written and the one after is on its way
+// from memory.  One barrier a stage.
+template <typename T, int D, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attention8_wide_kernel(Attn8Args a) {
+    constexpr int COLS = 16 * NT, PIECES = D / 32, TILES = D / 16, STEPS = D / 32;
+    constexpr int BLOCKS = 128 / D, LOADS = 8 / WAVES;      // of a stage; pieces of 1 KB of codes of a wave and stage
+    __shared__ __attribute__((aligned(16))) f16x8 staged[2][BLOCKS][4 * PIECES][64];    // keys' steps by tile, values' tiles
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const Part8 part(a, WAVES * COLS);
+    if (part.empty) return;
+    const Sequence8 seq(a, part.b);
+    Columns8<T, D, NT> cols(a, seq, part.head, part.first_col + wave * COLS);
+
+    const int32_t* table = a.table + (int64_t)part.b * a.table_pages;
+    const int first = part.from / kBlockTokens, end = (part.until + kBlockTokens - 1) / kBlockTokens;
+    const int mine = min(end, (cols.most + kBlockTokens - 1) / kBlockTokens);
+    struct Stage {
+        uint4 p[LOADS];
+        int ke[BLOCKS], ve[BLOCKS];                         // ve < 0: no page holds the block
+    };
+    auto load = [&](Stage& x, int block) {
+        int64_t at[BLOCKS];
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            const int64_t row = block + b < end ? block_row8(a.c, table, a.table_pages, block + b, part.head) : -1;
+            at[b] = row < 0 ? 0 : row;
+            x.ke[b] = a.c.ke[at[b] / kBlockTokens];
+            x.ve[b] = row < 0 ? -1 : a.c.ve[at[b] / kBlockTokens];
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int piece = wave * LOADS + i, b = piece / (2 * PIECES), r = piece % (2 * PIECES);
+            const int64_t row = BLOCKS == 1 || b == 0 ? at[0] : at[BLOCKS - 1];
+            x.p[i] = ldg16((r < PIECES ? a.c.k : a.c.v) + row * D + r % PIECES * 1024 + lane * 16);
         }
     };
-    if constexpr (WT == 1) {
+    auto write = [&](const Stage& x, int slot) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int c = col0 + 16 * n + col;
-            if (c < columns)
-#pragma unroll
-                for (int i = 0; i < 2 * PIECES; ++i) store(c, 16 * i + 4 * quarter, o[i][n], m[n], jj[n], l[n]);
+        for (int i = 0; i < LOADS; ++i) {
+            const int piece = wave * LOADS + i, b = piece / (2 * PIECES), r = piece % (2 * PIECES);
+            staged[slot][b][2 * r][lane] = operand8(x.p[i].x, x.p[i].y);
+            staged[slot][b][2 * r + 1][lane] = operand8(x.p[i].z, x.p[i].w);
         }
-    } else {
-        __shared__ float sums[4][COLS][D + 4], stat[4][COLS][3];
+    };
+    auto take = [&](const Stage& x, int block, int slot) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int i = 0; i < 2 * PIECES; ++i)
-                *reinterpret_cast<f32x4*>(&sums[wave][16 * n + col][16 * i + 4 * quarter]) = o[i][n];
-            if (quarter == 0) {
-                stat[wave][16 * n + col][0] = m[n];
-                stat[wave][16 * n + col][1] = jj[n];
-                stat[wave][16 * n + col][2] = l[n];
-            }
+        for (int b = 0; b < BLOCKS; ++b) {
+            if (block + b >= mine || __builtin_amdgcn_readfirstlane(x.ve[b]) < 0) continue;
+            cols.take(block + b, x.ke[b], x.ve[b], [&](int t, int s) { return staged[slot][b][t * STEPS + s][lane]; },
+                      [&](int i) { return staged[slot][b][2 * PIECES + i][lane]; });
         }
+    };
+    static_assert(2 * STEPS == 2 * PIECES && TILES == 2 * PIECES, "as many operands of keys as of values");
+    Stage x0, x1;
+    if (first < end) {
+        load(x0, first);
+        write(x0, 0);
+        load(x1, first + BLOCKS);
+    }
+    __syncthreads();
+    for (int block = first; block < end; block += 2 * BLOCKS) {
+        Stage x2;
+        write(x1, 1);
+        load(x2, block + 2 * BLOCKS);
+        take(x0, block, 0);
         __syncthreads();
-        for (int e = threadIdx.x; e < WC * COLS * (D / 4); e += 256) {
-            const int c = e / (D / 4), ch = e % (D / 4) * 4, w0 = c / COLS * WT, cc = c % COLS;
-            if (first_col + c >= columns) continue;
-            float mm = kLowest, j = kNone, ll = 0.0f;
+        write(x2, 0);
+        x0 = x2;
+        load(x2, block + 3 * BLOCKS);
+        take(x1, block + BLOCKS, 1);
+        x1 = x2;
+        __syncthreads();
+    }
+    cols.sum_up();
 #pragma unroll
-            for (int w = 0; w < WT; ++w) mm = fmaxf(mm, stat[w0 + w][cc][0]);
+    for (int n = 0; n < NT; ++n) {
+        const int c = part.first_col + wave * COLS + 16 * n + col;
+        if (c < part.columns)
 #pragma unroll
-            for (int w = 0; w < WT; ++w) j = fmaxf(j, stat[w0 + w][cc][1] + (stat[w0 + w][cc][0] - mm));
-            f32x4 sum = {};
-#pragma unroll
-            for (int w = 0; w < WT; ++w) {
-                const float by = stat[w0 + w][cc][0] - mm;
-                ll += stat[w0 + w][cc][2] * __builtin_amdgcn_exp2f(by);
-                sum += *reinterpret_cast<const f32x4*>(&sums[w0 + w][cc][ch]) * __builtin_amdgcn_exp2f(stat[w0 + w][cc][1] + by - j);
-            }
-            store(first_col + c, ch, sum, mm, j, ll);
-        }
+            for (int i = 0; i < TILES; ++i)
+                store_column8<T, D>(a, seq, part.head, c, 16 * i + 4 * quarter, cols.o[i][n], cols.m[n], cols.jj[n], cols.l[n], part.chunks == 1);
     }
 }
 
@@ -332,7 +458,7 @@ __global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attention8_join_kernel(Attn8Args a, int block_cols) {
     constexpr int LANES = D / 4, PARTS = 256 / LANES;
-    __shared__ float sums[PARTS][D + 4], heads[PARTS][2], ls[PARTS];
+    __shared__ float sums[PARTS][D + 4], ls[PARTS];
     const int most = a.max_q * a.group, unit = blockIdx.x / most, c = blockIdx.x % most;
     const int b = unit / a.c.heads, head = unit % a.c.heads;
     const Sequence8 seq(a, b);
@@ -344,14 +470,20 @@ __global__ __launch_bounds__(256) void attention8_join_kernel(Attn8Args a, int b
     if (chunks == 1 || row < 0 || row >= a.tokens) return;
     const int64_t stride = most, first = (int64_t)unit * a.chunks * stride + c;
     const int part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
+    // every wave finds the maxima, 64 chunks at a time
     float m = kLowest, j = kNone;
-    for (int i = 0; i < chunks; ++i) m = fmaxf(m, a.stats[3 * (first + i * stride)]);
-    for (int i = 0; i < chunks; ++i) {
+    for (int i = threadIdx.x & 63; i < chunks; i += 64) m = fmaxf(m, a.stats[3 * (first + i * stride)]);
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    for (int i = threadIdx.x & 63; i < chunks; i += 64) {
         const float* s = a.stats + 3 * (first + i * stride);
         j = fmaxf(j, s[1] + (s[0] - m));
     }
+#pragma unroll
+    for (int k = 32; k >= 1; k >>= 1) j = fmaxf(j, __shfl_xor(j, k));
     f32x4 sum = {};
     float l = 0.0f;
+#pragma unroll 4
     for (int i = part; i < chunks; i += PARTS) {
         const int64_t at = first + i * stride;
         const float by = a.stats[3 * at] - m;
@@ -378,10 +510,12 @@ __global__ __launch_bounds__(256) void attention8_join_kernel(Attn8Args a, int b
 
 // ---------------------------------------------------------------- host side --
 struct Plan8a {
-    int nt, wt;                         // 16 nt columns a wave, wt waves share out the tokens
+    int nt, wt;                         // few columns: 16 nt a wave, wt waves share out the tokens; wt = 0: many columns
+    int cols;                           // of a workgroup
     int blocks;                         // of columns
     int chunk, chunks;                  // tokens of a workgroup, and the most of them of a sequence
 };
+constexpr int kWideTiles = 2, kWideWaves = 4;
 static bool plan_attention8(int sequences, int heads, int group, int head_dim, int max_q, int64_t max_kv, Plan8a& p) {
     if (sequences < 0 || heads < 1 || heads > 65535 || group < 1 || group > 1024 || max_q < 0 || max_kv < 0 || max_kv > INT32_MAX - 65536 ||
         (head_dim != 64 && head_dim != 128))
@@ -389,11 +523,12 @@ static bool plan_attention8(int sequences, int heads, int group, int head_dim, i
     const int64_t columns = (int64_t)max_q * group;
     if (columns > INT32_MAX / 2) return false;
     p.nt = columns <= 16 ? 1 : 2;
-    p.wt = columns <= 32 ? 4 : 1;
-    const int cols = 16 * p.nt * (4 / p.wt);
+    p.wt = columns <= 32 ? 4 : columns <= 64 ? 2 : 0;
+    p.cols = p.wt ? 16 * p.nt * (4 / p.wt) : 16 * kWideTiles * kWideWaves;
+    const int cols = p.cols;
     const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols), units = (int64_t)sequences * heads * blocks;
     // chunks: about eight workgroups for each CU, of 128 tokens at least for each wave
-    const int64_t least = 128 * p.wt, want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, units));
+    const int64_t least = 128 * std::max(p.wt, 1), want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, units));
     int64_t chunk = std::max<int64_t>(least, ((max_kv + want - 1) / want + 31) / 32 * 32);
     p.chunk = (int)chunk;
     const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
@@ -450,12 +585,14 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
         using T = decltype(z);
         auto run = [&](auto d) {
             constexpr int D = decltype(d)::value;
-            if (p.wt == 4 && p.nt == 1) hipLaunchKernelGGL((attention8_kernel<T, D, 1, 4>), grid, dim3(256), 0, stream, a);
-            else if (p.wt == 4) hipLaunchKernelGGL((attention8_kernel<T, D, 2, 4>), grid, dim3(256), 0, stream, a);
-            else hipLaunchKernelGGL((attention8_kernel<T, D, 2, 1>), grid, dim3(256), 0, stream, a);
+            auto few = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+            if (p.wt == 4 && p.nt == 1) few(attention8_kernel<T, D, 1, 4>);
+            else if (p.wt == 4) few(attention8_kernel<T, D, 2, 4>);
+            else if (p.wt == 2) few(attention8_kernel<T, D, 2, 2>);
+            else hipLaunchKernelGGL((attention8_wide_kernel<T, D, kWideTiles, kWideWaves>), grid, dim3(64 * kWideWaves), 0, stream, a);
             if (p.chunks > 1)
                 hipLaunchKernelGGL((attention8_join_kernel<T, D>), dim3((unsigned)(sequences * cache->heads) * (unsigned)(max_q * group)),
-                                   dim3(256), 0, stream, a, 16 * p.nt * (4 / p.wt));
+                                   dim3(256), 0, stream, a, p.cols);
         };
         if (cache->head_dim == 64) run(std::integral_constant<int, 64>{});
         else run(std::integral_constant<int, 128>{});

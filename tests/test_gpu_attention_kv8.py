@@ -201,6 +201,21 @@ def test_scores_of_any_size(dtype):
         assert (o[b] - want).abs().max() <= size * (2.0 ** -11 + 300 * 2.0 ** -23) + so.UNIT[dtype] * 1.01 * want.abs().max() + 1e-7, b
 
 
+def test_smallest_queries_and_keys():
+    """Scales whose product leaves fp32's range: scores of nothing, and hidden tokens stay hidden."""
+    def change(kv):
+        kv[0][0].zero_()
+        kv[1][0].mul_(1e-36)
+        kv[1][1].mul_(1e-30)
+        kv[1][1][60:].mul_(1e-8)
+    t = Case([90, 90], 1, 64, 32, torch.bfloat16, change=change)
+    counts = [90, 40]
+    q = t.queries(counts, 2)
+    q[:60] *= 1e-38
+    q[100:] = 2.0 ** -133
+    t.check(q, counts, t.run(q, counts))
+
+
 def test_strides_streams_workspace_and_graph():
     m = mq()
     t = Case([1500, 40, 700], 2, 128, 64, torch.bfloat16)
