@@ -50,6 +50,7 @@ struct Attn8Args {
     float scale;                        // times log2(e)
     int64_t max_kv;
     int chunk, chunks;                  // tokens that a workgroup takes, and chunks of the longest sequence
+    const int2* order;                  // sequence and block of columns of each workgroup, or null
     float* part;                        // of each sequence, key head, chunk and column: O[D], then m, J, l in `stats`
     float* stats;
 };
@@ -154,7 +155,9 @@ struct Columns8 {
         most = __builtin_amdgcn_readfirstlane(most);
     }
 
-    // One block of 32 tokens: key(t, s) and value(i) give the operands of its two tiles of tokens, and of its channels.
+    // One block of 32 tokens: key(t, s) and value(i) give the operands of its two tiles of tokens, and of its channels.  A block
+    // that no page holds (ve < 0) is seen by none; it is not left out, as a branch around the products makes the compiler
+    // copy the accumulators.
     template <typename K, typename V>
     __device__ __forceinline__ void take(int block, int ke, int ve, K&& key, V&& value) {
         const int quarter = (threadIdx.x & 63) >> 4;
@@ -167,66 +170,87 @@ struct Columns8 {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][i], s[n][t], 0, 0, 0);
             }
+        // the two products and what is between them each load their own operands: loaded ahead of that they cost registers, and with
+        // them a wave (8 contexts of 4096 tokens by 2048 queries 1110 us, 880)
+        __builtin_amdgcn_sched_barrier(0);
         const float ev = (float)(ve - 127);
-        f16x8 w[NT];
+        float c[NT], e[NT];
+        bool moves = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float c = fminf(fmaxf(ldexpf(slope[n], ke - 127), FLT_MIN), FLT_MAX);   // not 0: hidden scores stay -infinity
-            if ((block + 1) * kBlockTokens > least) {
-                const int left = sees[n] - block * kBlockTokens - 4 * quarter;
+            c[n] = fminf(fmaxf(ldexpf(slope[n], ke - 127), FLT_MIN), FLT_MAX);  // not 0: hidden scores stay -infinity
+            if ((block + 1) * kBlockTokens > least || ve < 0) {
+                const int left = ve < 0 ? 0 : sees[n] - block * kBlockTokens - 4 * quarter;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (16 * t + r >= left) s[n][t][r] = -INFINITY;
             }
-            // Scores as they are usual: the product less m and the weights' exponent in one operation, and p from w.  Not so where
-            // a maximum moves, where m passes 2^20 (m is a rounded product: an exact one may differ from it by more than any
-            // weight allows), and where w may lose what p still has.
-            float e = ev - jj[n] + kLift, from_m = e - m[n];
-            float y[8], high = -INFINITY;
+            e[n] = ev - jj[n] + kLift;
+            float high = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                y[j] = __builtin_fmaf(s[n][j / 4][j % 4], c, from_m);
-                high = fmaxf(high, y[j]);
-            }
+            for (int j = 0; j < 8; ++j) high = fmaxf(high, s[n][j / 4][j % 4]);
             // p <= 2^kSlack, w <= 2^(kSlack + kLift)
-            if (__ballot(high > kSlack + fminf(e, kLift) || !(fabsf(m[n]) < 0x1p20f) || e < -60.0f)) {
-                float top = -INFINITY;
+            moves |= rounded_product(high, c[n]) - m[n] > kSlack + fminf(kLift - e[n], 0.0f);
+        }
+        if (__ballot(moves)) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    y[j] = rounded_product(s[n][j / 4][j % 4], c);
-                    top = fmaxf(top, y[j]);
-                }
-                top = column_max(top);
-                const float was = m[n];
-                if (top > was + kSlack || ceilf(top - was) + ev > jj[n] + kSlack) {
-                    m[n] = fmaxf(was, ceilf(top));
-                    const float old = jj[n] + (was - m[n]);     // J of what O holds, by the new m
-                    jj[n] = fmaxf(fmaxf(old, ceilf(top - m[n]) + ev), kNone);
-                    l[n] *= __builtin_amdgcn_exp2f(was - m[n]);
-                    const float by = __builtin_amdgcn_exp2f(old - jj[n]);
+            for (int n = 0; n < NT; ++n) {
+                float high = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < TILES; ++i) o[i][n] *= by;
-                }
-                const int by = (int)fminf(ev - jj[n] + kLift, 1000.0f);
+                for (int j = 0; j < 8; ++j) high = fmaxf(high, s[n][j / 4][j % 4]);
+                const float top = rounded_product(column_max(high), c[n]), was = m[n];
+                const bool up = top > was + kSlack || ceilf(top - was) + ev > jj[n] + kSlack;
+                m[n] = up ? fmaxf(was, ceilf(top)) : was;
+                const float old = jj[n] + (was - m[n]);     // J of what O holds, by the new m
+                jj[n] = up ? fmaxf(fmaxf(old, ceilf(top - m[n]) + ev), kNone) : old;
+                l[n] *= __builtin_amdgcn_exp2f(was - m[n]);
+                const float by = __builtin_amdgcn_exp2f(old - jj[n]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(y[j] - m[n]);
-                    l[n] += p;
-                    w[n][j] = (_Float16)ldexpf(p, by);
-                }
-            } else {
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(y[j]);
-                    sum += p;
-                    w[n][j] = (_Float16)p;
-                }
-                l[n] = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-e), l[n]);
+                for (int i = 0; i < TILES; ++i) o[i][n] *= by;
+                e[n] = ev - jj[n] + kLift;
             }
         }
+        // Scores as they are usual: the product less m and the weights' exponent in one operation, and p from w.  Not so in a
+        // column where m passes 2^20 (m is a rounded product: an exact one may differ from it by more than any weight
+        // allows), or where w may lose what p still has.
+        f16x8 w[NT];
+        auto usual = [&](int n) {
+            const float from = e[n] - m[n];
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][j / 4][j % 4], c[n], from));
+                sum += p;
+                w[n][j] = (_Float16)p;
+            }
+            l[n] = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-e[n]), l[n]);
+        };
+        auto is_far = [&](int n) { return !(fabsf(m[n]) < 0x1p20f) || e[n] < -60.0f; };
+        bool far = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) far |= is_far(n);
+        if (__ballot(far)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (is_far(n)) {
+                    const int by = (int)fminf(e[n], 1000.0f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(rounded_product(s[n][j / 4][j % 4], c[n]) - m[n]);
+                        l[n] += p;
+                        w[n][j] = (_Float16)ldexpf(p, by);
+                    }
+                } else {
+                    usual(n);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) usual(n);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < TILES; ++i) {
             const f16x8 v = value(i);
@@ -244,40 +268,57 @@ struct Columns8 {
     }
 };
 
-// Four channels ch .. of column c's result, as values, or where chunks share the column as sums.
+// Where a column's result goes: as values, or where chunks share the column as sums.
 template <typename T, int D>
-__device__ __forceinline__ void store_column8(const Attn8Args& a, const Sequence8& seq, int head, int c, int ch, f32x4 sum, float m, float j,
-                                              float l, bool direct) {
-    if (direct) {
+struct Target8 {
+    T* out;
+    float *sum, *stat;
+    __device__ __forceinline__ Target8(const Attn8Args& a, const Sequence8& seq, int b, int head, int c, bool direct) {
+        out = nullptr;
+        sum = stat = nullptr;
         const int64_t row = (int64_t)seq.first + c / a.group;
         if (row < 0 || row >= a.tokens) return;
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        f32x4 y;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = l == 0.0f ? 0.0f : ldexpf(sum[r] / l, (int)fmaxf(j - kLift, -1000.0f));
-        *reinterpret_cast<t4*>(static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head + ch) =
-            __builtin_convertvector(y, t4);
-    } else {
-        const int64_t at = ((int64_t)blockIdx.x * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
-        *reinterpret_cast<f32x4*>(a.part + at * D + ch) = sum;
-        if (ch == 0) {
-            a.stats[3 * at] = m;
-            a.stats[3 * at + 1] = j;
-            a.stats[3 * at + 2] = l;
+        if (direct) {
+            out = static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head;
+        } else {
+            const int64_t at = (((int64_t)b * a.c.heads + head) * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
+            sum = a.part + at * D;
+            stat = a.stats + 3 * at;
         }
     }
-}
+    // four channels ch ..
+    __device__ __forceinline__ void store(int ch, f32x4 o, float m, float j, float l) const {
+        if (out) {
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            f32x4 y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = l == 0.0f ? 0.0f : ldexpf(o[r] / l, (int)fmaxf(j - kLift, -1000.0f));
+            *reinterpret_cast<t4*>(out + ch) = __builtin_convertvector(y, t4);
+        } else if (sum) {
+            *reinterpret_cast<f32x4*>(sum + ch) = o;
+            if (ch == 0) {
+                stat[0] = m;
+                stat[1] = j;
+                stat[2] = l;
+            }
+        }
+    }
+};
 
 // What a workgroup takes: `cols` columns of a sequence and key head, and a chunk of the tokens that they see.
 struct Part8 {
     int b, head, first_col, columns, chunks, from, until;
     bool empty;
     __device__ __forceinline__ Part8(const Attn8Args& a, int cols) {
-        b = blockIdx.x / a.c.heads;
+        const int unit = blockIdx.x / a.c.heads;
         head = blockIdx.x % a.c.heads;
+        const int2 item = a.order ? a.order[unit] : make_int2(unit, (int)(gridDim.y - 1 - blockIdx.y));     // the longest first
+        b = item.x;
+        empty = b < 0;
+        if (empty) return;
         const Sequence8 seq(a, b);
         columns = seq.queries * a.group;
-        first_col = (int)(gridDim.y - 1 - blockIdx.y) * cols;               // the longest first
+        first_col = item.y * cols;
         empty = first_col >= columns;
         if (empty) return;
         const int seen = (int)seq.seen(a, (min(first_col + cols, columns) - 1) / a.group);
@@ -287,6 +328,48 @@ struct Part8 {
         until = min(from + a.chunk, seen);
     }
 };
+
+// Blocks of `cols` columns of all sequences, those that see the most tokens first (of the same 1024th in any order): the last
+// ones to begin are then the shortest.  `most` entries; those behind the last block are -1.
+__global__ __launch_bounds__(1024) void attention8_order_kernel(Attn8Args a, int sequences, int cols, int most, int2* __restrict__ order) {
+    __shared__ uint32_t first[1024], sums[16];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    first[t] = 0;
+    __syncthreads();
+    auto for_blocks = [&](auto&& f) {
+        for (int b = wave; b < sequences; b += 16) {
+            const Sequence8 seq(a, b);
+            const int columns = seq.queries * a.group;
+            for (int k = lane; k * cols < columns; k += 64) {
+                const int64_t seen = seq.seen(a, (min((k + 1) * cols, columns) - 1) / a.group);
+                f(b, k, 1023 - (int)(seen * 1024 / (a.max_kv + 1)));
+            }
+        }
+    };
+    for_blocks([&](int, int, int bin) { atomicAdd(&first[bin], 1u); });
+    __syncthreads();
+    const uint32_t mine = first[t];
+    uint32_t v = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t o = __shfl_up(v, m);
+        if (lane >= m) v += o;
+    }
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    uint32_t all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) v += sums[w];
+        all += sums[w];
+    }
+    first[t] = v - mine;
+    __syncthreads();
+    for_blocks([&](int b, int k, int bin) {
+        const uint32_t at = atomicAdd(&first[bin], 1u);
+        if (at < (uint32_t)most) order[at] = make_int2(b, k);
+    });
+    for (int i = (int)all + t; i < most; i += 1024) order[i] = make_int2(-1, 0);
+}
 
 // Few columns: the waves share out the tokens (WT of them; blocks in turn), 4 / WT take 16 NT columns of their own.  Codes go
 // from memory to registers, a block ahead.
@@ -317,9 +400,8 @@ __global__ __launch_bounds__(256, 2) void attention8_kernel(Attn8Args a) {
         x.ve = row < 0 ? -1 : a.c.ve[at / kBlockTokens];
     };
     auto take = [&](const Block& x, int block) {
-        if (__builtin_amdgcn_readfirstlane(x.ve) < 0) return;
         auto half = [](const uint4 p, int h) { return h ? operand8(p.z, p.w) : operand8(p.x, p.y); };
-        cols.take(block, x.ke, x.ve, [&](int t, int s) { return half(x.k[t * (PIECES / 2) + s / 2], s % 2); },
+        cols.take(block, x.ke, __builtin_amdgcn_readfirstlane(x.ve), [&](int t, int s) { return half(x.k[t * (PIECES / 2) + s / 2], s % 2); },
                   [&](int i) { return half(x.v[i / 2], i % 2); });
     };
     const int first_block = part.from / kBlockTokens + wt;
@@ -364,15 +446,15 @@ __global__ __launch_bounds__(256, 2) void attention8_kernel(Attn8Args a) {
             ll += stat[w0 + w][cc][2] * __builtin_amdgcn_exp2f(by);
             sum += *reinterpret_cast<const f32x4*>(&sums[w0 + w][cc][ch]) * __builtin_amdgcn_exp2f(stat[w0 + w][cc][1] + by - j);
         }
-        store_column8<T, D>(a, seq, part.head, part.first_col + c, ch, sum, mm, j, ll, part.chunks == 1);
+        Target8<T, D>(a, seq, part.b, part.head, part.first_col + c, part.chunks == 1).store(ch, sum, mm, j, ll);
     }
 }
 
 // Many columns: each wave takes 16 NT of them and all tokens.  A stage of 4096 / D tokens is turned to fp16 once, a share by each
-// wave, and lies in LDS in operand order, in two slots: while one is used the next is written and the one after is on its way
-// from memory.  One barrier a stage.
+// wave, and lies in LDS in operand order, in two slots: while one is used the next is on its way from memory, to be written
+// after it.  One barrier a stage.
 template <typename T, int D, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void attention8_wide_kernel(Attn8Args a) {
+__global__ __launch_bounds__(64 * WAVES, 3) void attention8_wide_kernel(Attn8Args a) {
     constexpr int COLS = 16 * NT, PIECES = D / 32, TILES = D / 16, STEPS = D / 32;
     constexpr int BLOCKS = 128 / D, LOADS = 8 / WAVES;      // of a stage; pieces of 1 KB of codes of a wave and stage
     __shared__ __attribute__((aligned(16))) f16x8 staged[2][BLOCKS][4 * PIECES][64];    // keys' steps by tile, values' tiles
@@ -414,43 +496,43 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention8_wide_kernel(Attn8Arg
             staged[slot][b][2 * r + 1][lane] = operand8(x.p[i].z, x.p[i].w);
         }
     };
-    auto take = [&](const Stage& x, int block, int slot) {
+    static_assert(2 * STEPS == 2 * PIECES && TILES == 2 * PIECES, "as many operands of keys as of values");
+    Stage x;
+    if (first < end) {
+        load(x, first);
+        write(x, 0);
+    }
+    int slot = 0, block = first;
+    for (; block < mine; block += BLOCKS) {
+        int ke[BLOCKS], ve[BLOCKS];
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-            if (block + b >= mine || __builtin_amdgcn_readfirstlane(x.ve[b]) < 0) continue;
-            cols.take(block + b, x.ke[b], x.ve[b], [&](int t, int s) { return staged[slot][b][t * STEPS + s][lane]; },
-                      [&](int i) { return staged[slot][b][2 * PIECES + i][lane]; });
+            ke[b] = x.ke[b];
+            ve[b] = __builtin_amdgcn_readfirstlane(x.ve[b]);
         }
-    };
-    static_assert(2 * STEPS == 2 * PIECES && TILES == 2 * PIECES, "as many operands of keys as of values");
-    Stage x0, x1;
-    if (first < end) {
-        load(x0, first);
-        write(x0, 0);
-        load(x1, first + BLOCKS);
+        __syncthreads();                                    // this stage is written, and the one before is read
+        load(x, block + BLOCKS);                            // (past the end: some page's, unused)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+            cols.take(block + b, ke[b], ve[b], [&](int t, int s) { return staged[slot][b][t * STEPS + s][lane]; },
+                      [&](int i) { return staged[slot][b][2 * PIECES + i][lane]; });
+        slot ^= 1;
+        write(x, slot);
     }
-    __syncthreads();
-    for (int block = first; block < end; block += 2 * BLOCKS) {
-        Stage x2;
-        write(x1, 1);
-        load(x2, block + 2 * BLOCKS);
-        take(x0, block, 0);
+    for (; block < end; block += BLOCKS) {                  // what only other waves' columns see
         __syncthreads();
-        write(x2, 0);
-        x0 = x2;
-        load(x2, block + 3 * BLOCKS);
-        take(x1, block + BLOCKS, 1);
-        x1 = x2;
-        __syncthreads();
+        load(x, block + BLOCKS);
+        slot ^= 1;
+        write(x, slot);
     }
     cols.sum_up();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int c = part.first_col + wave * COLS + 16 * n + col;
-        if (c < part.columns)
+        if (c >= part.columns) continue;
+        const Target8<T, D> to(a, seq, part.b, part.head, c, part.chunks == 1);
 #pragma unroll
-            for (int i = 0; i < TILES; ++i)
-                store_column8<T, D>(a, seq, part.head, c, 16 * i + 4 * quarter, cols.o[i][n], cols.m[n], cols.jj[n], cols.l[n], part.chunks == 1);
+        for (int i = 0; i < TILES; ++i) to.store(16 * i + 4 * quarter, cols.o[i][n], cols.m[n], cols.jj[n], cols.l[n]);
     }
 }
 
@@ -514,9 +596,10 @@ struct Plan8a {
     int cols;                           // of a workgroup
     int blocks;                         // of columns
     int chunk, chunks;                  // tokens of a workgroup, and the most of them of a sequence
+    int items;                          // entries of the order, 0 for none
 };
 constexpr int kWideTiles = 2, kWideWaves = 4;
-static bool plan_attention8(int sequences, int heads, int group, int head_dim, int max_q, int64_t max_kv, Plan8a& p) {
+static bool plan_attention8(int sequences, int tokens, int heads, int group, int head_dim, int max_q, int64_t max_kv, Plan8a& p) {
     if (sequences < 0 || heads < 1 || heads > 65535 || group < 1 || group > 1024 || max_q < 0 || max_kv < 0 || max_kv > INT32_MAX - 65536 ||
         (head_dim != 64 && head_dim != 128))
         return false;
@@ -526,17 +609,22 @@ static bool plan_attention8(int sequences, int heads, int group, int head_dim, i
     p.wt = columns <= 32 ? 4 : columns <= 64 ? 2 : 0;
     p.cols = p.wt ? 16 * p.nt * (4 / p.wt) : 16 * kWideTiles * kWideWaves;
     const int cols = p.cols;
-    const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols), units = (int64_t)sequences * heads * blocks;
+    const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols);
+    // many columns of several sequences: workgroups in order of their work, and none for blocks that are not there (prompts of
+    // 1025 to 1877 queries over 1025 to 4095 tokens 365 us, in order 240)
+    const int64_t items = p.wt == 0 && sequences > 1 ? std::min((int64_t)tokens * group / cols + sequences, sequences * blocks) : 0;
+    const int64_t units = (items ? items : sequences * blocks) * heads;
     // chunks: about eight workgroups for each CU, of 128 tokens at least for each wave
     const int64_t least = 128 * std::max(p.wt, 1), want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, units));
-    int64_t chunk = std::max<int64_t>(least, ((max_kv + want - 1) / want + 31) / 32 * 32);
-    p.chunk = (int)chunk;
+    const int64_t chunk = std::max<int64_t>(least, ((max_kv + want - 1) / want + 31) / 32 * 32);
     const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
-    if (blocks > 65535 || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256) ||
+    if ((!items && blocks > 65535) || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256) ||
         (chunks > 1 && !mq_host::launch_holds((int64_t)sequences * heads * columns, 256)))
         return false;
+    p.chunk = (int)chunk;
     p.blocks = (int)blocks;
     p.chunks = (int)chunks;
+    p.items = (int)items;
     return true;
 }
 
@@ -544,14 +632,16 @@ static bool plan_attention8(int sequences, int heads, int group, int head_dim, i
 
 using namespace mq;
 
+// The order, then the chunks' sums and what belongs to them.
+static size_t order_bytes(const Plan8a& p) { return ((size_t)p.items * sizeof(int2) + 15) / 16 * 16; }
 static size_t workspace_of(const Plan8a& p, int sequences, int heads, int group, int head_dim, int max_q) {
-    return p.chunks == 1 ? 0 : (size_t)sequences * heads * p.chunks * ((size_t)max_q * group) * (head_dim + 3) * sizeof(float) + 16;
+    return order_bytes(p) + (p.chunks == 1 ? 0 : (size_t)sequences * heads * p.chunks * ((size_t)max_q * group) * (head_dim + 3) * sizeof(float));
 }
 
 extern "C" size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group, int head_dim, int max_q,
                                                   int64_t max_kv) {
     Plan8a p;
-    if (tokens < 0 || !plan_attention8(sequences, heads, group, head_dim, max_q, max_kv, p)) return 0;
+    if (tokens < 0 || !plan_attention8(sequences, tokens, heads, group, head_dim, max_q, max_kv, p)) return 0;
     return workspace_of(p, sequences, heads, group, head_dim, max_q);
 }
 
@@ -567,7 +657,7 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
         if (s < 0 || s % 8 != 0) return MQ_ERR_UNSUPPORTED_SHAPE;
     Plan8a p;
     if (max_kv > (int64_t)table_pages * cache->page_size ||
-        !plan_attention8(sequences, cache->heads, group, cache->head_dim, cu_q ? max_q : std::min(max_q, 1), max_kv, p))
+        !plan_attention8(sequences, tokens, cache->heads, group, cache->head_dim, cu_q ? max_q : std::min(max_q, 1), max_kv, p))
         return MQ_ERR_UNSUPPORTED_SHAPE;
     if (tokens == 0 || sequences == 0 || max_q == 0) return MQ_OK;
     if (!Q || !O || !kv_lens || (!page_table && max_kv > 0)) return MQ_ERR_INVALID_ARG;
@@ -578,9 +668,15 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
     const size_t need = workspace_of(p, sequences, cache->heads, group, cache->head_dim, max_q);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     Attn8Args a{device_cache8(cache), Q, O, q_token, q_head, o_token, o_head, page_table, kv_lens, cu_q, table_pages, tokens, group, max_q,
-                causal != 0, scale * kLog2e, max_kv, p.chunk, p.chunks, static_cast<float*>(workspace), nullptr};
+                causal != 0, scale * kLog2e, max_kv, p.chunk, p.chunks, nullptr, nullptr, nullptr};
+    int2* order = static_cast<int2*>(workspace);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + order_bytes(p));
     a.stats = a.part + (size_t)sequences * cache->heads * p.chunks * ((size_t)max_q * group) * cache->head_dim;
-    const dim3 grid(sequences * cache->heads, p.blocks, p.chunks);
+    const dim3 grid(p.items ? p.items * cache->heads : sequences * cache->heads, p.items ? 1 : p.blocks, p.chunks);
+    if (p.items) {
+        hipLaunchKernelGGL(attention8_order_kernel, dim3(1), dim3(1024), 0, stream, a, sequences, p.cols, p.items, order);
+        a.order = order;
+    }
     return mq_host::with_half_type(type, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto d) {
