@@ -98,8 +98,8 @@ def starts(counts):
 def attention_error(q, k, v, n8, scale, dtype, o, ev):
     """A bound of the attention's error for one sequence (all queries see at least one token), from its roundings.
     n8: the values' codes, ev their exponents by token [n, H]:
-    each weight in fp16, half a step of 2^-11 relative, or 2^-25 where it is below fp16's normal range, the largest
-    product of weight and scale being at least 2^6 there;
+    each weight in fp16, half a step of 2^-11 relative (fp16 calls: twice, 2^-22 and a little for the first rest's own), or
+    2^-25 where it is below fp16's normal range, the largest product of weight and scale being at least 2^6 there;
     scores in fp32: D products, their scaling and the exponential, whose error is a relative one of the weight above
     and below; sums of n in fp32; the result's own rounding."""
     n, _, d = k.shape
@@ -108,4 +108,4 @@ def attention_error(q, k, v, n8, scale, dtype, o, ev):
     mass = (q.double().abs().sum(-1).max() * torch.nan_to_num(k).abs().max()).item() * scale
     score = (d + 8) * 2.0 ** -24 * mass + 2.0 ** -22
     lost = n * torch.nan_to_num(n8).abs().max().item() * 2.0 ** -25 * 2.0 ** -6 * torch.exp2(ev).max().item()
-    return (2.0 ** -11 * 1.01 + 2 * score + 2 * (n + 8) * 2.0 ** -24) * size + lost + UNIT[dtype] * o.abs() * 1.01 + TINY[dtype]
+    return ((2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -21) * 1.01 + 2 * score + 2 * (n + 8) * 2.0 ** -24) * size + lost + UNIT[dtype] * o.abs() * 1.01 + TINY[dtype]
