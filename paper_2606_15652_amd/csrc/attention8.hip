@@ -101,8 +101,8 @@ template <typename T, int D, int NT>
 struct Columns8 {
     static constexpr int STEPS = D / 32, TILES = D / 16;    // of 32 channels of keys, of 16 channels of values
     // fp16 results show one rounding of the weights to fp16 (2.9e-4 of their norm off, 2.1e-4 of it their own rounding): the rest
-    // of a weight is a second operand (contexts in memory as before, prompts of 2047 queries 208 us instead of 200); in bf16 it
-    // does not show.
+    // of a weight is a second operand (single tokens take as long, four ragged prompts 289 us instead of 226); in bf16 it does not
+    // show.
     static constexpr int WEIGHTS = __is_same(T, _Float16) ? 2 : 1;
     f16x8 q[NT][STEPS];
     float slope[NT];                                        // of the scores, in log2
@@ -621,12 +621,17 @@ static bool plan_attention8(int sequences, int tokens, int heads, int group, int
     const int cols = p.cols;
     const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols);
     // many columns of several sequences: workgroups in order of their work, and none for blocks that are not there (prompts of
-    // 1025 to 1877 queries over 1025 to 4095 tokens 365 us, in order 240)
+    // 1025 to 1877 queries over 1025 to 4095 tokens 365 us, in order 211)
     const int64_t items = p.wt == 0 && sequences > 1 ? std::min((int64_t)tokens * group / cols + sequences, sequences * blocks) : 0;
     const int64_t units = (items ? items : sequences * blocks) * heads;
-    // chunks: about eight workgroups for each CU, of 128 tokens at least for each wave
-    const int64_t least = 128 * std::max(p.wt, 1), want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, units));
-    const int64_t chunk = std::max<int64_t>(least, ((max_kv + want - 1) / want + 31) / 32 * 32);
+    // Chunks: as many as there are CUs for one query and little more, two or three a CU for more columns (8 contexts of 8192
+    // tokens by 4 columns: 256 workgroups 32.7 us, 512 31.6, 1024 33.9; 32 of 2048 with heads of 64: 15.3, then 19.6, as 4 of it are
+    // the join's; 8 of 8192 by 64 columns 57, 50 and 62; by 256 columns 172, 134, 137, and 768 of them 124), of 256 tokens at
+    // least for each wave, or 128; where there are enough without, single tokens take 2048 at a time, as contexts may be
+    // ragged (64 of 257 to 8191 tokens: in chunks of 2048 114 us, of 4096 118; 128 of 1000 tokens whole 51, in halves 64).
+    const int64_t least = p.wt ? 256 * p.wt / p.nt : 128, want = (p.wt ? 256 * p.nt : 768) / std::max<int64_t>(1, units);
+    const int64_t share = want > 1 ? (max_kv + want - 1) / want : p.wt ? std::min<int64_t>(max_kv, 2048) : max_kv;
+    const int64_t chunk = std::max<int64_t>(least, (share + 31) / 32 * 32);
     const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
     if ((!items && blocks > 65535) || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256) ||
         (chunks > 1 && !mq_host::launch_holds((int64_t)sequences * heads * columns, 256)))
