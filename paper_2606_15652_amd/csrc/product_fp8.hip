@@ -75,6 +75,23 @@ __device__ __forceinline__ void store_row_f8(const ProductF8Args& a, int m, int 
     }
 }
 
+// 16 rows of a wave's 64 channels n0 .. where rows of Y are not 16-byte aligned: through LDS, so that a store takes 64 neighbours
+// (131 rows of 8191 channels: one value a lane and 16 rows a store 22-24 us, so 18).
+template <typename T>
+__device__ __forceinline__ void store_block_f8(const ProductF8Args& a, int m0, int n0, const f32x4 (&sum)[4], float (*lds)[68]) {
+    const int lane = threadIdx.x & 63, lrow = lane & 15, lq = lane >> 4, n = n0 + lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(&lds[lrow][16 * lq + 4 * i]) = sum[i];
+    wave_sync();
+    if (n < a.N) {
+        const float bias = a.bias ? (float)static_cast<const T*>(a.bias)[n] : 0.0f;
+        T* y = static_cast<T*>(a.Y) + m0 * a.ldy + n;
+        const int rows = min(16, a.M - m0);
+        for (int r = 0; r < rows; ++r) y[r * a.ldy] = (T)(a.bias ? lds[r][lane] + bias : lds[r][lane]);
+    }
+    wave_sync();
+}
+
 // --------------------------------------------------------------------------
 // Tiled kernel: WM x WN waves, each 16 MI rows of X by one block of 64 channels.
 // --------------------------------------------------------------------------
@@ -186,6 +203,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_f8_tiled_kernel(Produ
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // nothing may write LDS after the workgroup has gone
 
     const int n = (b0 + wn) * kBlockF8 + 16 * lq;
+    if (!SPLIT && !a.y16) {
+        __syncthreads();                                    // the slots are everybody's, and their last loads write zeros
+        static_assert(sizeof(L.x) + sizeof(L.w) >= NW * 16 * 68 * sizeof(float), "16 rows of each wave");
+        float(*rows16)[68] = reinterpret_cast<float(*)[68]>(&L) + 16 * wave;
+#pragma unroll
+        for (int j = 0; j < MI; ++j) {
+            const int m = m0 + wm * 16 * MI + 16 * j;
+            const f32x4 sum[4] = {acc[0][j], acc[1][j], acc[2][j], acc[3][j]};
+            if (m < a.M) store_block_f8<T>(a, m, n - 16 * lq, sum, rows16);
+        }
+        return;
+    }
     if (n >= a.N) return;
 #pragma unroll
     for (int j = 0; j < MI; ++j) {
@@ -431,16 +460,24 @@ __global__ __launch_bounds__(256) void unpack_weight_f8_kernel(const uint8_t* __
 static bool shape_f8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
 
 // ---------------------------------------------------------------- host side --
+// Which kernel takes a product.  Up to 16 rows, and up to 32 where the weight is small, the streaming kernel (5000 -> 8191 at 17 rows
+// 12.2 us, 64 x 64 tiles 16; 4096 -> 14336 14.5 and 14.6).  Beyond, of four tiles and one, two or four splits of K the one with
+// the least estimated time: groups by the time of one (a workgroup alone on its CU waits for memory; more of them
+// share it), or W at the rate that the tiles reach, whichever is longer, and what writing and joining a split's sums
+// takes.  128 x 128 has four slots where there is no more than one workgroup a CU, and two where two share it (8192 ->
+// 8192 at 512 rows 43 us instead of 57, at 1024 rows 87 instead of 76).  Measured (us): 8192 -> 8192 at 64 rows by 64 x 64 in two
+// splits 20, unsplit 25; at 200 rows by 128 x 64 31, 64 x 64 35; at 300 by 128 x 128 38, 128 x 64 49; 4096 -> 4096 at
+// 4096 by 256 x 256 68, 128 x 128 75; 14336 -> 4096 at 131 rows by 128 x 128 in four splits 28, 128 x 64 30.
 struct TileF8 {
     int rows, cols;
     double alone, share;                // us of a stage: one workgroup a CU, and of each of several
     bool splits;
 };
 constexpr TileF8 kTilesF8[4] = {
-    {64, 64, 0.26, 0.25, true},
-    {128, 64, 0.45, 0.345, true},
-    {128, 128, 0.95, 0.60, false},
-    {256, 256, 1.60, 1.60, false},
+    {64, 64, 0.36, 0.28, true},
+    {128, 64, 0.45, 0.38, true},
+    {128, 128, 0.60, 0.59, true},
+    {256, 256, 1.90, 1.90, false},
 };
 struct PlanF8 {
     int rows, cols;                     // of a workgroup's tile; cols of the streaming kernel: 16 P
@@ -462,7 +499,7 @@ static PlanF8 plan_f8(int M, int N, int K) {
             const int64_t a_cu = (groups + 255) / 256;
             const int per = (stages + splits - 1) / splits;
             const double compute = per * std::max(t.alone, a_cu * t.share), memory = (double)N * K / 4.6e6;
-            const double join = splits == 1 ? 0.0 : 7.0 + (double)M * N * 4 * (splits + 1) / 5.0e6;
+            const double join = splits == 1 ? 0.0 : 6.0 + (double)M * N * 4 * (splits + 1) / 5.0e6;
             const double us = std::max(compute, memory) + join;
             if (least == 0.0 || us < least) {
                 least = us;
@@ -583,7 +620,9 @@ extern "C" mq_status mq_gemm_fp8(int M, int N, int K, const void* Xq, int ldx, c
         } else if (p.rows == 256) {
             tile(product_f8_tiled_kernel<T, 2, 4, 8, 2, false>, 512);
         } else if (p.cols == 128) {
-            tile(product_f8_tiled_kernel<T, 4, 2, 2, 2, false>, 512);
+            if (p.splits > 1) tile(product_f8_tiled_kernel<T, 4, 2, 2, 4, true>, 512);
+            else if (groups <= 256) tile(product_f8_tiled_kernel<T, 4, 2, 2, 4, false>, 512);
+            else tile(product_f8_tiled_kernel<T, 4, 2, 2, 2, false>, 512);
         } else if (p.rows == 128) {
             if (p.splits > 1) tile(product_f8_tiled_kernel<T, 4, 1, 2, 3, true>, 256);
             else tile(product_f8_tiled_kernel<T, 4, 1, 2, 3, false>, 256);
