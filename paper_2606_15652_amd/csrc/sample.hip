@@ -93,54 +93,85 @@ __device__ __forceinline__ int bin_of(double d) { return d < kBins / kBinsPerUni
 struct SampleLds {
     uint64_t sums[kBins];               // of the bins, then running, the bin's own among it
     uint32_t counts[kBins];
-    uint64_t part_sums[256];            // of a long bin's parts
-    uint32_t part_counts[256];
+    uint64_t part_sums[kThreads];       // of parts of the list, running; of a long bin's parts
+    uint32_t part_counts[kThreads];
+    uint32_t few_keys[64];              // one part of the list
+    int32_t few_at[64];
     uint32_t keys[kList];               // the list: larger first
     int32_t at[kList];
     uint64_t scan[kThreads / 64];
-    uint32_t listed, bounds[2];
+    uint32_t scan_counts[kThreads / 64];
+    uint32_t listed, few, bounds[2];
     int found, token, nan;
     uint64_t found_before, found_count, found_tokens, found_sum, found_weight;
     float best[kThreads / 64];
 };
 
-// The least float x (as its key) with before(x), which holds for all from there to the key `top`: 64 keys at a time, by
+// The least float x (as its key) with before(x), which holds for all from there to the key `top`: six bits of it at a time, by
 // every wave.
 template <typename F>
 __device__ __forceinline__ uint32_t least_key(uint32_t top, F&& before) {
     const uint32_t lane = threadIdx.x & 63;
-    uint64_t lo = order_key(-INFINITY), hi = (uint64_t)top + 1;     // the answer is in [lo, hi), and hi - 1 says yes
-    while (hi - lo > 1) {
-        const uint64_t step = (hi - lo + 63) / 64, k = lo + lane * step;
-        const uint64_t yes = __ballot(k < hi && before(value_of_key((uint32_t)k)));
-        const uint64_t no = yes ? (uint64_t)__builtin_ctzll(yes) : (hi - lo + step - 1) / step;     // lanes that say no
-        if (yes) hi = lo + no * step + 1;
-        if (no) lo += (no - 1) * step + 1;
+    uint32_t key = 0;
+#pragma unroll 1
+    for (int shift = 26; shift > -6; shift -= 6) {
+        // the first of 64 ranges of keys whose last one says yes (the last round: of 4 keys)
+        const int down = shift < 0 ? 0 : shift;
+        const uint32_t k = key + (lane << down) + ((1u << down) - 1u);
+        const uint64_t yes = __ballot((k >= top || k < key) || before(value_of_key(k)));
+        key += (uint32_t)__builtin_ctzll(yes) << down;
     }
-    return (uint32_t)(hi - 1);
+    return key;
 }
 
-// Inclusive running sums over the workgroup's threads, and the sum of all.
-__device__ __forceinline__ uint64_t scan_threads(SampleLds& L, uint64_t v, uint64_t& all) {
+// Inclusive running sums over the wave, by DPP: within rows of 16 lanes, then the rows' sums carried on.
+__device__ __forceinline__ void scan_wave(uint64_t& v, uint32_t& c) {
+    auto step = [&](auto ctrl, auto rows) {
+        auto from = [&](uint32_t x) {
+            return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, true);
+        };
+        const uint32_t lo = from((uint32_t)v), hi = from((uint32_t)(v >> 32)), n = from(c);
+        v += (uint64_t)hi << 32 | lo;
+        c += n;
+    };
+    constexpr std::integral_constant<int, 0xf> every{};
+    step(std::integral_constant<int, 0x111>{}, every);                              // row_shr:1, 2, 4, 8
+    step(std::integral_constant<int, 0x112>{}, every);
+    step(std::integral_constant<int, 0x114>{}, every);
+    step(std::integral_constant<int, 0x118>{}, every);
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}); // row_bcast:15, to rows 1 and 3
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}); // row_bcast:31, to rows 2 and 3
+}
+
+// Inclusive running sums (and numbers) over the workgroup's threads, and the sum (and number) of all.
+__device__ __forceinline__ void scan_threads(SampleLds& L, uint64_t& v, uint32_t& c, uint64_t& all, uint32_t& all_count) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const uint64_t o = (uint64_t)__shfl_up((unsigned long long)v, m);
-        if (lane >= m) v += o;
+    scan_wave(v, c);
+    __syncthreads();
+    if (lane == 63) {
+        L.scan[wave] = v;
+        L.scan_counts[wave] = c;
     }
     __syncthreads();
-    if (lane == 63) L.scan[wave] = v;
-    __syncthreads();
-    uint64_t before = 0;
     all = 0;
+    all_count = 0;
+    uint64_t before = 0;
+    uint32_t before_count = 0;
+#pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) {
-        if (w < wave) before += L.scan[w];
+        if (w == wave) {
+            before = all;
+            before_count = all_count;
+        }
         all += L.scan[w];
+        all_count += L.scan_counts[w];
     }
-    return v + before;
+    v += before;
+    c += before_count;
 }
 
-// f(v, i, m) for the m <= EACH logits v of the row at i(j), j < m: all of them, by all threads, some loads at a time.
+// f(v, i, E) for E logits v of the row at i(j), j < E, at a time: all of them, by all threads, AHEAD loads at once and the
+// next ones on their way meanwhile.  Where fewer are left the rest of v is -infinity, which is nothing to any of the passes.
 template <int AHEAD, typename T, typename F>
 __device__ __forceinline__ void for_parts(const T* x, int n, F&& f) {
     typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -148,22 +179,23 @@ __device__ __forceinline__ void for_parts(const T* x, int n, F&& f) {
     // up to the first 16-byte border one by one
     const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T)), body = (n - head) / per;
     const vec* v = reinterpret_cast<const vec*>(x + head);
-    int c = threadIdx.x;
-    for (; c + (AHEAD - 1) * kThreads < body; c += AHEAD * kThreads) {
-        vec y[AHEAD];
+    auto load = [&](vec (&y)[AHEAD], int c) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) y[a] = v[c + a * kThreads];
+        for (int a = 0; a < AHEAD; ++a) {
+            y[a] = (vec)(T)-INFINITY;
+            if (c + a * kThreads < body) y[a] = v[c + a * kThreads];
+        }
+    };
+    vec y[AHEAD], next[AHEAD];
+    load(y, threadIdx.x);
+    for (int c = threadIdx.x; c < body; c += AHEAD * kThreads) {
+        load(next, c + AHEAD * kThreads);
         float z[AHEAD * per];
 #pragma unroll
         for (int j = 0; j < AHEAD * per; ++j) z[j] = (float)y[j / per][j % per];
         f(z, [&](int j) { return head + (c + j / per * kThreads) * per + j % per; }, std::integral_constant<int, AHEAD * per>{});
-    }
-    for (; c < body; c += kThreads) {
-        const vec y = v[c];
-        float z[per];
 #pragma unroll
-        for (int j = 0; j < per; ++j) z[j] = (float)y[j];
-        f(z, [&](int j) { return head + c * per + j; }, std::integral_constant<int, per>{});
+        for (int a = 0; a < AHEAD; ++a) y[a] = next[a];
     }
     const int rest = n - body * per;                        // fewer than 2 per: one for each of the first threads
     if ((int)threadIdx.x < rest) {
@@ -178,6 +210,18 @@ __device__ __forceinline__ void for_row(const T* x, int n, F&& f) {
 #pragma unroll
         for (int j = 0; j < decltype(each)::value; ++j) f(v[j], at(j));
     });
+}
+
+// One step of a bitonic sort among a wave's lanes: element i and the one at i ^ j, in stage k.
+__device__ __forceinline__ void sort_step(uint32_t& key, int& at, int i, int j, int k) {
+    const uint32_t ok = (uint32_t)__shfl_xor((int)key, j);
+    const int oa = __shfl_xor(at, j);
+    const bool other_first = ok > key || (ok == key && oa < at);
+    // the lower of the pair keeps the first where the stage ascends, the upper one the second
+    if (other_first == (((i & j) == 0) == ((i & k) == 0))) {
+        key = ok;
+        at = oa;
+    }
 }
 
 // Sorts the list (keys descending, index ascending among equals): bitonic, a wave's 64 neighbours by their lanes, further
@@ -198,16 +242,7 @@ __device__ __forceinline__ void sort_list(SampleLds& L, int n) {
             uint32_t key = L.keys[i];
             int at = L.at[i];
             for (int k = first_stage; k <= last_stage; k <<= 1)
-                for (int j = min(k >> 1, most); j > 0; j >>= 1) {
-                    const uint32_t ok = (uint32_t)__shfl_xor((int)key, j);
-                    const int oa = __shfl_xor(at, j);
-                    const bool other_first = ok > key || (ok == key && oa < at);
-                    // the lower of the pair keeps the first where the stage ascends, the upper one the second
-                    if (other_first == (((i & j) == 0) == ((i & k) == 0))) {
-                        key = ok;
-                        at = oa;
-                    }
-                }
+                for (int j = min(k >> 1, most); j > 0; j >>= 1) sort_step(key, at, i, j, k);
             L.keys[i] = key;
             L.at[i] = at;
         }
@@ -247,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     // 1. the maximum, the two largest that this thread has seen, and whether there is a NaN
     float best = -INFINITY, second = -INFINITY;
     uint32_t bits = 0;
-    for_row<16 / sizeof(T)>(x, n, [&](float v, int) {
+    for_row<4>(x, n, [&](float v, int) {
         second = fmaxf(second, fminf(best, v));
         best = fmaxf(best, v);
         bits = max(bits, __float_as_uint(v) & 0x7FFFFFFFu);
@@ -291,203 +326,304 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 
     const uint32_t top = order_key(best);
     const uint64_t least = min_p > 0.0f ? (uint64_t)ceil((double)fminf(min_p, 1.0f) * (double)(1ull << kShift)) : 0;
-
-    // the tokens with logits lo <= x <= hi whose place above `shift` bits is `prefix`, sorted; false if they are more than kList
-    // (a token's place in the order: 32 bits of its logit, the larger the lower, and 20 of its index)
-    constexpr int BITS = 52;
-    auto place = [](float v, int i) { return (uint64_t)~order_key(v) << 20 | (uint64_t)i; };
-    auto make_list = [&](float lo, float hi, int shift, uint64_t prefix) {
-        __syncthreads();
-        if (t == 0) L.listed = 0;
-        __syncthreads();
-        for_parts<sizeof(T) == 4 ? 8 : 4>(x, n, [&](const auto& v, auto&& i, auto each) {
-            constexpr int E = decltype(each)::value;
-            static_assert(E <= 32, "a bit for each");
-            uint32_t hits = 0;
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (v[j] >= lo && v[j] <= hi && (shift == BITS || place(v[j], i(j)) >> shift == prefix)) hits |= 1u << j;
-            if (hits == 0) return;
-            uint32_t p = atomicAdd(&L.listed, (uint32_t)__popc(hits));
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (hits >> j & 1) {
-                    if (p < kList) {
-                        L.keys[p] = order_key(v[j]);
-                        L.at[p] = i(j);
-                    }
-                    ++p;
-                }
-        });
-        __syncthreads();
-        const uint32_t tokens = L.listed;
-        if (tokens > kList) return false;
-        sort_list(L, (int)tokens);
-        return true;
-    };
-    // The weights of the list's first m tokens, and their running sums from `before` on, four tokens a thread; the sum of all
-    // m, and of those that min_p keeps.
-    constexpr int EACH = kList / kThreads;
-    uint64_t w[EACH], runs[EACH];
-    auto weigh = [&](int m, uint64_t before, uint64_t& sum, uint64_t& kept) {
-        uint64_t mine = 0, keeps = 0;
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            const int i = t * EACH + j;
-            w[j] = i < m ? weight_of(row.distance(value_of_key(L.keys[i]))) : 0;
-            mine += w[j];
-            keeps += w[j] >= least ? w[j] : 0;
-        }
-        runs[0] = before + scan_threads(L, mine, sum) - mine + w[0];
-#pragma unroll
-        for (int j = 1; j < EACH; ++j) runs[j] = runs[j - 1] + w[j];
-        kept = sum;
-        if (least) scan_threads(L, keeps, kept);
-    };
-    // Of them the one at which the running sum passes `target` (or the one in place `index`): to L.token, L.found_weight, and the
-    // running sum with it to L.found_sum.
-    auto pick = [&](uint64_t target, int index) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < EACH; ++j)
-            if (index >= 0 ? t * EACH + j == index : runs[j] - w[j] <= target && target < runs[j]) {
-                L.token = L.at[t * EACH + j];
-                L.found_weight = w[j];
-                L.found_sum = runs[j];
-            }
-        __syncthreads();
-    };
     auto drawn = [&](uint64_t sum) { return u < 1.0f ? part_of<false>(fmaxf(u, 0.0f), sum) : sum - 1; };
     // the least beginning with a sum of top_p of it at least: it passes that less one
     auto cut = [&](uint64_t sum) { return max(part_of<true>(fmaxf(top_p, 0.0f), sum), (uint64_t)1) - 1; };
+    auto add = [](uint64_t& to, uint64_t w) { atomicAdd(reinterpret_cast<unsigned long long*>(&to), (unsigned long long)w); };
+    // a token's place in the order: 32 bits of its logit, the larger the lower, and 20 of its index
+    constexpr int BITS = 52;
+    auto place = [](float v, int i) { return (uint64_t)~order_key(v) << 20 | (uint64_t)i; };
     static_assert(kBins == 2 * kThreads, "two bins a thread");
-    uint64_t none;
 
-    // 2. few tokens down to the k-th.  The k-th largest of the threads' two largest logits is no more than the k-th of all, so
-    // its bin is the last in question.  Of logits in no order, k = 1000 of the 2048 are found among some 1130 tokens, 1536 among
-    // 2070; where they are more than the list holds, all are looked at below.
-    if (top_k > 0 && top_k <= 3 * kThreads / 2) {
-        const float slope = (float)fmin(row.slope * kBinsPerUnit, 1e30);
-        auto bin = [&](float v) { return v == best ? 0 : (int)fminf((best - v) * slope, (float)(kBins - 1)); };
-        for (float v : {first, second})
-            if (const int b = bin(v); b < kBins - 1) atomicAdd(&L.counts[b], 1u);
-        if (t == 0) L.found = -1;
-        __syncthreads();
-        const uint32_t c0 = L.counts[2 * t], c1 = L.counts[2 * t + 1];
-        const uint64_t down = scan_threads(L, (uint64_t)c0 + c1, none), k = (uint64_t)top_k;
-        if (down - c1 - c0 < k && k <= down) L.found = down - c1 >= k ? 2 * t : 2 * t + 1;
-        L.counts[2 * t] = L.counts[2 * t + 1] = 0;
-        __syncthreads();
-        const int last = L.found;
-        if (last >= 0) {
-            const uint32_t lo = least_key(top, [&](float v) { return bin(v) <= last; });
-            if (make_list(value_of_key(lo), best, BITS, 0)) {
-                uint64_t sum, kept;
-                weigh(top_k, 0, sum, kept);
-                if (top_p < 1.0f) {
-                    pick(cut(sum), -1);
-                    sum = L.found_sum;
-                }
-                sum = min(sum, kept);
-                pick(drawn(sum), -1);
-                if (t == 0) answer(L.token, (float)((double)L.found_weight / (double)sum));
-                return;
-            }
-        }
-    }
+    // The list: tokens in question, in any order, before which there are `before_count` with the sum `before`.  Thread t has
+    // its tokens t, t + 1024, ..: their weights, and in which of 1024 equal ranges they are (by key, and by index among equals).
+    constexpr int EACH = kList / kThreads;
+    uint64_t w[EACH], before = 0, before_count = 0;
+    uint32_t part[EACH];
+    bool all_listed = false, sorted = false;            // whether it has every token in question; whether it is in order
+    int in_list = -1;                                   // the bin that it holds
+    uint64_t sum = 0, kept = 0, count = 0;              // of all tokens in question, of those that min_p keeps; their number
 
-    // 3. counts and sums by bins; how many tokens min_p keeps does not matter, only their sum
-    uint64_t kept = 0;
-    for_row<sizeof(T) / 2>(x, n, [&](float v, int) {
-        const double d = row.distance(v);
-        const int b = bin_of(d);
-        if (b >= kBins) return;
-        const uint64_t w = weight_of(d);
-        if (w >= least) kept += w;
-        atomicAdd(&L.counts[b], 1u);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&L.sums[b]), (unsigned long long)w);
-    });
-    __syncthreads();
-    uint64_t sum, count;
-    {
-        const uint64_t s0 = L.sums[2 * t], s1 = L.sums[2 * t + 1];
-        const uint32_t c0 = L.counts[2 * t], c1 = L.counts[2 * t + 1];
-        const uint64_t run = scan_threads(L, s0 + s1, sum), runs = scan_threads(L, (uint64_t)c0 + c1, count);
-        scan_threads(L, kept, none);
-        kept = none;
-        L.sums[2 * t] = run - s1;
-        L.sums[2 * t + 1] = run;
-        L.counts[2 * t] = (uint32_t)(runs - c1);
-        L.counts[2 * t + 1] = (uint32_t)runs;
-        __syncthreads();
-    }
-
-    // in turn the k-th token, the end of top_p, the drawn token
-    int in_list = -1;                                   // the bin that the list holds
+    // Turn -1: the list of few tokens down to the k-th, or the sums by bins.  Then in turn the k-th token, the end of top_p, the drawn
+    // token.  (Every step has one place in the code: what a workgroup runs through once is bound by its loading.)
 #pragma unroll 1
-    for (int turn = 0; turn < 3; ++turn) {
+    for (int turn = -1; turn < 3; ++turn) {
         const bool by_count = turn == 0;
         if (by_count ? top_k <= 0 || (uint64_t)top_k >= count : turn == 1 && !(top_p < 1.0f)) continue;
         if (turn == 2 && least) sum = min(sum, kept);
-        const uint64_t target = by_count ? (uint64_t)top_k - 1 : turn == 1 ? cut(sum) : drawn(sum);
+        const uint64_t target = by_count ? (uint64_t)top_k - 1 : turn == 1 ? cut(sum) : turn == 2 ? drawn(sum) : 0;
+        int bin = -1;
         __syncthreads();
-        for (int b = 2 * t; b < 2 * t + 2; ++b) {
-            const uint64_t lo_s = b ? L.sums[b - 1] : 0, lo_c = b ? L.counts[b - 1] : 0;
-            if (by_count ? lo_c <= target && target < L.counts[b] : lo_s <= target && target < L.sums[b]) {
-                L.found = b;
-                L.found_before = lo_s;
-                L.found_count = lo_c;
-                L.found_tokens = L.counts[b] - lo_c;
+        if (t == 0) L.found = -1;
+        __syncthreads();
+        if (turn < 0 && top_k > 0 && top_k <= 3 * kThreads / 2) {
+            // The k-th largest of the threads' two largest logits is no more than the k-th of all, so its bin is the last in
+            // question.  Of logits in no order, k = 1000 of the 2048 are found among some 1130 tokens, 1536 among 2070; where
+            // they are more than the list holds, the sums by bins are taken.
+            for (float v : {first, second})
+                if (const int b = bin_of(row.distance(v)); b < kBins) atomicAdd(&L.counts[b], 1u);
+            __syncthreads();
+            const uint32_t c0 = L.counts[2 * t], c1 = L.counts[2 * t + 1], k = (uint32_t)top_k;
+            uint64_t zero = 0, none;
+            uint32_t down = c0 + c1, number;
+            scan_threads(L, zero, down, none, number);
+            if (down - c1 - c0 < k && k <= down) L.found = down - c1 >= k ? 2 * t : 2 * t + 1;
+            L.counts[2 * t] = L.counts[2 * t + 1] = 0;
+            __syncthreads();
+            bin = L.found;
+        } else if (turn >= 0 && !all_listed) {
+            for (int b = 2 * t; b < 2 * t + 2; ++b) {
+                const uint64_t lo_s = b ? L.sums[b - 1] : 0, lo_c = b ? L.counts[b - 1] : 0;
+                if (by_count ? lo_c <= target && target < L.counts[b] : lo_s <= target && target < L.sums[b]) {
+                    L.found = b;
+                    L.found_before = lo_s;
+                    L.found_count = lo_c;
+                }
             }
+            __syncthreads();
+            bin = L.found;
         }
-        __syncthreads();
-        const int bin = L.found;
-        uint64_t before = L.found_before, before_count = L.found_count, tokens = L.found_tokens;
-        if (in_list != bin) {
-            // its lowest logit, and the lowest of the bins before it: by the even waves and the odd ones
+        bool listed = false;
+        uint32_t key_lo = 0, key_hi = top;
+        if (bin >= 0 && bin != in_list) {
+            // the bin's lowest logit, and the lowest of the bins before it: by the even waves and the odd ones
             const int upto = bin - (wave & 1);
             const uint32_t key = upto >= 0 ? least_key(top, [&](float v) { return bin_of(row.distance(v)) <= upto; }) : top + 1;
             if (t == 0) L.bounds[0] = key;
             if (t == 64) L.bounds[1] = key;
             __syncthreads();
-            const float lo = value_of_key(L.bounds[0]), hi = value_of_key(L.bounds[1] - 1);
+            key_lo = L.bounds[0];
+            if (turn >= 0) {
+                key_hi = L.bounds[1] - 1;
+                before = L.found_before;
+                before_count = L.found_count;
+            }
+            const float lo = value_of_key(key_lo), hi = value_of_key(key_hi);
             uint64_t prefix = 0;
             int shift = BITS;                           // places with this prefix above `shift` bits are in question
-            while (tokens > kList) {                    // (each turn settles eight bits: places differ)
+            while (true) {
+                __syncthreads();
+                if (t == 0) L.listed = 0;
+                __syncthreads();
+                // A bit for each of 64 logits; those that are in question, one or two of the 64 in most rows, are read again (put
+                // down where they are met: 128 rows of 131071 53 us, so 45).
+                uint64_t hits = 0;
+                int bits = 0, from[4];
+                auto put = [&] {
+                    if (hits) {
+                        uint32_t p = atomicAdd(&L.listed, (uint32_t)__popcll(hits));
+                        do {
+                            const int j = __builtin_ctzll(hits);
+                            hits &= hits - 1;
+                            constexpr int per = 16 / sizeof(T);     // of a load, 16 of a part
+                            const int base = j < 32 ? j < 16 ? from[0] : from[1] : j < 48 ? from[2] : from[3];
+                            const int i = base + j % 16 / per * (kThreads * per) + j % per;
+                            if (p < kList) {
+                                L.keys[p] = order_key((float)x[i]);
+                                L.at[p] = i;
+                            }
+                            ++p;
+                        } while (hits);
+                    }
+                    bits = 0;
+                };
+                for_parts<sizeof(T)>(x, n, [&](const auto& v, auto&& i, auto each) {
+                    constexpr int E = decltype(each)::value;
+                    static_assert(E == 16 || E == 1, "16 logits, or one of those beside the 16-byte borders");
+                    uint32_t now = 0;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) now |= (uint32_t)((v[j] >= lo) & (v[j] <= hi)) << j;    // (no branches)
+                    if (shift < BITS && now) {
+                        for (uint32_t rest = now; rest; rest &= rest - 1)
+                            if (const int j = __builtin_ctz(rest); place((float)x[i(j)], i(j)) >> shift != prefix) now &= ~(1u << j);
+                    }
+                    hits |= (uint64_t)now << bits;
+                    (bits < 32 ? bits < 16 ? from[0] : from[1] : bits < 48 ? from[2] : from[3]) = i(0);
+                    bits += 16;
+                    if (bits == 64) put();
+                });
+                put();
+                __syncthreads();
+                listed = L.listed <= kList;
+                if (listed || turn < 0) break;
+                // more than the list holds: by parts of eight bits of their places, which all differ
                 const int next = max(shift - 8, 0);
                 __syncthreads();
-                if (t < 256) {
-                    L.part_sums[t] = 0;
-                    L.part_counts[t] = 0;
-                }
+                L.part_sums[t] = 0;
+                L.part_counts[t] = 0;
                 __syncthreads();
                 for_row<1>(x, n, [&](float v, int i) {
                     if (!(v >= lo && v <= hi) || place(v, i) >> shift != prefix) return;
-                    const int part = (int)(place(v, i) >> next) & ((1 << (shift - next)) - 1);
-                    atomicAdd(&L.part_counts[part], 1u);
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&L.part_sums[part]), (unsigned long long)weight_of(row.distance(v)));
+                    const int p = (int)(place(v, i) >> next) & ((1 << (shift - next)) - 1);
+                    atomicAdd(&L.part_counts[p], 1u);
+                    add(L.part_sums[p], weight_of(row.distance(v)));
                 });
                 __syncthreads();
-                const uint64_t ps = t < 256 ? L.part_sums[t] : 0, pc = t < 256 ? L.part_counts[t] : 0;
-                const uint64_t rs = before + scan_threads(L, ps, none), rc = before_count + scan_threads(L, pc, none);
-                if (by_count ? rc - pc <= target && target < rc : rs - ps <= target && target < rs) {
+                const uint64_t s = L.part_sums[t];
+                const uint32_t c = L.part_counts[t];
+                uint64_t run = s, none;
+                uint32_t runs = c, number;
+                scan_threads(L, run, runs, none, number);
+                const uint64_t rs = before + run, rc = before_count + runs;
+                if (by_count ? rc - c <= target && target < rc : rs - s <= target && target < rs) {
                     L.found = t;
-                    L.found_before = rs - ps;
-                    L.found_count = rc - pc;
-                    L.found_tokens = pc;
+                    L.found_before = rs - s;
+                    L.found_count = rc - c;
                 }
                 __syncthreads();
                 prefix = prefix << (shift - next) | (uint64_t)L.found;
                 shift = next;
                 before = L.found_before;
                 before_count = L.found_count;
-                tokens = L.found_tokens;
             }
-            make_list(lo, hi, shift, prefix);           // (of `tokens`)
-            in_list = shift == BITS ? bin : -1;
+            if (shift < BITS) {                         // what the prefix leaves of the range
+                const int low = shift - 20;             // bits of the key in question, none where the index is
+                key_hi = ~(uint32_t)(low > 0 ? prefix << low : prefix >> -low);
+                key_lo = low > 0 ? key_hi - ((1u << low) - 1) : key_hi;
+            }
+            in_list = shift == BITS && turn >= 0 ? bin : -1;
         }
-        weigh((int)tokens, before, none, none);
-        pick(target, by_count ? (int)(target - before_count) : -1);
+        if (turn < 0) {
+            all_listed = listed;
+            if (listed) count = UINT64_MAX;
+            else {
+                // counts (where there is a top_k) and sums by bins; how many tokens min_p keeps does not matter, only their sum
+                for_row<sizeof(T) / 2>(x, n, [&](float v, int) {
+                    const double d = row.distance(v);
+                    const int b = bin_of(d);
+                    if (b >= kBins) return;
+                    const uint64_t weight = weight_of(d);
+                    if (weight >= least) kept += weight;
+                    if (top_k > 0) atomicAdd(&L.counts[b], 1u);
+                    add(L.sums[b], weight);
+                });
+                __syncthreads();
+                const uint64_t s1 = L.sums[2 * t + 1];
+                const uint32_t c1 = L.counts[2 * t + 1];
+                uint64_t run = L.sums[2 * t] + s1;
+                uint32_t runs = L.counts[2 * t] + c1, number;
+                scan_threads(L, run, runs, sum, number);
+                count = number;
+                L.sums[2 * t] = run - s1;
+                L.sums[2 * t + 1] = run;
+                L.counts[2 * t] = runs - c1;
+                L.counts[2 * t + 1] = runs;
+            }
+        }
+        if (listed) {
+            sorted = false;
+            L.part_sums[t] = 0;
+            L.part_counts[t] = 0;
+            if (t == 0) L.few = 0;
+            __syncthreads();
+            const double each = (double)kThreads / (((double)(key_hi - key_lo) + 1.0) * n);
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int i = t + j * kThreads;
+                w[j] = 0;
+                part[j] = kThreads;
+                if (i >= (int)L.listed) continue;
+                const uint32_t key = L.keys[i];
+                w[j] = weight_of(row.distance(value_of_key(key)));
+                if (all_listed) kept += w[j] >= least ? w[j] : 0;
+                part[j] = min((uint32_t)(((double)(key_hi - key) * n + L.at[i]) * each), (uint32_t)kThreads - 1);    // (keeps order)
+                atomicAdd(&L.part_counts[part[j]], 1u);
+                add(L.part_sums[part[j]], w[j]);
+            }
+            __syncthreads();
+            uint64_t run = L.part_sums[t], here;
+            uint32_t runs = L.part_counts[t], number;
+            scan_threads(L, run, runs, here, number);
+            L.part_sums[t] = run;
+            L.part_counts[t] = runs;
+            if (all_listed) sum = here;
+        }
+        if (turn < 0) {
+            if (least) {                                // (of all that are listed: no less than of the kept ones, if those are fewer)
+                uint32_t zero = 0, number;
+                uint64_t mine = kept;
+                scan_threads(L, mine, zero, kept, number);
+            }
+            continue;
+        }
+
+        // The token at which the running number of tokens (by_count) or the running sum passes `target`: to L.token, L.found_weight,
+        // and the running sum with it to L.found_sum.  Where its part of the list has up to 64 tokens, one wave compares them all;
+        // else the list is sorted.
+        __syncthreads();
+        const int tokens = (int)L.listed;
+        if (!sorted) {
+            const uint64_t hi_s = before + L.part_sums[t], lo_s = t ? before + L.part_sums[t - 1] : before;
+            const uint64_t hi_c = before_count + L.part_counts[t], lo_c = t ? before_count + L.part_counts[t - 1] : before_count;
+            if (by_count ? lo_c <= target && target < hi_c : lo_s <= target && target < hi_s) {
+                L.found = t;
+                L.found_before = lo_s;
+                L.found_count = lo_c;
+                L.found_tokens = hi_c - lo_c;
+            }
+            __syncthreads();
+            if (L.found_tokens <= 64) {
+#pragma unroll
+                for (int j = 0; j < EACH; ++j)
+                    if (part[j] == (uint32_t)L.found) {
+                        const uint32_t p = atomicAdd(&L.few, 1u);
+                        L.few_keys[p] = L.keys[t + j * kThreads];
+                        L.few_at[p] = L.at[t + j * kThreads];
+                    }
+                __syncthreads();
+                if (wave == 0) {
+                    const int few = (int)L.found_tokens;
+                    uint32_t key = lane < few ? L.few_keys[lane] : 0;
+                    int at = lane < few ? L.few_at[lane] : INT32_MAX;
+                    const uint64_t weight = lane < few ? weight_of(row.distance(value_of_key(key))) : 0;
+                    // how many of them, and which sum, come before this one
+                    uint64_t run = L.found_before, rank = L.found_count;
+                    for (int i = 0; i < few; ++i) {
+                        const uint32_t ki = (uint32_t)__builtin_amdgcn_readlane((int)key, i);
+                        const int ai = __builtin_amdgcn_readlane(at, i);
+                        const uint64_t wi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)weight, i) |
+                                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(weight >> 32), i) << 32;
+                        if (ki > key || (ki == key && ai < at)) {
+                            run += wi;
+                            ++rank;
+                        }
+                    }
+                    if (lane < few && (by_count ? rank == target : run <= target && target < run + weight)) {
+                        L.token = at;
+                        L.found_weight = weight;
+                        L.found_sum = run + weight;
+                    }
+                    if (lane == 0) L.few = 0;
+                }
+            } else {
+                sort_list(L, tokens);
+                sorted = true;
+            }
+        }
+        if (sorted) {                                   // thread t has the tokens 4 t ..
+            uint64_t v[EACH], mine = 0, none;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int i = t * EACH + j;
+                v[j] = i < tokens ? weight_of(row.distance(value_of_key(L.keys[i]))) : 0;
+                mine += v[j];
+            }
+            uint64_t run = mine;
+            uint32_t zero = 0, number;
+            scan_threads(L, run, zero, none, number);
+            run += before - mine;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const int i = t * EACH + j;
+                if (i < tokens && (by_count ? before_count + i == target : run <= target && target < run + v[j])) {
+                    L.token = L.at[i];
+                    L.found_weight = v[j];
+                    L.found_sum = run + v[j];
+                }
+                run += v[j];
+            }
+        }
+        __syncthreads();
         if (turn < 2) sum = L.found_sum;
     }
     if (t == 0) answer(L.token, (float)((double)L.found_weight / (double)sum));
