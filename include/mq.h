@@ -669,14 +669,16 @@ mq_status mq_kv8_read(const mq_kv8_cache* cache, int T, mq_dtype type, const int
  * Attention over the 8-bit cache: arguments and result as mq_attention_kv4.
  * Scores, maxima, sums and the running results are fp32; queries enter the products
  * in fp16 (bf16 ones scaled by a power of two for each query and head, which
- * keeps what is 2^-39 of the largest value and more), weights in fp16, up to 2^15
- * and down to 2^-24 for the largest product of a weight and its block's scale.
- * Weights below 2^-126 of the largest are 0.
+ * keeps what is 2^-39 of the largest value and more), weights in fp16 (fp16 calls: each as
+ * two numbers, so that their rounding does not show), up to 2^15 and down to 2^-24 for the
+ * largest product of a weight and its block's scale.  Weights below 2^-126 of the largest are 0.
  * A query with a value that is not finite gives NaN, and changes no other's
  * result.  A token whose key is NaN makes the queries that see it NaN, and no others.
- * Sizes past the launch's indexes are refused, and have the workspace size 0: 2^24
- * workgroups of 128 columns max_q group (of 16 or 32 up to 32 columns) or more for the
- * sequences and key heads, or 2^24 sequences, key heads and columns where contexts are split.
+ * Sizes past the launch's indexes are refused, and have the workspace size 0: with blocks
+ * of 16, 32, 64 or (from 65 on) 128 columns max_q group, a launch has less than 2^24
+ * workgroups, of which every sequence, key head, block and chunk of tokens is one; one
+ * sequence has at most 65535 blocks, and where contexts are split there are less than 2^24
+ * columns of all sequences and key heads; max_kv is at most 2^31 - 1 - 65536.
  */
 size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group,
                                        int head_dim, int max_q, int64_t max_kv);

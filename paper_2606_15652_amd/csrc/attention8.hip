@@ -332,10 +332,10 @@ struct Part8 {
         empty = first_col >= columns;
         if (empty) return;
         const int seen = (int)seq.seen(a, (min(first_col + cols, columns) - 1) / a.group);
-        chunks = max(1, (seen + a.chunk - 1) / a.chunk);
+        chunks = max(1, (int)(((int64_t)seen + a.chunk - 1) / a.chunk));
         empty = (int)blockIdx.z >= chunks;
-        from = (int)blockIdx.z * a.chunk;
-        until = min(from + a.chunk, seen);
+        from = (int)blockIdx.z * a.chunk;                   // (below `seen` where it is not empty)
+        until = (int)min((int64_t)from + a.chunk, (int64_t)seen);
     }
 };
 

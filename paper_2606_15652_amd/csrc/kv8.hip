@@ -60,39 +60,72 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
     const int64_t len = a.lens[b], had = len - count;       // had < 0: the first -had tokens have no place
     const int64_t block = (had > 0 ? had : 0) / kBlockTokens + (a.starts ? which - first_unit(a.starts, b) : 0);
     const int64_t at = block * kBlockTokens;
-    if (count <= 0 || at >= len) return;
+    if (count <= 0 || at < 0 || at >= len) return;          // (below 0: starts that do not ascend)
     const int64_t row = block_row8(a.c, a.table + (int64_t)b * a.table_pages, a.table_pages, block, head);
     if (row < 0) return;
     const int64_t base = row * D, blk = row / kBlockTokens;
 
-    // the block's new tokens, and which of them are finite in key and value
-    f32x8 x[2][TURNS];
-    uint32_t fresh = 0, fine = 0;                           // bit i: this lane's token of turn i
-    uint32_t amax[2] = {0, 0};
+    // The block's new tokens, and which of them are finite in key and value (bits, the same in every lane).  Of keys a lane has
+    // eight channels of TURNS tokens; of values two channels of every token (of a half of them where rows have 64), so that
+    // four tokens of a channel, which lie side by side in the cache, are one word (byte by byte, 16381 tokens of 8 heads
+    // 31 us, so 24).
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    constexpr int PAIRS = D / 2, QUADS = kBlockTokens / 4 * PAIRS / 64;
+    const int pair = lane % PAIRS, half = lane / PAIRS;     // lanes of half h have the quads h, h + 64 / PAIRS, ..
+    auto there = [&](int t) {
+        const int64_t from = first_new + at + t - had;
+        return at + t >= had && at + t < len && from >= 0 && from < a.tokens;
+    };
+    auto row_of = [&](int t) { return first_new + at + t - had; };
+    typename Vec8<T>::type k8[TURNS];
+    t2 v2[QUADS][4];
+    uint32_t fresh = 0, bad = 0, amax[2] = {0, 0};
+#pragma unroll
+    for (int t = 0; t < kBlockTokens; ++t) fresh |= (uint32_t)there(t) << t;
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) {
-        const int64_t t = at + i * ROWS + sub, from = first_new + t - had;
-        const bool there = t >= had && t < len && from >= 0 && from < a.tokens;
-        x[0][i] = x[1][i] = f32x8{};
-        if (there) {
-            x[0][i] = load8(static_cast<const T*>(a.k) + from * a.k_token + head * a.k_head + ch);
-            x[1][i] = load8(static_cast<const T*>(a.v) + from * a.v_token + head * a.v_head + ch);
-        }
-        uint32_t most[2] = {0, 0};
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) most[w] = max(most[w], __float_as_uint(x[w][i][j]) & 0x7FFFFFFFu);
-        const uint64_t bad = __ballot(max(most[0], most[1]) >= kFloatInf);
-        const bool finite = ((bad >> (lane & ~(LANES - 1))) & ((1u << LANES) - 1)) == 0;
-        fresh |= (uint32_t)there << i;
-        fine |= (uint32_t)finite << i;
-        if (finite) {
-            amax[0] = max(amax[0], most[0]);
-            amax[1] = max(amax[1], most[1]);
-        }
+        const int t = i * ROWS + sub;
+        k8[i] = (typename Vec8<T>::type)(T)0.0f;
+        if (fresh >> t & 1) k8[i] = *reinterpret_cast<const typename Vec8<T>::type*>(static_cast<const T*>(a.k) + row_of(t) * a.k_token + head * a.k_head + ch);
     }
-    const bool whole = __ballot(fresh != (1u << TURNS) - 1) == 0;
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = 4 * (i * (64 / PAIRS) + half) + j;
+            v2[i][j] = (t2)(T)0.0f;
+            if (fresh >> t & 1) v2[i][j] = *reinterpret_cast<const t2*>(static_cast<const T*>(a.v) + row_of(t) * a.v_token + head * a.v_head + 2 * pair);
+        }
+    auto bits_of = [](T x) { return __float_as_uint((float)x) & 0x7FFFFFFFu; };
+    uint32_t most_k[TURNS], most_v[QUADS][4];
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        most_k[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most_k[i] = max(most_k[i], bits_of(k8[i][j]));
+        const uint64_t lanes = __ballot(most_k[i] >= kFloatInf);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) bad |= (uint32_t)((lanes >> (r * LANES) & ((1ull << LANES) - 1)) != 0) << (i * ROWS + r);
+    }
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            most_v[i][j] = max(bits_of(v2[i][j][0]), bits_of(v2[i][j][1]));
+            const uint64_t lanes = __ballot(most_v[i][j] >= kFloatInf);
+#pragma unroll
+            for (int h = 0; h < 64 / PAIRS; ++h)
+                bad |= (uint32_t)((PAIRS == 64 ? lanes : lanes >> (h * PAIRS) & ((1ull << (PAIRS % 64)) - 1)) != 0) << (4 * (i * (64 / PAIRS) + h) + j);
+        }
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i)
+        if (!(bad >> (i * ROWS + sub) & 1)) amax[0] = max(amax[0], most_k[i]);
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!(bad >> (4 * (i * (64 / PAIRS) + half) + j) & 1)) amax[1] = max(amax[1], most_v[i][j]);
+    const bool whole = fresh == 0xFFFFFFFFu;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         uint8_t *codes = (w ? a.c.v : a.c.k) + base, *held = (w ? a.c.ve : a.c.ke) + blk;
@@ -120,24 +153,38 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
             }
             wave_sync();
         }
+        auto scaled = [&](T x) { return ldexpf((float)x, 127 - e); };
+        // a token that is not finite: NaN throughout its key, and a value of zeros
+        if (w == 0) {
 #pragma unroll
-        for (int i = 0; i < TURNS; ++i) {
-            if (!(fresh >> i & 1)) continue;
-            const int t = i * ROWS + sub;
-            uint32_t q[2];
+            for (int i = 0; i < TURNS; ++i) {
+                const int t = i * ROWS + sub;
+                if (!(fresh >> t & 1)) continue;
+                uint32_t q[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float f[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = ldexpf(x[w][i][4 * h + j], 127 - e);
-                // a token that is not finite: NaN throughout its key, and a value of zeros
-                q[h] = fine >> i & 1 ? to_e4m3x4(f[0], f[1], f[2], f[3]) : w ? 0u : 0x7F7F7F7Fu;
-            }
-            if (w == 0) {
+                for (int h = 0; h < 2; ++h)
+                    q[h] = bad >> t & 1 ? 0x7F7F7F7Fu : to_e4m3x4(scaled(k8[i][4 * h]), scaled(k8[i][4 * h + 1]), scaled(k8[i][4 * h + 2]), scaled(k8[i][4 * h + 3]));
                 *reinterpret_cast<uint2*>(im + key_offset8<D>(t, ch)) = make_uint2(q[0], q[1]);
-            } else {
+            }
+        } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) im[value_offset8(t, ch + j)] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+            for (int i = 0; i < QUADS; ++i) {
+                const int t0 = 4 * (i * (64 / PAIRS) + half);
+                const uint32_t news = fresh >> t0 & 15u, bads = bad >> t0 & 15u;
+                if (news == 0) continue;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float f[4];
+                    uint32_t mask = 0;                      // bytes of the new tokens
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        f[j] = bads >> j & 1 ? 0.0f : scaled(v2[i][j][c]);
+                        mask |= news >> j & 1 ? 0xFFu << (8 * j) : 0u;
+                    }
+                    uint32_t* to = reinterpret_cast<uint32_t*>(im + value_offset8(t0, 2 * pair + c));
+                    const uint32_t q = to_e4m3x4(f[0], f[1], f[2], f[3]);
+                    *to = mask == 0xFFFFFFFFu ? q : (*to & ~mask) | (q & mask);
+                }
             }
         }
         wave_sync();
@@ -156,24 +203,29 @@ struct Read8Args {
     int tokens;
 };
 
+// A wave takes 512 / D tokens of a head.  Where they are neighbours in a block, four tokens of a channel of values are one word
+// (byte by byte, 16381 tokens of 8 heads 38 us, so 24).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv8_read_kernel(Read8Args a) {
-    constexpr int LANES = D / 8, ROWS = 64 / LANES;
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, PAIRS = D / 2;
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int head = (int)(unit % a.c.heads), ch = 8 * (lane % LANES);
-    const int64_t token = unit / a.c.heads * ROWS + lane / LANES;
+    const int head = (int)(unit % a.c.heads), ch = 8 * (lane % LANES), sub = lane / LANES;
+    const int64_t first = unit / a.c.heads * ROWS, token = first + sub;
+    const int64_t slot = token < a.tokens ? a.slots[token] : -1;
+    const bool inside = slot >= 0 && slot < (int64_t)a.c.pages << a.c.page_bits;
+    auto base_of = [&](int64_t s) {                         // row of its block
+        const int64_t page = s >> a.c.page_bits, in = s & ((1 << a.c.page_bits) - 1);
+        return ((page * a.c.heads + head) << a.c.page_bits) + in / kBlockTokens * kBlockTokens;
+    };
+    const int64_t slot0 = __shfl((long long)slot, 0);
+    const bool together = __ballot(inside && slot == slot0 + sub) == ~0ull && slot0 % ROWS == 0;
     if (token >= a.tokens) return;
-    const int64_t slot = a.slots[token];
     f32x8 kx{}, vx{};
-    if (slot >= 0 && slot < (int64_t)a.c.pages << a.c.page_bits) {
-        const int64_t page = slot >> a.c.page_bits, in = slot & ((1 << a.c.page_bits) - 1);
-        const int64_t row = ((page * a.c.heads + head) << a.c.page_bits) + in / kBlockTokens * kBlockTokens;
-        const int t = (int)(in % kBlockTokens), ke = a.c.ke[row / kBlockTokens] - 127, ve = a.c.ve[row / kBlockTokens] - 127;
+    if (inside) {
+        const int64_t row = base_of(slot);
+        const int t = (int)(slot % kBlockTokens), ke = a.c.ke[row / kBlockTokens] - 127;
         const uint2 kw = *reinterpret_cast<const uint2*>(a.c.k + row * D + key_offset8<D>(t, ch));
-        uint32_t vw[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vw[j / 4] |= (uint32_t)a.c.v[row * D + value_offset8(t, ch + j)] << (8 * (j % 4));
         auto values = [](uint32_t a, uint32_t b, int e) {
             const f32x2 p[4] = {from_e4m3<false>(a), from_e4m3<true>(a), from_e4m3<false>(b), from_e4m3<true>(b)};
             f32x8 y;
@@ -182,10 +234,33 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Read8Args a) {
             return y;
         };
         kx = values(kw.x, kw.y, ke);
-        vx = values(vw[0], vw[1], ve);
+        const int ve = a.c.ve[row / kBlockTokens] - 127;
+        if (together) {
+            typedef T t2 __attribute__((ext_vector_type(2)));
+            const int pair = lane % PAIRS, t0 = (int)(slot0 % kBlockTokens) + 4 * (lane / PAIRS);
+            f32x2 y[2][2];                                  // of a channel, by token
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(a.c.v + row * D + value_offset8(t0, 2 * pair + c));
+                y[c][0] = from_e4m3<false>(w);
+                y[c][1] = from_e4m3<true>(w);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                t2 v;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) v[c] = (T)ldexpf(y[c][j / 2][j % 2], ve);
+                *reinterpret_cast<t2*>(static_cast<T*>(a.v) + (first + 4 * (lane / PAIRS) + j) * a.v_token + head * a.v_head + 2 * pair) = v;
+            }
+        } else {
+            uint32_t vw[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vw[j / 4] |= (uint32_t)a.c.v[row * D + value_offset8(t, ch + j)] << (8 * (j % 4));
+            vx = values(vw[0], vw[1], ve);
+        }
     }
     store8(static_cast<T*>(a.k) + token * a.k_token + head * a.k_head + ch, kx);
-    store8(static_cast<T*>(a.v) + token * a.v_token + head * a.v_head + ch, vx);
+    if (!together) store8(static_cast<T*>(a.v) + token * a.v_token + head * a.v_head + ch, vx);
 }
 
 // What a cache has to be, for every call that takes one.
