@@ -72,16 +72,14 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
     typedef T t2 __attribute__((ext_vector_type(2)));
     constexpr int PAIRS = D / 2, QUADS = kBlockTokens / 4 * PAIRS / 64;
     const int pair = lane % PAIRS, half = lane / PAIRS;     // lanes of half h have the quads h, h + 64 / PAIRS, ..
-    auto there = [&](int t) {
-        const int64_t from = first_new + at + t - had;
-        return at + t >= had && at + t < len && from >= 0 && from < a.tokens;
-    };
-    auto row_of = [&](int t) { return first_new + at + t - had; };
     typename Vec8<T>::type k8[TURNS];
     t2 v2[QUADS][4];
-    uint32_t fresh = 0, bad = 0, amax[2] = {0, 0};
-#pragma unroll
-    for (int t = 0; t < kBlockTokens; ++t) fresh |= (uint32_t)there(t) << t;
+    // tokens t of the block that are new, and have their row among those given: from <= t < to
+    const int64_t row0 = first_new + at - had, from = max(max(had - at, -row0), (int64_t)0);
+    const int64_t to = min(min(len - at, a.tokens - row0), (int64_t)kBlockTokens);
+    const uint32_t fresh = to <= from ? 0u : (uint32_t)((1ull << to) - (1ull << from));
+    auto row_of = [&](int t) { return row0 + t; };
+    uint32_t bad = 0, amax[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) {
         const int t = i * ROWS + sub;
