@@ -698,11 +698,12 @@ mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens,
  *   1. top_k (if positive): the first top_k tokens;
  *   2. top_p (below 1): of these the shortest beginning whose sum of w is top_p times
  *      theirs, one token at least;
- *   3. min_p (above 0): of these the tokens with w >= min_p (which min_p above 1 is taken as 1);
+ *   3. min_p (above 0; above 1 it counts as 1): of these the tokens with w >= min_p;
  * the token is the first at which the running sum of w passes u times the sum of all
  * that is left; its probability is w over that sum.  Weights are held as whole
- * multiples of 2^-43, sums and comparisons of them are exact: a token whose weight is below 2^-44
- * is never drawn, and the result does not depend on the order in which anything runs.
+ * multiples of 2^-43, and sums and comparisons of them are exact: a token whose weight is
+ * below 2^-44 is never drawn, and the result does not depend on the order in which anything
+ * runs.
  * temperature 0 (and any in the array that is not positive) gives the first token
  * with the largest logit, and the probability 1.
  * Tokens at -infinity have no weight; where one is at +infinity, only those have.  A row of

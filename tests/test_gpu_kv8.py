@@ -235,6 +235,11 @@ def test_long_offsets():
     s = (torch.arange(70) + (pages - 1) * page).cuda()
     for got, w in zip(m.kv8_read(cache, s), want):
         assert torch.equal(got.cpu(), w.half())
+    for counts in ([1], [70]):                                      # and the attention reads them there
+        q = torch.randn(counts[0], heads, dim, generator=so.generator(9)).half()
+        o = m.attention_kv8(q.cuda(), cache, table, torch.tensor([70], dtype=torch.int32).cuda(), cu_q=fo.starts(counts).cuda(), max_kv=70)
+        exact = so.attention(q, *want, 1 / math.sqrt(dim), True)
+        assert (o.cpu().double() - exact).abs().max() <= 2.0 ** -10 * exact.abs().max()
 
 
 def test_refusals():
