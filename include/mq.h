@@ -716,15 +716,12 @@ mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens,
  *            >= 0.  In arrays, NaN and what is out of range filter nothing (top_p
  *            below 0 is 0).
  *   tokens, probs : out, int64 [rows], fp32 [rows].
- *   workspace : >= mq_sample_workspace_size(rows, vocab) bytes, 16-byte aligned (may
- *               be NULL when that is 0).
  */
-size_t mq_sample_workspace_size(int rows, int vocab);
 mq_status mq_sample(int rows, int vocab, mq_dtype type, const void* logits, int64_t ldx,
                     const float* u, const float* temperature, float temperature_all,
                     const int32_t* top_k, int top_k_all, const float* top_p, float top_p_all,
                     const float* min_p, float min_p_all, int64_t* tokens, float* probs,
-                    void* workspace, size_t ws_bytes, hipStream_t stream);
+                    hipStream_t stream);
 
 /* ======================================================================== */
 /* Offline weight preparation (not on the timed path)                        */

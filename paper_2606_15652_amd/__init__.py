@@ -91,8 +91,7 @@ _SIG = {
     "mq_attention_kv8_workspace_size": (C.c_size_t, [_I, _I, _I, _I, _I, _I, _L]),
     "mq_attention_kv8": (_I, [_P, _I, _I, _I, _I, _L, _I, _P, _L, _L, _P, _I, _P, _P, _F, _I, _P, _L, _L, _P,
                               C.c_size_t, _P]),
-    "mq_sample_workspace_size": (C.c_size_t, [_I, _I]),
-    "mq_sample": (_I, [_I, _I, _I, _P, _L, _P, _P, _F, _P, _I, _P, _F, _P, _F, _P, _P, _P, C.c_size_t, _P]),
+    "mq_sample": (_I, [_I, _I, _I, _P, _L, _P, _P, _F, _P, _I, _P, _F, _P, _F, _P, _P, _P]),
 }
 
 _lib: Optional[C.CDLL] = None

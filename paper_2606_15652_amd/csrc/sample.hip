@@ -638,16 +638,10 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
 
 using namespace mq;
 
-extern "C" size_t mq_sample_workspace_size(int rows, int vocab) {
-    (void)rows;
-    (void)vocab;
-    return 0;
-}
-
 extern "C" mq_status mq_sample(int rows, int vocab, mq_dtype type, const void* logits, int64_t ldx, const float* u,
                                const float* temperature, float temperature_all, const int32_t* top_k, int top_k_all,
                                const float* top_p, float top_p_all, const float* min_p, float min_p_all, int64_t* tokens,
-                               float* probs, void* workspace, size_t ws_bytes, hipStream_t stream) {
+                               float* probs, hipStream_t stream) {
     if (rows < 0 || vocab < 0 || (!mq_host::is_half_type(type) && type != MQ_FP32)) return MQ_ERR_INVALID_ARG;
     if ((!temperature && !(temperature_all >= 0.0f)) || (!top_p && !(top_p_all >= 0.0f)) || (!min_p && !(min_p_all >= 0.0f)))
         return MQ_ERR_INVALID_ARG;
@@ -656,10 +650,8 @@ extern "C" mq_status mq_sample(int rows, int vocab, mq_dtype type, const void* l
     if (!logits || !u || !tokens || !probs) return MQ_ERR_INVALID_ARG;
     if (!mq_host::aligned(logits, type == MQ_FP32 ? 4 : 2) || !mq_host::aligned(u, 4) || !mq_host::aligned(temperature, 4) ||
         !mq_host::aligned(top_k, 4) || !mq_host::aligned(top_p, 4) || !mq_host::aligned(min_p, 4) || !mq_host::aligned(tokens, 8) ||
-        !mq_host::aligned(probs, 4) || !mq_host::aligned(workspace, 16))
+        !mq_host::aligned(probs, 4))
         return MQ_ERR_MISALIGNED;
-    const size_t need = mq_sample_workspace_size(rows, vocab);
-    if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     const SampleArgs a{logits, ldx, rows, vocab, u, temperature, top_p, min_p, top_k, temperature_all, top_p_all, min_p_all, top_k_all,
                        tokens, probs};
     auto run = [&](auto z) {

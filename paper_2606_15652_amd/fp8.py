@@ -360,7 +360,7 @@ def _of_rows(value, rows, dtype, name, none, device):
     return None, value
 
 
-def sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=None, workspace=None, stream=None):
+def sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=None, stream=None):
     """(tokens int64 [rows], probabilities fp32 [rows]): a token drawn from each row of logits [rows, vocab] (fp16, bf16 or
     fp32, contiguous rows) by the uniform numbers ``u`` (fp32 [rows], in [0, 1)).  ``temperature``, ``top_k``, ``top_p`` and
     ``min_p`` filter in this order (include/mq.h); each is a number for all rows or a tensor [rows] (fp32, top_k
@@ -387,12 +387,8 @@ def sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=N
         tokens, probs = out
         _need_out(tokens, (rows,), torch.int64, "out[0] (tokens)")
         _need_out(probs, (rows,), torch.float32, "out[1] (probs)")
-    _same_device(logits, "logits", u=u, tokens=tokens, probs=probs, workspace=workspace)
-    lib = load()
-    ws = lib.mq_sample_workspace_size(rows, vocab)
+    _same_device(logits, "logits", u=u, tokens=tokens, probs=probs)
     with _on(logits, stream):
-        wbuf = _scratch(ws, logits.device, stream, workspace)
-        _check("mq_sample", lib.mq_sample(rows, vocab, code, logits.data_ptr(), ldx if rows > 1 else vocab, u.data_ptr(), _ptr(t), t1,
-                                          _ptr(k), k1, _ptr(p), p1, _ptr(m), m1, tokens.data_ptr(), probs.data_ptr(), _ptr(wbuf), ws,
-                                          _stream(stream)))
+        _check("mq_sample", load().mq_sample(rows, vocab, code, logits.data_ptr(), ldx if rows > 1 else vocab, u.data_ptr(), _ptr(t), t1,
+                                             _ptr(k), k1, _ptr(p), p1, _ptr(m), m1, tokens.data_ptr(), probs.data_ptr(), _stream(stream)))
     return tokens, probs

@@ -131,9 +131,8 @@ def test_attention_kv8(lib):
 
 
 def test_sample(lib):
-    def f(rows=3, vocab=100, type=2, x=A, ldx=100, u=A, t=None, t1=1.0, k=None, k1=0, p=None, p1=1.0, m=None, m1=0.0, tokens=A, probs=A,
-          ws=None, nb=0):
-        return lib.mq_sample(rows, vocab, type, x, ldx, u, t, t1, k, k1, p, p1, m, m1, tokens, probs, ws, nb, None)
+    def f(rows=3, vocab=100, type=2, x=A, ldx=100, u=A, t=None, t1=1.0, k=None, k1=0, p=None, p1=1.0, m=None, m1=0.0, tokens=A, probs=A):
+        return lib.mq_sample(rows, vocab, type, x, ldx, u, t, t1, k, k1, p, p1, m, m1, tokens, probs, None)
     assert f(rows=0) == OK and f(rows=0, t=A, t1=-1.0) == OK
     for bad in (dict(rows=-1), dict(vocab=-1), dict(type=3), dict(x=None), dict(u=None), dict(tokens=None), dict(probs=None), dict(t1=-1.0),
                 dict(t1=math.nan), dict(p1=-0.5), dict(p1=math.nan), dict(m1=-0.5), dict(m1=math.nan)):
@@ -143,7 +142,3 @@ def test_sample(lib):
     for bad in (dict(x=A + 2), dict(type=0, x=A + 1), dict(u=A + 2), dict(t=A + 2), dict(k=A + 2), dict(p=A + 1), dict(m=A + 2),
                 dict(tokens=A + 4), dict(probs=A + 2)):
         assert f(**bad) == MISALIGNED, bad
-    need = lib.mq_sample_workspace_size(1, 100000)
-    if need:
-        assert f(rows=1, vocab=100000, ldx=100000) == WORKSPACE
-        assert f(rows=1, vocab=100000, ldx=100000, ws=A, nb=need - 1) == WORKSPACE
