@@ -13,7 +13,7 @@ from contextlib import nullcontext
 from dataclasses import dataclass, field
 
 from . import _check, _need, _need_out, _ptr, _scratch, _stream, _torch, load
-from .serving import _dtype_code, _empty, _need_heads, _need_rows, _same_device
+from .serving import _INT_MAX, _dtype_code, _empty, _need_heads, _need_max_q, _need_rows, _same_device
 
 _no_guard = nullcontext()
 
@@ -60,7 +60,11 @@ def _need_scales(s_x, M, K):
     token, group = s_x.stride()
     if (token != 1 and M > 1) or (group < M and s_x.shape[1] > 1):
         raise ValueError("s_x must have the tokens of a group next to each other (strides 1, at least the tokens)")
-    return group if s_x.shape[1] > 1 else M
+    if s_x.shape[1] == 1:
+        return M
+    if group > _INT_MAX:
+        raise ValueError(f"s_x's groups must be less than 2^31 apart, got {group}")
+    return group
 
 
 def quantize_rows_fp8(X, out=None, stream=None):
@@ -101,7 +105,7 @@ class PackedWeightFP8:
         of, Wq, s_w = self._of, self.Wq, self.s_w
         if not (of and of[0] is Wq and of[1] is s_w and of[2] == (self.N, self.K, Wq.numel(), s_w.numel())):
             torch, need = _torch(), load().mq_weight_fp8_bytes(self.N, self.K)
-            if need == 0:
+            if need == 0 or self.N > _INT_MAX or self.K > _INT_MAX:
                 raise ValueError(f"no e4m3 weight of {self.N} channels and {self.K} codes")
             _need_out(Wq, (need,), torch.uint8, "Wq")
             _need_out(s_w, (_groups(self.N), _groups(self.K)), torch.float32, "s_w")
@@ -116,7 +120,7 @@ class PackedWeightFP8:
 
 def _weight_fp8(N, K, device, stream):
     nbytes = load().mq_weight_fp8_bytes(N, K)
-    if nbytes == 0:
+    if nbytes == 0 or N > _INT_MAX or K > _INT_MAX:
         raise ValueError(f"no e4m3 weight of {N} channels and {K} codes")
     return _empty((nbytes,), _torch().uint8, device, stream)
 
@@ -324,6 +328,7 @@ def attention_kv8(Q, cache: KVCache8, page_table, kv_lens, cu_q=None, max_q=None
     if cu_q is not None:
         _need_out(cu_q, (B + 1,), torch.int32, "cu_q")
         max_q = T if max_q is None else max_q
+        _need_max_q(max_q)
     else:
         if T != B:
             raise ValueError(f"without cu_q, Q has one row for each of the {B} sequences; got {T}")
@@ -373,6 +378,8 @@ def sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=N
     ldx, col = logits.stride()
     if col != 1 and vocab > 1:
         raise ValueError("logits must have contiguous rows")
+    if rows > _INT_MAX or vocab > _INT_MAX:
+        raise ValueError(f"logits must have fewer than 2^31 rows and columns, got {tuple(logits.shape)}")
     device = logits.get_device()
     _need_out(u, (rows,), torch.float32, "u")
     t, t1 = _of_rows(temperature, rows, torch.float32, "temperature", 1.0, device)

@@ -23,6 +23,7 @@ def _types():
 
 
 _types_of = None
+_INT_MAX = 2 ** 31 - 1                          # ctypes cuts what is beyond to its low 32 bits, without an error
 
 
 def _dtype_code(dtype, name, fp32=False):
@@ -43,8 +44,8 @@ def _empty(shape, dtype, device, stream):
 
 
 def _need_rows(t, name, cols=None):
-    """A matrix with contiguous rows (any row stride): its row stride; of a single row, which says nothing, its
-    columns rounded up to 8."""
+    """A matrix with contiguous rows (any row stride that a C int holds): its row stride; of a single row, which says
+    nothing, its columns rounded up to 8."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     shape = t.shape
@@ -53,7 +54,15 @@ def _need_rows(t, name, cols=None):
     row, col = t.stride()
     if col != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return row if shape[0] > 1 else -(-shape[1] // 8) * 8
+    ld = row if shape[0] > 1 else -(-shape[1] // 8) * 8
+    if ld > _INT_MAX or shape[0] > _INT_MAX or shape[1] > _INT_MAX:
+        raise ValueError(f"{name}'s sizes and row stride must be below 2^31, got shape {tuple(shape)}, rows {ld} apart")
+    return ld
+
+
+def _need_max_q(max_q):
+    if max_q > _INT_MAX:
+        raise ValueError(f"max_q must be below 2^31, got {max_q}")
 
 
 def _same_device(first, name, **others):
@@ -197,7 +206,7 @@ class PackedWeight8:
         of, Wq, s_w = self._of, self.Wq, self.s_w
         if not (of and of[0] is Wq and of[1] is s_w and of[2] == (self.N, self.K, Wq.numel(), s_w.numel())):
             torch, need = _torch(), load().mq_weight8_bytes(self.N, self.K)
-            if need == 0:
+            if need == 0 or self.N > _INT_MAX or self.K > _INT_MAX:
                 raise ValueError(f"no INT8 weight of {self.N} channels and {self.K} codes")
             _need_out(Wq, (need,), torch.uint8, "Wq")
             _need_out(s_w, (self.N,), torch.float32, "s_w")
@@ -212,7 +221,7 @@ class PackedWeight8:
 
 def _weight8(N, K, device, stream):
     nbytes = load().mq_weight8_bytes(N, K)
-    if nbytes == 0:
+    if nbytes == 0 or N > _INT_MAX or K > _INT_MAX:
         raise ValueError(f"no INT8 weight of {N} channels and {K} codes")
     return _empty((nbytes,), _torch().uint8, device, stream)
 
@@ -357,6 +366,8 @@ def _need_heads(t, name, heads, head_dim, tokens=None, dtype=None):
     shape, strides = t.shape, t.stride()
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim or (tokens is not None and shape[0] != tokens):
         raise ValueError(f"{name} must be [{'tokens' if tokens is None else tokens}, {heads}, {head_dim}], got {tuple(shape)}")
+    if shape[0] > _INT_MAX:
+        raise ValueError(f"{name} must have fewer than 2^31 tokens, got {shape[0]}")
     if strides[2] != 1:
         raise ValueError(f"{name} must have contiguous rows of {head_dim}")
     # a dimension of one is never stepped along
@@ -424,6 +435,7 @@ def attention_kv4(Q, cache: KVCache4, page_table, kv_lens, cu_q=None, max_q=None
     if cu_q is not None:
         _need_out(cu_q, (B + 1,), torch.int32, "cu_q")
         max_q = T if max_q is None else max_q
+        _need_max_q(max_q)
     else:
         if T != B:
             raise ValueError(f"without cu_q, Q has one row for each of the {B} sequences; got {T}")
