@@ -133,7 +133,7 @@ def quantize_weight_fp8(W, stream=None) -> PackedWeightFP8:
     Wq = _weight_fp8(N, K, W.device, stream)
     s_w = _empty((_groups(N), _groups(K)), torch.float32, W.device, stream)
     with _on(W, stream):
-        _check("mq_quantize_weight_fp8", load().mq_quantize_weight_fp8(W.data_ptr(), N, K, W.stride(0), Wq.data_ptr(), s_w.data_ptr(),
+        _check("mq_quantize_weight_fp8", load().mq_quantize_weight_fp8(W.data_ptr(), N, K, K, Wq.data_ptr(), s_w.data_ptr(),
                                                                        _stream(stream)))
     return PackedWeightFP8(N, K, Wq, s_w)
 
@@ -147,7 +147,7 @@ def repack_weight_fp8(Wc, s_w, stream=None) -> PackedWeightFP8:
     _same_device(Wc, "Wc", s_w=s_w)
     Wq = _weight_fp8(N, K, Wc.device, stream)
     with _on(Wc, stream):
-        _check("mq_repack_weight_fp8", load().mq_repack_weight_fp8(N, K, Wc.data_ptr(), Wc.stride(0), Wq.data_ptr(), _stream(stream)))
+        _check("mq_repack_weight_fp8", load().mq_repack_weight_fp8(N, K, Wc.data_ptr(), K, Wq.data_ptr(), _stream(stream)))
     return PackedWeightFP8(N, K, Wq, s_w)
 
 

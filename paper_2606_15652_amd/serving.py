@@ -232,7 +232,7 @@ def quantize_weight8(W, stream=None) -> PackedWeight8:
     _need(W, torch.float32, "W", 2)
     N, K = W.shape
     Wq, s_w = _weight8(N, K, W.device, stream), _empty((N,), torch.float32, W.device, stream)
-    _check("mq_quantize_weight8", load().mq_quantize_weight8(W.data_ptr(), N, K, W.stride(0), Wq.data_ptr(), s_w.data_ptr(),
+    _check("mq_quantize_weight8", load().mq_quantize_weight8(W.data_ptr(), N, K, K, Wq.data_ptr(), s_w.data_ptr(),
                                                              _stream(stream)))
     return PackedWeight8(N, K, Wq, s_w)
 
@@ -245,7 +245,7 @@ def repack_weight8(Wc, s_w, stream=None) -> PackedWeight8:
     _need_out(s_w, (N,), torch.float32, "s_w")
     _same_device(Wc, "Wc", s_w=s_w)
     Wq = _weight8(N, K, Wc.device, stream)
-    _check("mq_repack_weight8", load().mq_repack_weight8(N, K, Wc.data_ptr(), Wc.stride(0), Wq.data_ptr(), _stream(stream)))
+    _check("mq_repack_weight8", load().mq_repack_weight8(N, K, Wc.data_ptr(), K, Wq.data_ptr(), _stream(stream)))
     return PackedWeight8(N, K, Wq, s_w)
 
 
