@@ -647,7 +647,10 @@ size_t mq_kv8_code_bytes(int pages, int page_size, int heads, int head_dim);
  * page_table[b][t / page_size].  Where new tokens raise a block's e, the codes of the
  * block's earlier tokens are divided by that power of two (ties to even; exact unless
  * they fall below 2^-6).  What lies in a block behind kv_lens[b] counts for
- * nothing and may change.  A block belongs to one sequence of the call.
+ * nothing and may change: a sequence may have been shortened since it was written.
+ * Earlier tokens keep the block's e if one of their codes is 224 or more; where none is (the
+ * tokens that needed it are gone) they count in e with the values they have, whose
+ * codes that changes, exactly.  A block belongs to one sequence of the call.
  *   K, V       : `type` (MQ_FP16 or MQ_BF16), token t's head h at t k_token + h k_head
  *                (elements, multiples of 8), head_dim contiguous values, 16-byte aligned.
  *   page_table : int32 [sequences, table_pages]; tokens past it, or of a page outside

@@ -3,7 +3,9 @@
 // A block of 32 tokens of a sequence and head has one scale 2^e for its keys and
 // one for its values, e the least with |x| <= 448 2^e; codes are e4m3(x 2^-e).
 // Later tokens of the block may raise e: the codes that are there are then
-// divided by the power of two, exactly but where they pass below 2^-6.
+// divided by the power of two, exactly but where they pass below 2^-6.  Where the
+// tokens that raised it have been taken back (the sequence's length went down), it
+// goes down again, and codes are multiplied, exactly.
 //
 // One wave takes one block and head: what the block holds comes to LDS, new codes
 // go there, and it goes back in whole lines.  Nobody else writes the block, so
@@ -42,15 +44,18 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int sequences,
     return first;
 }
 
-// Least e with amax <= 448 2^e = 1.75 2^(e + 8), for the exponent's byte: e + 127 in 0 .. 254.
-__device__ __forceinline__ int exponent_byte(uint32_t amax_bits) {
+// Least e with 2^by amax <= 448 2^e = 1.75 2^(e + 8), for the exponent's byte: e + 127 in 0 .. 254.
+__device__ __forceinline__ int exponent_byte(uint32_t amax_bits, int by = 0) {
     const int x = (int)(amax_bits >> 23) + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return max(x - 8, 0);
+    return amax_bits ? max(x - 8 + by, 0) : 0;
 }
+
+// The bytes of four codes that are NaN, as 0xFF.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t d) { return ((d & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) / 0x80u * 0xFFu; }
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
-    constexpr int LANES = D / 8, ROWS = 64 / LANES, TURNS = kBlockTokens / ROWS, BYTES = kBlockTokens * D;
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, TURNS = kBlockTokens / ROWS, BYTES = kBlockTokens * D, PIECES = BYTES / 1024;
     __shared__ __attribute__((aligned(16))) uint8_t image[4][2][BYTES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
@@ -132,25 +137,54 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
         uint8_t* im = image[wave][w];
         int e = exponent_byte(wave_max_dpp(amax[w]));
         if (!whole) {
-            const int e_old = *held;
-            const bool moves = at < had && e > e_old;       // only tokens from before hold a block's scale up
-            if (at < had) e = max(e, e_old);
+            const int e_old = *held, kept = (int)min(had - at, (int64_t)kBlockTokens);      // tokens from before
+            uint4 p[PIECES];
 #pragma unroll
-            for (int i = 0; i < BYTES / 1024; ++i) {
-                uint4 p = ldg16(codes + i * 1024 + lane * 16);
-                if (moves) {
+            for (int i = 0; i < PIECES; ++i) p[i] = ldg16(codes + i * 1024 + lane * 16);
+            if (kept > 0) {
+                // The kept tokens' bytes: of keys a lane has one token for each tile of 16, of values four for each.
+                uint32_t keep[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int n = w ? kept - 16 * h - lane / 16 * 4 : 4 * (kept - 16 * h - lane % 16);
+                    keep[h] = n >= 4 ? ~0u : n > 0 ? (1u << (8 * n)) - 1u : 0u;
+                }
+                auto each = [&](auto&& f) {
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) {
+                        const uint32_t d[4] = {p[i].x, p[i].y, p[i].z, p[i].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f(d[j] & 0x7F7F7F7Fu & keep[w ? j % 2 : i / (PIECES / 2)]);
+                    }
+                };
+                // A scale that one of them needed shows as a code of 224 (0x76) and more, not NaN.
+                uint32_t needed = 0;
+                each([&](uint32_t d) { needed |= (d + 0x0A0A0A0Au) & ~(d + 0x01010101u); });
+                int e_kept = e_old;
+                if (__ballot((needed & 0x80808080u) != 0) == 0) {
+                    uint32_t most = 0;
+                    each([&](uint32_t d) {
+                        d &= ~nan_bytes(d);
+                        const f32x2 lo = from_e4m3<false>(d), hi = from_e4m3<true>(d);
+                        most = max(most, __float_as_uint(fmaxf(fmaxf(lo[0], lo[1]), fmaxf(hi[0], hi[1]))));
+                    });
+                    e_kept = exponent_byte(wave_max_dpp(most), e_old - 127);
+                }
+                e = max(e, e_kept);
+                if (e != e_old) {
                     auto moved = [&](uint32_t d) {
                         const f32x2 lo = from_e4m3<false>(d), hi = from_e4m3<true>(d);
-                        const int by = e_old - e;
-                        const uint32_t to = to_e4m3x4(ldexpf(lo[0], by), ldexpf(lo[1], by), ldexpf(hi[0], by), ldexpf(hi[1], by));
-                        // a NaN stays the one it was (the conversion may change its sign)
-                        const uint32_t nan = ((d & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) / 0x80u * 0xFFu;
-                        return (to & ~nan) | (d & nan);
+                        // (codes behind the kept ones may pass the largest where the scale goes down)
+                        auto by = [&](float x) { return __builtin_amdgcn_fmed3f(ldexpf(x, e_old - e), -kE4m3Max, kE4m3Max); };
+                        const uint32_t to = to_e4m3x4(by(lo[0]), by(lo[1]), by(hi[0]), by(hi[1])), nan = nan_bytes(d);
+                        return (to & ~nan) | (d & nan);     // a NaN stays the one it was
                     };
-                    p = make_uint4(moved(p.x), moved(p.y), moved(p.z), moved(p.w));
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) p[i] = make_uint4(moved(p[i].x), moved(p[i].y), moved(p[i].z), moved(p[i].w));
                 }
-                *reinterpret_cast<uint4*>(im + i * 1024 + lane * 16) = p;
             }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) *reinterpret_cast<uint4*>(im + i * 1024 + lane * 16) = p[i];
             wave_sync();
         }
         auto scaled = [&](T x) { return ldexpf((float)x, 127 - e); };
@@ -189,7 +223,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Append8Args a) {
         }
         wave_sync();
 #pragma unroll
-        for (int i = 0; i < BYTES / 1024; ++i)
+        for (int i = 0; i < PIECES; ++i)
             *reinterpret_cast<uint4*>(codes + i * 1024 + lane * 16) = *reinterpret_cast<const uint4*>(im + i * 1024 + lane * 16);
         if (lane == 0) *held = (uint8_t)e;
     }

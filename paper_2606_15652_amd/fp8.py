@@ -263,7 +263,8 @@ def kv8_append(cache: KVCache8, K, V, page_table, kv_lens, cu_new=None, stream=N
     """Quantises the tokens K, V [T, heads, head_dim] (fp16 or bf16, any token and head strides that are multiples of 8)
     into the ends of sequences: sequence b has kv_lens[b] (int32) tokens with them, in the pages page_table[b] (int32
     [sequences, pages]), and rows cu_new[b] .. cu_new[b + 1] (int32 [sequences + 1]) are its last ones.  Without
-    ``cu_new`` each sequence has one new token.  A block of 32 tokens whose scale grows is coded anew."""
+    ``cu_new`` each sequence has one new token.  A block of 32 tokens whose scale changes is coded anew; sequences may
+    have been shortened since they were written."""
     torch = _torch()
     code = _dtype_code(getattr(K, "dtype", None), "K")
     kt, kh = _need_heads(K, "K", cache.heads, cache.head_dim)
