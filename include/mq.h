@@ -679,9 +679,9 @@ mq_status mq_kv8_read(const mq_kv8_cache* cache, int T, mq_dtype type, const int
  * result.  A token whose key is NaN makes the queries that see it NaN, and no others.
  * Sizes past the launch's indexes are refused, and have the workspace size 0: with blocks
  * of 16, 32, 64 or (from 65 on) 128 columns max_q group, a launch has less than 2^24
- * workgroups, of which every sequence, key head, block and chunk of tokens is one; one
- * sequence has at most 65535 blocks, and where contexts are split there are less than 2^24
- * columns of all sequences and key heads; max_kv is at most 2^31 - 1 - 65536.
+ * workgroups, of which every sequence, key head, block and chunk of tokens is one; up to 64
+ * columns, and of a single sequence, there are at most 65535 blocks of one, and where contexts are
+ * split less than 2^24 columns of all sequences and key heads; max_kv is at most 2^31 - 1 - 65536.
  */
 size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group,
                                        int head_dim, int max_q, int64_t max_kv);

@@ -57,9 +57,15 @@ struct Attn8Args {
     int64_t max_kv;
     int chunk, chunks;                  // tokens that a workgroup takes, and chunks of the longest sequence
     const int2* order;                  // sequence and block of columns of each workgroup, or null
-    float* part;                        // of each sequence, key head, chunk and column: O[D], then m, J, l in `stats`
+    float* part;                        // sums (sums_at): O[D], then m, J, l in `stats`
     float* stats;
 };
+
+// Where the sums of a column are: entries are the order's blocks or else the sequences, of `cols` columns each (a block's, or
+// max_q queries'), by key head, chunk and column.
+__device__ __forceinline__ int64_t sums_at(const Attn8Args& a, int entry_head, int chunk, int cols, int col) {
+    return ((int64_t)entry_head * a.chunks + chunk) * cols + col;
+}
 
 // One sequence's lengths, as the arguments bound them.
 struct Sequence8 {
@@ -289,7 +295,7 @@ template <typename T, int D>
 struct Target8 {
     T* out;
     float *sum, *stat;
-    __device__ __forceinline__ Target8(const Attn8Args& a, const Sequence8& seq, int b, int head, int c, bool direct) {
+    __device__ __forceinline__ Target8(const Attn8Args& a, const Sequence8& seq, int head, int c, int entry_cols, int entry_col, bool direct) {
         out = nullptr;
         sum = stat = nullptr;
         const int64_t row = (int64_t)seq.first + c / a.group;
@@ -297,7 +303,7 @@ struct Target8 {
         if (direct) {
             out = static_cast<T*>(a.o) + row * a.o_token + (int64_t)(head * a.group + c % a.group) * a.o_head;
         } else {
-            const int64_t at = (((int64_t)b * a.c.heads + head) * a.chunks + blockIdx.z) * ((int64_t)a.max_q * a.group) + c;
+            const int64_t at = sums_at(a, blockIdx.x, blockIdx.z, entry_cols, entry_col);
             sum = a.part + at * D;
             stat = a.stats + 3 * at;
         }
@@ -462,7 +468,7 @@ __global__ __launch_bounds__(256, 2) void attention8_kernel(Attn8Args a) {
             ll += stat[w0 + w][cc][2] * __builtin_amdgcn_exp2f(by);
             sum += *reinterpret_cast<const f32x4*>(&sums[w0 + w][cc][ch]) * __builtin_amdgcn_exp2f(stat[w0 + w][cc][1] + by - j);
         }
-        Target8<T, D>(a, seq, part.b, part.head, part.first_col + c, part.chunks == 1).store(ch, sum, mm, j, ll);
+        Target8<T, D>(a, seq, part.head, part.first_col + c, a.max_q * a.group, part.first_col + c, part.chunks == 1).store(ch, sum, mm, j, ll);
     }
 }
 
@@ -546,27 +552,30 @@ __global__ __launch_bounds__(64 * WAVES, 3) void attention8_wide_kernel(Attn8Arg
     for (int n = 0; n < NT; ++n) {
         const int c = part.first_col + wave * COLS + 16 * n + col;
         if (c >= part.columns) continue;
-        const Target8<T, D> to(a, seq, part.b, part.head, c, part.chunks == 1);
+        const Target8<T, D> to(a, seq, part.head, c, a.order ? WAVES * COLS : a.max_q * a.group, a.order ? c - part.first_col : c, part.chunks == 1);
 #pragma unroll
         for (int i = 0; i < TILES; ++i) to.store(16 * i + 4 * quarter, cols.o[i][n], cols.m[n], cols.jj[n], cols.l[n]);
     }
 }
 
 // The chunks of one column to its result: one workgroup, D / 4 threads for four channels each, the rest share the chunks.
-template <typename T, int D>
+template <typename T, int D, bool ORDERED>
 __global__ __launch_bounds__(256) void attention8_join_kernel(Attn8Args a, int block_cols) {
     constexpr int LANES = D / 4, PARTS = 256 / LANES;
     __shared__ float sums[PARTS][D + 4], ls[PARTS];
-    const int most = a.max_q * a.group, unit = blockIdx.x / most, c = blockIdx.x % most;
-    const int b = unit / a.c.heads, head = unit % a.c.heads;
-    const Sequence8 seq(a, b);
+    const int cols = ORDERED ? block_cols : a.max_q * a.group;
+    const int entry = blockIdx.x / cols, col = blockIdx.x % cols, head = entry % a.c.heads;
+    const int2 item = ORDERED ? a.order[entry / a.c.heads] : make_int2(entry / a.c.heads, 0);
+    if (item.x < 0) return;
+    const Sequence8 seq(a, item.x);
+    const int c = ORDERED ? item.y * block_cols + col : col;
     const int columns = seq.queries * a.group;
     if (c >= columns) return;
     const int64_t seen = seq.seen(a, (min(c / block_cols * block_cols + block_cols, columns) - 1) / a.group);
     const int chunks = max(1, (int)((seen + a.chunk - 1) / a.chunk));
     const int64_t row = (int64_t)seq.first + c / a.group;
     if (chunks == 1 || row < 0 || row >= a.tokens) return;
-    const int64_t stride = most, first = (int64_t)unit * a.chunks * stride + c;
+    const int64_t stride = cols, first = sums_at(a, entry, 0, cols, col);
     const int part = threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
     // every wave finds the maxima, 64 chunks at a time
     float m = kLowest, j = kNone;
@@ -613,6 +622,7 @@ struct Plan8a {
     int blocks;                         // of columns
     int chunk, chunks;                  // tokens of a workgroup, and the most of them of a sequence
     int items;                          // entries of the order, 0 for none
+    int64_t sums;                       // columns whose chunks' sums are kept, 0 for one chunk
 };
 constexpr int kWideTiles = 2, kWideWaves = 4;
 static bool plan_attention8(int sequences, int tokens, int heads, int group, int head_dim, int max_q, int64_t max_kv, Plan8a& p) {
@@ -627,7 +637,8 @@ static bool plan_attention8(int sequences, int tokens, int heads, int group, int
     const int cols = p.cols;
     const int64_t blocks = std::max<int64_t>(1, (columns + cols - 1) / cols);
     // many columns of several sequences: workgroups in order of their work, and none for blocks that are not there (prompts of
-    // 1025 to 1877 queries over 1025 to 4095 tokens 365 us, in order 211)
+    // 1025 to 1877 queries over 1025 to 4095 tokens 365 us, in order 211).  Chunks' sums go by it, too: laid out for max_q
+    // queries of every sequence, 64 of one token and one of 2048 over 8192 tokens took 1.6 GB and a million workgroups to join.
     const int64_t items = p.wt == 0 && sequences > 1 ? std::min((int64_t)tokens * group / cols + sequences, sequences * blocks) : 0;
     const int64_t units = (items ? items : sequences * blocks) * heads;
     // Chunks: as many as there are CUs for one query and little more, two or three a CU for more columns (8 contexts of 8192
@@ -639,9 +650,10 @@ static bool plan_attention8(int sequences, int tokens, int heads, int group, int
     const int64_t share = want > 1 ? (max_kv + want - 1) / want : p.wt ? std::min<int64_t>(max_kv, 2048) : max_kv;
     const int64_t chunk = std::max<int64_t>(least, (share + 31) / 32 * 32);
     const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
-    if ((!items && blocks > 65535) || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256) ||
-        (chunks > 1 && !mq_host::launch_holds((int64_t)sequences * heads * columns, 256)))
+    if ((!items && blocks > 65535) || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256))
         return false;
+    p.sums = chunks == 1 ? 0 : (items ? items * cols : sequences * columns) * heads;
+    if (!mq_host::launch_holds(p.sums, 256)) return false;
     p.chunk = (int)chunk;
     p.blocks = (int)blocks;
     p.chunks = (int)chunks;
@@ -655,15 +667,13 @@ using namespace mq;
 
 // The order, then the chunks' sums and what belongs to them.
 static size_t order_bytes(const Plan8a& p) { return ((size_t)p.items * sizeof(int2) + 15) / 16 * 16; }
-static size_t workspace_of(const Plan8a& p, int sequences, int heads, int group, int head_dim, int max_q) {
-    return order_bytes(p) + (p.chunks == 1 ? 0 : (size_t)sequences * heads * p.chunks * ((size_t)max_q * group) * (head_dim + 3) * sizeof(float));
-}
+static size_t workspace_of(const Plan8a& p, int head_dim) { return order_bytes(p) + (size_t)p.sums * p.chunks * (head_dim + 3) * sizeof(float); }
 
 extern "C" size_t mq_attention_kv8_workspace_size(int sequences, int tokens, int heads, int group, int head_dim, int max_q,
                                                   int64_t max_kv) {
     Plan8a p;
     if (tokens < 0 || !plan_attention8(sequences, tokens, heads, group, head_dim, max_q, max_kv, p)) return 0;
-    return workspace_of(p, sequences, heads, group, head_dim, max_q);
+    return workspace_of(p, head_dim);
 }
 
 extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, int tokens, int group, int max_q, int64_t max_kv,
@@ -686,13 +696,13 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
         !mq_host::aligned(cu_q, 4) || !mq_host::aligned(workspace, 16))
         return MQ_ERR_MISALIGNED;
     if (!cu_q) max_q = 1;
-    const size_t need = workspace_of(p, sequences, cache->heads, group, cache->head_dim, max_q);
+    const size_t need = workspace_of(p, cache->head_dim);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     Attn8Args a{device_cache8(cache), Q, O, q_token, q_head, o_token, o_head, page_table, kv_lens, cu_q, table_pages, tokens, group, max_q,
                 causal != 0, scale * kLog2e, max_kv, p.chunk, p.chunks, nullptr, nullptr, nullptr};
     int2* order = static_cast<int2*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + order_bytes(p));
-    a.stats = a.part + (size_t)sequences * cache->heads * p.chunks * ((size_t)max_q * group) * cache->head_dim;
+    a.stats = a.part + (size_t)p.sums * p.chunks * cache->head_dim;
     const dim3 grid(p.items ? p.items * cache->heads : sequences * cache->heads, p.items ? 1 : p.blocks, p.chunks);
     if (p.items) {
         hipLaunchKernelGGL(attention8_order_kernel, dim3(1), dim3(1024), 0, stream, a, sequences, p.cols, p.items, order);
@@ -707,9 +717,8 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
             else if (p.wt == 4) few(attention8_kernel<T, D, 2, 4>);
             else if (p.wt == 2) few(attention8_kernel<T, D, 2, 2>);
             else hipLaunchKernelGGL((attention8_wide_kernel<T, D, kWideTiles, kWideWaves>), grid, dim3(64 * kWideWaves), 0, stream, a);
-            if (p.chunks > 1)
-                hipLaunchKernelGGL((attention8_join_kernel<T, D>), dim3((unsigned)(sequences * cache->heads) * (unsigned)(max_q * group)),
-                                   dim3(256), 0, stream, a, p.cols);
+            auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.sums), dim3(256), 0, stream, a, p.cols); };
+            if (p.chunks > 1) p.items ? join(attention8_join_kernel<T, D, true>) : join(attention8_join_kernel<T, D, false>);
         };
         if (cache->head_dim == 64) run(std::integral_constant<int, 64>{});
         else run(std::integral_constant<int, 128>{});
