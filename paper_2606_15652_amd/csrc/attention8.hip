@@ -647,7 +647,12 @@ static bool plan_attention8(int sequences, int tokens, int heads, int group, int
     // least for each wave, or 128; where there are enough without, single tokens take 2048 at a time, as contexts may be
     // ragged (64 of 257 to 8191 tokens: in chunks of 2048 114 us, of 4096 118; 128 of 1000 tokens whole 51, in halves 64).
     const int64_t least = p.wt ? 256 * p.wt / p.nt : 128, want = (p.wt ? 256 * p.nt : 768) / std::max<int64_t>(1, units);
-    const int64_t share = want > 1 ? (max_kv + want - 1) / want : p.wt ? std::min<int64_t>(max_kv, 2048) : max_kv;
+    // Sums take 1 GB at most: as many chunks as that holds, where a launch's bound is far above the contexts that are there (1024
+    // sequences of 500 tokens, 8 queries each by 8 x 8 heads, bounded by 131072: in chunks of 2048 17.6 GB and 1680 us, so 0.8 and 1010; with one of 131072
+    // among them 1870 and 1860).
+    const int64_t sums = (int64_t)sequences * heads * columns * (head_dim + 3) * (int64_t)sizeof(float);
+    const int64_t holds = std::max<int64_t>(1, (1 << 30) / std::max<int64_t>(1, sums));
+    const int64_t share = want > 1 ? (max_kv + want - 1) / want : p.wt ? std::max(std::min<int64_t>(max_kv, 2048), (max_kv + holds - 1) / holds) : max_kv;
     const int64_t chunk = std::max<int64_t>(least, (share + 31) / 32 * 32);
     const int64_t chunks = std::max<int64_t>(1, (max_kv + chunk - 1) / chunk);
     if ((!items && blocks > 65535) || chunks > 65535 || (int64_t)sequences * heads > INT32_MAX || !mq_host::launch_holds(units * chunks, 256))
