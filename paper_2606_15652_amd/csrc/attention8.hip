@@ -117,7 +117,7 @@ struct Columns8 {
     // show.
     static constexpr int WEIGHTS = __is_same(T, _Float16) ? 2 : 1;
     f16x8 q[NT][STEPS];
-    float slope[NT];                                        // of the scores, in log2
+    int by[NT];                                             // queries as operands are 2^by of what they are
     int sees[NT];                                           // tokens that the column sees
     int least, most;                                        // over the columns that are there
     f32x4 o[TILES][NT];
@@ -147,13 +147,12 @@ struct Columns8 {
             big = max(big, (uint32_t)__shfl_xor((int)big, 16));
             big = max(big, (uint32_t)__shfl_xor((int)big, 32));
             // bf16: by a power of two so that the largest is in [2^14, 2^15).  A query that is not finite is NaN throughout.
-            const int by = __is_same(T, __bf16) && big ? 141 - (int)(big >> 23) : 0;
+            by[n] = __is_same(T, __bf16) && big ? 141 - (int)(big >> 23) : 0;
             const bool bad = big >= kFloatInf;
-            slope[n] = fminf(ldexpf(a.scale, -by), FLT_MAX);
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) q[n][s][j] = bad ? (_Float16)__builtin_nanf("") : (_Float16)ldexpf(x[s][j], by);
+                for (int j = 0; j < 8; ++j) q[n][s][j] = bad ? (_Float16)__builtin_nanf("") : (_Float16)ldexpf(x[s][j], by[n]);
             least = has && sees[n] < least ? sees[n] : least;
             most = max(most, sees[n]);
             m[n] = kLowest;
@@ -175,7 +174,7 @@ struct Columns8 {
     // that no page holds (ve < 0) is seen by none; it is not left out, as a branch around the products makes the compiler
     // copy the accumulators.
     template <typename K, typename V>
-    __device__ __forceinline__ void take(int block, int ke, int ve, K&& key, V&& value) {
+    __device__ __forceinline__ void take(float scale, int block, int ke, int ve, K&& key, V&& value) {
         const int quarter = (threadIdx.x & 63) >> 4;
         f32x4 s[NT][2] = {};
 #pragma unroll
@@ -194,7 +193,8 @@ struct Columns8 {
         bool moves = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            c[n] = fminf(fmaxf(ldexpf(slope[n], ke - 127), FLT_MIN), FLT_MAX);  // not 0: hidden scores stay -infinity
+            // (by both powers at once: by one of them it may be below fp32's normal numbers); not 0: hidden scores stay -infinity
+            c[n] = fminf(fmaxf(ldexpf(scale, ke - 127 - by[n]), FLT_MIN), FLT_MAX);
             if ((block + 1) * kBlockTokens > least || ve < 0) {
                 const int left = ve < 0 ? 0 : sees[n] - block * kBlockTokens - 4 * quarter;
 #pragma unroll
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256, 2) void attention8_kernel(Attn8Args a) {
     };
     auto take = [&](const Block& x, int block) {
         auto half = [](const uint4 p, int h) { return h ? operand8(p.z, p.w) : operand8(p.x, p.y); };
-        cols.take(block, x.ke, __builtin_amdgcn_readfirstlane(x.ve), [&](int t, int s) { return half(x.k[t * (PIECES / 2) + s / 2], s % 2); },
+        cols.take(a.scale, block, x.ke, __builtin_amdgcn_readfirstlane(x.ve), [&](int t, int s) { return half(x.k[t * (PIECES / 2) + s / 2], s % 2); },
                   [&](int i) { return half(x.v[i / 2], i % 2); });
     };
     const int first_block = part.from / kBlockTokens + wt;
@@ -536,7 +536,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void attention8_wide_kernel(Attn8Arg
         load(x, block + BLOCKS);                            // (past the end: some page's, unused)
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
-            cols.take(block + b, ke[b], ve[b], [&](int t, int s) { return staged[slot][b][t * STEPS + s][lane]; },
+            cols.take(a.scale, block + b, ke[b], ve[b], [&](int t, int s) { return staged[slot][b][t * STEPS + s][lane]; },
                       [&](int i) { return staged[slot][b][2 * PIECES + i][lane]; });
         slot ^= 1;
         write(x, slot);
@@ -648,9 +648,9 @@ static bool plan_attention8(int sequences, int tokens, int heads, int group, int
     // ragged (64 of 257 to 8191 tokens: in chunks of 2048 114 us, of 4096 118; 128 of 1000 tokens whole 51, in halves 64).
     const int64_t least = p.wt ? 256 * p.wt / p.nt : 128, want = (p.wt ? 256 * p.nt : 768) / std::max<int64_t>(1, units);
     // Sums take 1 GB at most: as many chunks as that holds, where a launch's bound is far above the contexts that are there (1024
-    // sequences of 500 tokens, 8 queries each by 8 x 8 heads, bounded by 131072: in chunks of 2048 17.6 GB and 1680 us, so 0.8 and 1010; with one of 131072
-    // among them 1870 and 1860).
-    const int64_t sums = (int64_t)sequences * heads * columns * (head_dim + 3) * (int64_t)sizeof(float);
+    // sequences of 500 tokens, 8 queries each by 8 x 8 heads, bounded by 131072: in chunks of 2048 17.6 GB and 1680 us, so 0.8 and
+    // 1010; with one of 131072 among them 1870 and 1860).
+    const int64_t sums = p.wt ? (int64_t)sequences * heads * columns * (head_dim + 3) * (int64_t)sizeof(float) : 0;
     const int64_t holds = std::max<int64_t>(1, (1 << 30) / std::max<int64_t>(1, sums));
     const int64_t share = want > 1 ? (max_kv + want - 1) / want : p.wt ? std::max(std::min<int64_t>(max_kv, 2048), (max_kv + holds - 1) / holds) : max_kv;
     const int64_t chunk = std::max<int64_t>(least, (share + 31) / 32 * 32);
@@ -704,7 +704,7 @@ extern "C" mq_status mq_attention_kv8(const mq_kv8_cache* cache, int sequences, 
     const size_t need = workspace_of(p, cache->head_dim);
     if (need > 0 && (!workspace || ws_bytes < need)) return MQ_ERR_WORKSPACE;
     Attn8Args a{device_cache8(cache), Q, O, q_token, q_head, o_token, o_head, page_table, kv_lens, cu_q, table_pages, tokens, group, max_q,
-                causal != 0, scale * kLog2e, max_kv, p.chunk, p.chunks, nullptr, nullptr, nullptr};
+                causal != 0, std::min(scale * kLog2e, FLT_MAX), max_kv, p.chunk, p.chunks, nullptr, nullptr, nullptr};
     int2* order = static_cast<int2*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + order_bytes(p));
     a.stats = a.part + (size_t)p.sums * p.chunks * cache->head_dim;
