@@ -598,7 +598,10 @@ mq_status mq_unpack_weight_fp8(int N, int K, const uint8_t* Wq, uint8_t* Wc, int
  * Product of both:
  *     Y[m,n] = rn( sum_g s_x[m,g] s_w[n/128,g] sum_{k in g} Xq[m,k] Wq[n,k] + bias[n] )
  * in fp32: the sum of a group, the product of its scales, the sum of the groups (in an
- * order that the sizes alone choose) and the bias; rounded once to `type`.
+ * order that the sizes alone choose) and the bias; rounded once to `type`.  For 16-bit
+ * types a group's sum is the 8-bit matrix unit's: of each eight neighbouring products
+ * it cuts all, towards zero, to multiples of 2^(e - 13), e the sum of the exponents of the
+ * largest one's factors (1.4e-5 to 3e-5 of the norm; such results' own rounding is 2e-4 and more).
  *   Xq, s_x   : as mq_quantize_rows_fp8 writes them, any K; ldx, lds as there.  A row's
  *               bytes between K and the next multiple of 16 are read: they must not be NaN
  *               codes.  Beyond 32 rows, (31 ldx + K) below 2^31 (fewer: (M - 1) ldx + K).
@@ -609,7 +612,8 @@ mq_status mq_unpack_weight_fp8(int N, int K, const uint8_t* Wq, uint8_t* Wc, int
  *               (may be NULL when that is 0).
  */
 size_t mq_gemm_fp8_workspace_size(int M, int N, int K);
-/* Output tile of one workgroup of that launch, and the splits of K. */
+/* Output tile of one workgroup of that launch, and the splits of K (MQ_FP32: 128 x 128
+ * where this says 256 x 256). */
 mq_status mq_gemm_fp8_tile(int M, int N, int K, int* rows, int* cols, int* splits);
 mq_status mq_gemm_fp8(int M, int N, int K, const void* Xq, int ldx, const float* s_x, int lds,
                       const uint8_t* Wq, const float* s_w, mq_dtype type, const void* bias,

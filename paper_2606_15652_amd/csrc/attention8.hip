@@ -38,8 +38,6 @@ namespace mq {
 mq_status check_cache8(const mq_kv8_cache* c);
 Cache8 device_cache8(const mq_kv8_cache* c);
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;          // weights up to 2^kSlack before a maximum moves
 constexpr float kLift = 7.0f;           // and as operands up to 2^(kSlack + kLift) < 65504, down to 2^-24
@@ -87,14 +85,6 @@ struct Sequence8 {
         return n < 0 ? 0 : n < len ? n : len;
     }
 };
-
-__device__ __forceinline__ f16x8 operand8(uint32_t a, uint32_t b) {
-    struct {
-        f16x2 v[4];
-    } r = {{__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
-            __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)}};
-    return __builtin_bit_cast(f16x8, r);
-}
 
 // A product that is rounded before anything is taken from it.
 __device__ __forceinline__ float rounded_product(float a, float b) {

@@ -9,6 +9,7 @@ constexpr float kE4m3Max = 448.0f;
 constexpr int kBlockTokens = 32;        // tokens that share a scale for each head
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // Two numbers to e4m3, ties to even, in the lower (or upper, HIGH) half of `into`: |a|, |b| <= 448, or NaN.
@@ -23,6 +24,15 @@ __device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d
 template <bool HIGH>
 __device__ __forceinline__ f32x2 from_e4m3(uint32_t w) {
     return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_pk_f32_fp8((int)w, HIGH));
+}
+
+// Eight codes as fp16, exactly.
+__device__ __forceinline__ f16x8 operand8(uint32_t a, uint32_t b) {
+    struct {
+        f16x2 v[4];
+    } r = {{__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
+            __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)}};
+    return __builtin_bit_cast(f16x8, r);
 }
 
 // What other lanes of the wave have written to LDS is there.

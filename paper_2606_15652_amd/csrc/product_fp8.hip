@@ -2,16 +2,18 @@
 // 128 channels, and for each block of 128 x 128 of the weight:
 //   Y[m,n] = rn( sum_g s_x[m,g] s_w[n/128,g] sum_{k in g} Xq[m,k] Wq[n,k] + bias[n] ).
 //
-// One v_mfma_f32_16x16x128_f8f6f4 sums a group of 128 for 16 x 16 outputs, and one
+// One v_mfma_f32_16x16x128_f8f6f4 sums a group of 128 for 16 x 16 outputs (fp32 results: four
+// v_mfma_f32_16x16x32_f16, the codes turned to fp16), and one
 // fp32 fma an output puts it to the rest, by the product of the two scales.  The
 // weight's layout is that of the INT8 product (mq.h): lane l's 16 bytes of two
 // pieces of 64 codes are the instruction's 32, and X's rows are taken the same way.
 // Codes of X past K are not read; weights past K and N are zero.
 //
-// Inside the instruction eight neighbouring products at a time are cut, towards zero, to multiples of 2^(e - 13), e the
+// Inside the 8-bit instruction eight neighbouring products at a time are cut, towards zero, to multiples of 2^(e - 13), e the
 // sum of the exponents of the largest one's factors (measured; the 32-long fp8 instruction does the same).  It costs
-// outputs some 1e-4 of their norm where values are of one size, less than fp16's rounding of them; fp16 operands would
-// avoid it at half the rate.  Everything after a group's sum is fp32.
+// outputs 1.4e-5 of their norm where values are of one size, some 3e-5 beside outlier channels; a 16-bit result's own rounding
+// is 2e-4 and more, an fp32 one's is not.  Those go by fp16 operands, at half the rate: 1e-7 of the norm; 1 x 4096 -> 131071
+// 91 us instead of 88, 128 rows of it 163 and 147, 4096 x 4096 -> 32768 1030 and 620.  Everything after a group's sum is fp32.
 //
 // Two kernels, as there:
 //  * tiled: output tiles through LDS slots of one group, filled by the LDS DMA, scales of X among them.  The matrix
@@ -24,6 +26,7 @@
 #include "kv8.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mq {
 
@@ -52,9 +55,18 @@ __host__ __device__ __forceinline__ int blocks_of(int N) { return (N + kBlockF8 
 __device__ __forceinline__ i32x8 operand_f8(const uint4 a, const uint4 b) {
     return i32x8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
-// the sum of 128 products for 16 x 16 outputs
+// The sum of 128 products for 16 x 16 outputs of type T: of fp32 ones in fp32, of others cut as above.
+template <typename T>
 __device__ __forceinline__ f32x4 mfma_f8(const i32x8 a, const i32x8 b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{}, 0, 0, 0, 0, 0, 0);
+    if constexpr (__is_same(T, float)) {
+        f32x4 sum = {};
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand8((uint32_t)a[i], (uint32_t)a[i + 1]), operand8((uint32_t)b[i], (uint32_t)b[i + 1]), sum, 0, 0, 0);
+        return sum;
+    } else {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{}, 0, 0, 0, 0, 0, 0);
+    }
 }
 
 // y[c] = sum + bias for 16 channels n .. n + 15 of row m, stored.
@@ -114,7 +126,7 @@ __device__ __forceinline__ void store_block_f8(const ProductF8Args& a, int m0, i
 // without both, 1690).
 // SPLIT: workgroup y takes the groups [y, y + 1) per_split and writes its sums to part[y][M][N].
 template <typename T, int WM, int WN, int MI, int SLOTS, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product_f8_tiled_kernel(ProductF8Args a, int per_split, float* __restrict__ part) {
+__device__ __forceinline__ void product_tiled(ProductF8Args a, int per_split, float* __restrict__ part) {
     constexpr int TM = 16 * MI * WM, TN = kBlockF8 * WN, NW = WM * WN;
     constexpr int XL = TM / 8 / NW, WL = TN / 8 / NW;       // 1 KB loads of a wave and stage
     constexpr int SW = (TN + kGroup - 1) / kGroup;          // rows of blocks of W's scales
@@ -205,7 +217,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_f8_tiled_kernel(Produ
                     issue(slot);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[j % 2][i] = mfma_f8(w[i], x[j % 3]);
+                for (int i = 0; i < 4; ++i) sum[j % 2][i] = mfma_f8<T>(w[i], x[j % 3]);
             }
             if (j > 0) {
 #pragma unroll
@@ -251,6 +263,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_f8_tiled_kernel(Produ
     }
 }
 
+// 16-bit results, and fp32 ones (whose matrix instruction is another).
+template <typename T, int WM, int WN, int MI, int SLOTS, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_f8_tiled_kernel(ProductF8Args a, int per_split, float* __restrict__ part) {
+    product_tiled<T, WM, WN, MI, SLOTS, SPLIT>(a, per_split, part);
+}
+template <int WM, int WN, int MI, int SLOTS, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_fp32_tiled_kernel(ProductF8Args a, int per_split, float* __restrict__ part) {
+    product_tiled<float, WM, WN, MI, SLOTS, SPLIT>(a, per_split, part);
+}
+
 // Sums of the splits, in order -> Y, 16 channels a thread.
 template <typename T>
 __global__ __launch_bounds__(256) void product_f8_join_kernel(ProductF8Args a, int splits, const float* __restrict__ part) {
@@ -274,7 +296,7 @@ __global__ __launch_bounds__(256) void product_f8_join_kernel(ProductF8Args a, i
 // --------------------------------------------------------------------------
 constexpr int kStreamWavesF8 = 8;
 template <typename T, int P, int MT>
-__global__ __launch_bounds__(64 * kStreamWavesF8) void product_f8_stream_kernel(ProductF8Args a) {
+__device__ __forceinline__ void product_stream(ProductF8Args a) {
     constexpr int U = P + MT >= 4 ? 1 : 6 / (P + MT);       // groups in flight, twice
     __shared__ float sums[kStreamWavesF8][16 * MT][16 * P + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -322,7 +344,7 @@ __global__ __launch_bounds__(64 * kStreamWavesF8) void product_f8_stream_kernel(
                 const float scale = b.s[u][j] * b.by[u];
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const f32x4 sum = mfma_f8(operand_f8(b.w[u][i][0], b.w[u][i][1]), xo);
+                    const f32x4 sum = mfma_f8<T>(operand_f8(b.w[u][i][0], b.w[u][i][1]), xo);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(scale, sum[r], acc[i][j][r]);
                 }
@@ -357,6 +379,15 @@ __global__ __launch_bounds__(64 * kStreamWavesF8) void product_f8_stream_kernel(
         if (a.bias) y += (float)static_cast<const T*>(a.bias)[n];
         static_cast<T*>(a.Y)[m * a.ldy + n] = (T)y;
     }
+}
+
+template <typename T, int P, int MT>
+__global__ __launch_bounds__(64 * kStreamWavesF8) void product_f8_stream_kernel(ProductF8Args a) {
+    product_stream<T, P, MT>(a);
+}
+template <int P, int MT>
+__global__ __launch_bounds__(64 * kStreamWavesF8) void product_fp32_stream_kernel(ProductF8Args a) {
+    product_stream<float, P, MT>(a);
 }
 
 // --------------------------------------------------------------------------
@@ -474,6 +505,8 @@ __global__ __launch_bounds__(256) void unpack_weight_f8_kernel(const uint8_t* __
     }
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
 static bool shape_f8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
 
 // ---------------------------------------------------------------- host side --
@@ -604,7 +637,8 @@ extern "C" mq_status mq_gemm_fp8(int M, int N, int K, const void* Xq, int ldx, c
     if (M < 0 || N < 0 || K < 0 || (!mq_host::is_half_type(type) && type != MQ_FP32)) return MQ_ERR_INVALID_ARG;
     if (M > (1 << 24) || !shape_f8_ok(N, K) || ldx < (K + 15) / 16 * 16 || ldx % 16 != 0 || ldy < N || lds < M) return MQ_ERR_UNSUPPORTED_SHAPE;
     if (M == 0) return MQ_OK;
-    const PlanF8 p = plan_f8(M, N, K);
+    PlanF8 p = plan_f8(M, N, K);
+    if (type == MQ_FP32 && p.rows == 256) p.rows = p.cols = 128;   // (operands in fp16 leave no registers for more: 4096 x 4096 -> 32768 1320 us)
     const int64_t groups = p.streams ? (int64_t)blocks_of(N) * (kBlockF8 / p.cols)
                                      : (int64_t)((M + p.rows - 1) / p.rows) * ((N + p.cols - 1) / p.cols);
     const int64_t joins = p.splits > 1 ? ((int64_t)M * (blocks_of(N) * kBlockF8 / 16) + 255) / 256 : 0;
@@ -623,29 +657,44 @@ extern "C" mq_status mq_gemm_fp8(int M, int N, int K, const void* Xq, int ldx, c
     auto run = [&](auto z) {
         using T = decltype(z);
         float* part = static_cast<float*>(workspace);
-        auto stream_rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * kStreamWavesF8), 0, stream, a); };
-        auto tile = [&](auto kernel, int threads) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)groups, p.splits), dim3(threads), 0, stream, a, p.per_split, part);
+        auto stream_rows = [&](auto pieces, auto rows) {
+            constexpr int P = decltype(pieces)::value, MT = decltype(rows)::value;
+            const dim3 grid((unsigned)groups), threads(64 * kStreamWavesF8);
+            if constexpr (__is_same(T, float)) hipLaunchKernelGGL((product_fp32_stream_kernel<P, MT>), grid, threads, 0, stream, a);
+            else hipLaunchKernelGGL((product_f8_stream_kernel<T, P, MT>), grid, threads, 0, stream, a);
         };
+        auto tile = [&](auto wm, auto wn, auto mi, auto slots, auto split) {
+            constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, MI = decltype(mi)::value, SLOTS = decltype(slots)::value;
+            constexpr bool SPLIT = decltype(split)::value;
+            const dim3 grid((unsigned)groups, p.splits), threads(64 * WM * WN);
+            if constexpr (__is_same(T, float)) hipLaunchKernelGGL((product_fp32_tiled_kernel<WM, WN, MI, SLOTS, SPLIT>), grid, threads, 0, stream, a, p.per_split, part);
+            else hipLaunchKernelGGL((product_f8_tiled_kernel<T, WM, WN, MI, SLOTS, SPLIT>), grid, threads, 0, stream, a, p.per_split, part);
+        };
+        constexpr Int<1> _1{};
+        constexpr Int<2> _2{};
+        constexpr Int<3> _3{};
+        constexpr Int<4> _4{};
+        constexpr std::true_type split{};
+        constexpr std::false_type whole{};
         if (p.streams && p.rows == 16) {
-            if (p.cols == 64) stream_rows(product_f8_stream_kernel<T, 4, 1>);
-            else if (p.cols == 32) stream_rows(product_f8_stream_kernel<T, 2, 1>);
-            else stream_rows(product_f8_stream_kernel<T, 1, 1>);
+            if (p.cols == 64) stream_rows(_4, _1);
+            else if (p.cols == 32) stream_rows(_2, _1);
+            else stream_rows(_1, _1);
         } else if (p.streams) {
-            if (p.cols == 32) stream_rows(product_f8_stream_kernel<T, 2, 2>);
-            else stream_rows(product_f8_stream_kernel<T, 1, 2>);
+            if (p.cols == 32) stream_rows(_2, _2);
+            else stream_rows(_1, _2);
         } else if (p.rows == 256) {
-            tile(product_f8_tiled_kernel<T, 2, 4, 8, 2, false>, 512);
+            if constexpr (!__is_same(T, float)) tile(_2, _4, Int<8>{}, _2, whole);
         } else if (p.cols == 128) {
-            if (p.splits > 1) tile(product_f8_tiled_kernel<T, 4, 2, 2, 4, true>, 512);
-            else if (groups <= 256) tile(product_f8_tiled_kernel<T, 4, 2, 2, 4, false>, 512);
-            else tile(product_f8_tiled_kernel<T, 4, 2, 2, 2, false>, 512);
+            if (p.splits > 1) tile(_4, _2, _2, _4, split);
+            else if (groups <= 256) tile(_4, _2, _2, _4, whole);
+            else tile(_4, _2, _2, _2, whole);
         } else if (p.rows == 128) {
-            if (p.splits > 1) tile(product_f8_tiled_kernel<T, 4, 1, 2, 3, true>, 256);
-            else tile(product_f8_tiled_kernel<T, 4, 1, 2, 3, false>, 256);
+            if (p.splits > 1) tile(_4, _1, _2, _3, split);
+            else tile(_4, _1, _2, _3, whole);
         } else {
-            if (p.splits > 1) tile(product_f8_tiled_kernel<T, 4, 1, 1, 4, true>, 256);
-            else tile(product_f8_tiled_kernel<T, 4, 1, 1, 4, false>, 256);
+            if (p.splits > 1) tile(_4, _1, _1, _4, split);
+            else tile(_4, _1, _1, _4, whole);
         }
         if (p.splits > 1)
             hipLaunchKernelGGL(product_f8_join_kernel<T>, dim3((unsigned)joins), dim3(256), 0, stream, a, p.splits, part);
