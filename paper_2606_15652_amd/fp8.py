@@ -34,7 +34,7 @@ def _groups(K):
 
 def _need_codes_fp8(Xq, K=None):
     """e4m3 rows as the kernels take them: their stride in bytes.  The bytes up to the next multiple of 16 after a row's
-    last code have to be there too."""
+    last code have to be there too, and must not be NaN codes (0x7F, 0xFF): products read them."""
     torch = _torch()
     ld = _need_rows(Xq, "Xq", K)
     if Xq.dtype != torch.float8_e4m3fn:
@@ -173,7 +173,9 @@ def gemm_fp8_tile(M: int, N: int, K: int):
 
 
 def gemm_fp8(Xq, s_x, pw: PackedWeightFP8, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
-    """Y [M, N] = sum over groups of s_x s_w (Xq Wq^T) + bias, in fp16 (or ``out_dtype`` bf16, fp32); bias in Y's type."""
+    """Y [M, N] = sum over groups of s_x s_w (Xq Wq^T) + bias, in fp16 (or ``out_dtype`` bf16, fp32); bias in Y's type.
+    Rows whose K is no multiple of 16 are followed by their padding to 16 bytes, which must not hold NaN codes (as memory that was never
+    written may): ``quantize_rows_fp8`` clears it, a program that makes codes itself does."""
     torch = _torch()
     ldx = _need_codes_fp8(Xq, pw.K)
     M = Xq.shape[0]
