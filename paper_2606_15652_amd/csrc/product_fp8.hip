@@ -511,8 +511,11 @@ using Int = std::integral_constant<int, N>;
 static bool shape_f8_ok(int N, int K) { return N >= 1 && N <= (1 << 24) && K >= 1 && K <= MQ_W8A8_MAX_K; }
 
 // ---------------------------------------------------------------- host side --
-// Which kernel takes a product.  Up to 16 rows, and up to 32 where the weight is small, the streaming kernel (5000 -> 8191 at 17 rows
-// 12.2 us, 64 x 64 tiles 16; 4096 -> 14336 14.5 and 14.6).  Beyond, of four tiles and one, two or four splits of K the one with
+// Which kernel takes a product.  Up to 16 rows, and up to 32 where the weight is small, the streaming kernel (a graph of calls; 5000 ->
+// 8191 at 17 rows 10.3 us, 64 x 64 tiles 16.2; 4096 -> 14336 15.0 and 14.4; at 16 rows 13.2 and 14.4).  It takes as many pieces
+// a workgroup as leave every CU one: four from 192 blocks on (1 x 4096 -> 14336 by one, two, four 17.9, 14.9, 12.1; 5120 wide 7.9, 6.1,
+// 5.9), two from 64 on (16 x 8192 -> 8191 20.4, 14.5, 18.3; 1 x 8192 -> 2048 5.6, 6.0, 8.3), one where K is long besides (1 x 14336 ->
+// 4096 12.5, 14.4, 22.3; not the best from 65 blocks on: 16 x 14336 -> 5120 25.7, 19.4).  Beyond, of four tiles and one, two or four splits of K the one with
 // the least estimated time: groups by the time of one (a workgroup alone on its CU waits for memory; more of them
 // share it), or W at the rate that the tiles reach, whichever is longer, and what writing and joining a split's sums
 // takes.  128 x 128 has four slots where there is no more than one workgroup a CU, and two where two share it (8192 ->
