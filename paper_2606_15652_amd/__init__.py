@@ -172,11 +172,26 @@ def _need_out(t, shape, dtype, name):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory that a launch on `stream` writes.  When that is not torch's current
+    stream it comes from the stream's own pool (what the current stream's pool
+    hands out, work that is still waiting there may be using), and is tied to the
+    current stream, where the caller goes on with it."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _scratch(nbytes, device, stream, given=None, name="workspace"):
     """Workspace for one launch on `stream`.  A caller-provided tensor is
-    checked for size; an allocated one is tied to `stream` when that is not
-    torch's current stream, so that the caching allocator does not hand it
-    out again while the launch still uses it."""
+    checked for size."""
     torch = _torch()
     if nbytes == 0:
         return None
@@ -185,10 +200,7 @@ def _scratch(nbytes, device, stream, given=None, name="workspace"):
         if given.numel() < nbytes:
             raise ValueError(f"{name} needs {nbytes} bytes, got {given.numel()}")
         return given
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None and stream != torch.cuda.current_stream(device):
-        buf.record_stream(stream)
-    return buf
+    return _empty((nbytes,), torch.uint8, device, stream)
 
 
 # -------------------------------------------------------------- hot path --
@@ -204,8 +216,8 @@ def quantize_act(X, out=None, stream=None):
     _need(X, torch.float16, "X", 2)
     M, K = X.shape
     if out is None:
-        Xq = torch.empty((M, act_bytes(K)), dtype=torch.uint8, device=X.device)
-        s_x = torch.empty((M,), dtype=torch.float16, device=X.device)
+        Xq = _empty((M, act_bytes(K)), torch.uint8, X.device, stream)
+        s_x = _empty((M,), torch.float16, X.device, stream)
     else:
         Xq, s_x = out
         _need_out(Xq, (M, act_bytes(K)), torch.uint8, "out[0] (Xq)")
@@ -279,7 +291,7 @@ def fused_gemm(Xq, s_x, pw: PackedWeight, out=None, variant: str = "auto", strea
     M = Xq.shape[0]
     if Xq.shape[1] != act_bytes(pw.K) or s_x.shape[0] != M:
         raise ValueError("Xq / s_x shapes do not match the weight")
-    Y = out if out is not None else torch.empty((M, pw.N), dtype=torch.float16, device=Xq.device)
+    Y = out if out is not None else _empty((M, pw.N), torch.float16, Xq.device, stream)
     if out is not None:
         _need_out(Y, (M, pw.N), torch.float16, "out")
     rp, kb, rq, sr = _res_ptrs(pw)
@@ -301,7 +313,7 @@ def unfused_gemm(Xq, s_x, pw: PackedWeight, out=None, stream=None, workspace=Non
     M = Xq.shape[0]
     if Xq.shape[1] != act_bytes(pw.K) or s_x.shape[0] != M:
         raise ValueError("Xq / s_x shapes do not match the weight")
-    Y = out if out is not None else torch.empty((M, pw.N), dtype=torch.float16, device=Xq.device)
+    Y = out if out is not None else _empty((M, pw.N), torch.float16, Xq.device, stream)
     if out is not None:
         _need_out(Y, (M, pw.N), torch.float16, "out")
     rp, kb, rq, sr = _res_ptrs(pw)
@@ -321,8 +333,8 @@ def fused_gemm_acc_i32(Xq, pw: PackedWeight, variant: str = "auto", stream=None)
     M = Xq.shape[0]
     if Xq.shape[1] != act_bytes(pw.K):
         raise ValueError("Xq shape does not match the weight")
-    Tb = torch.empty((M, pw.N), dtype=torch.int32, device=Xq.device)
-    Tr = torch.empty((M, pw.N), dtype=torch.int32, device=Xq.device)
+    Tb = _empty((M, pw.N), torch.int32, Xq.device, stream)
+    Tr = _empty((M, pw.N), torch.int32, Xq.device, stream)
     rp, kb, rq, _ = _res_ptrs(pw)
     _check("mq_fused_gemm_acc_i32", load().mq_fused_gemm_acc_i32(
         VARIANTS[variant], M, pw.N, pw.K, _ptr(Xq), _ptr(pw.Wq), rp, kb, pw.nnzb, rq,
@@ -338,8 +350,8 @@ def quantize_act8(X, out=None, stream=None):
     _need(X, torch.float16, "X", 2)
     M, K = X.shape
     if out is None:
-        Xq8 = torch.empty((M, 3 * K // 2), dtype=torch.uint8, device=X.device)
-        s_x = torch.empty((M,), dtype=torch.float16, device=X.device)
+        Xq8 = _empty((M, 3 * K // 2), torch.uint8, X.device, stream)
+        s_x = _empty((M,), torch.float16, X.device, stream)
     else:
         Xq8, s_x = out
         _need_out(Xq8, (M, 3 * K // 2), torch.uint8, "out[0] (Xq8)")
@@ -357,7 +369,7 @@ def fused_gemm_a8(Xq8, s_x, pw: PackedWeight, out=None, stream=None):
     M = Xq8.shape[0]
     if Xq8.shape[1] * 2 != 3 * pw.K or s_x.shape[0] != M:
         raise ValueError("Xq8 / s_x shapes do not match the weight")
-    Y = out if out is not None else torch.empty((M, pw.N), dtype=torch.float16, device=Xq8.device)
+    Y = out if out is not None else _empty((M, pw.N), torch.float16, Xq8.device, stream)
     if out is not None:
         _need_out(Y, (M, pw.N), torch.float16, "out")
     rp, kb, rq, sr = _res_ptrs(pw)
@@ -371,8 +383,8 @@ def fused_gemm_a8_acc_i32(Xq8, pw: PackedWeight, stream=None):
     torch = _torch()
     _need(Xq8, torch.uint8, "Xq8", 2)
     M = Xq8.shape[0]
-    Tb = torch.empty((M, pw.N), dtype=torch.int32, device=Xq8.device)
-    Tr = torch.empty((M, pw.N), dtype=torch.int32, device=Xq8.device)
+    Tb = _empty((M, pw.N), torch.int32, Xq8.device, stream)
+    Tr = _empty((M, pw.N), torch.int32, Xq8.device, stream)
     rp, kb, rq, _ = _res_ptrs(pw)
     _check("mq_fused_gemm_a8_acc_i32", load().mq_fused_gemm_a8_acc_i32(
         M, pw.N, pw.K, _ptr(Xq8), _ptr(pw.Wq), rp, kb, pw.nnzb, rq, _ptr(Tb), _ptr(Tr), _stream(stream)))
@@ -384,7 +396,7 @@ def unpack_act8(Xq8, stream=None):
     torch = _torch()
     _need(Xq8, torch.uint8, "Xq8", 2)
     M, K = Xq8.shape[0], Xq8.shape[1] * 2 // 3
-    Xc = torch.empty((M, K), dtype=torch.int8, device=Xq8.device)
+    Xc = _empty((M, K), torch.int8, Xq8.device, stream)
     _check("mq_unpack_act8", load().mq_unpack_act8(M, K, _ptr(Xq8), _ptr(Xc), K, _stream(stream)))
     return Xc
 
@@ -394,7 +406,7 @@ def repack_act8(Xc, n_invalid=None, stream=None):
     torch = _torch()
     _need(Xc, torch.int8, "Xc", 2)
     M, K = Xc.shape
-    Xq8 = torch.empty((M, 3 * K // 2), dtype=torch.uint8, device=Xc.device)
+    Xq8 = _empty((M, 3 * K // 2), torch.uint8, Xc.device, stream)
     if n_invalid is not None:
         _need(n_invalid, torch.int32, "n_invalid", 1)
     _check("mq_repack_act8", load().mq_repack_act8(M, K, _ptr(Xc), Xc.stride(0), _ptr(Xq8),
@@ -414,7 +426,7 @@ def linear(X, pw: PackedWeight, out=None, workspace=None, stream=None):
     M, K = X.shape
     if K != pw.K:
         raise ValueError("X does not match the weight")
-    Y = out if out is not None else torch.empty((M, pw.N), dtype=torch.float16, device=X.device)
+    Y = out if out is not None else _empty((M, pw.N), torch.float16, X.device, stream)
     if out is not None:
         _need_out(Y, (M, pw.N), torch.float16, "out")
     rp, kb, rq, sr = _res_ptrs(pw)
@@ -438,9 +450,9 @@ def repack_weights(Wq_c, s_w_c, rowptr, kb, Rq_c, s_r, n_invalid=None, stream=No
     _need(s_w_c, torch.float16, "s_w_c", 2)
     N, K = Wq_c.shape[0], Wq_c.shape[1] * 2
     nnzb = int(kb.numel())
-    Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=Wq_c.device)
-    s_w = torch.empty((N, K // BLOCK), dtype=torch.float16, device=Wq_c.device)
-    Rq = torch.empty((max(nnzb, 1), BLOCK, BLOCK // 2), dtype=torch.uint8, device=Wq_c.device)
+    Wq = _empty((N, K // 2), torch.uint8, Wq_c.device, stream)
+    s_w = _empty((N, K // BLOCK), torch.float16, Wq_c.device, stream)
+    Rq = _empty((max(nnzb, 1), BLOCK, BLOCK // 2), torch.uint8, Wq_c.device, stream)
     if nnzb:
         _need(Rq_c, torch.uint8, "Rq_c", 3)
     if n_invalid is not None:
@@ -455,9 +467,9 @@ def unpack_weights(pw: PackedWeight, stream=None):
     """Library layout -> canonical (Wq_c [N, K/2], s_w_c [N, K/128], Rq_c [nnzb, 128, 64])."""
     torch = _torch()
     dev = pw.Wq.device
-    Wq_c = torch.empty((pw.N, pw.K // 2), dtype=torch.uint8, device=dev)
-    s_w_c = torch.empty((pw.N, pw.K // BLOCK), dtype=torch.float16, device=dev)
-    Rq_c = torch.empty((max(pw.nnzb, 1), BLOCK, BLOCK // 2), dtype=torch.uint8, device=dev)
+    Wq_c = _empty((pw.N, pw.K // 2), torch.uint8, dev, stream)
+    s_w_c = _empty((pw.N, pw.K // BLOCK), torch.float16, dev, stream)
+    Rq_c = _empty((max(pw.nnzb, 1), BLOCK, BLOCK // 2), torch.uint8, dev, stream)
     _check("mq_unpack_weights", load().mq_unpack_weights(
         pw.N, pw.K, _ptr(pw.Wq), _ptr(pw.s_w), pw.nnzb, _ptr(pw.Rq) if pw.nnzb else None,
         _ptr(Wq_c), _ptr(s_w_c), _ptr(Rq_c) if pw.nnzb else None, _stream(stream)))
@@ -469,7 +481,7 @@ def repack_act(Xq_c, n_invalid=None, stream=None):
     torch = _torch()
     _need(Xq_c, torch.uint8, "Xq_c", 2)
     M, K = Xq_c.shape[0], Xq_c.shape[1] * 2
-    Xq = torch.empty((M, act_bytes(K)), dtype=torch.uint8, device=Xq_c.device)
+    Xq = _empty((M, act_bytes(K)), torch.uint8, Xq_c.device, stream)
     if n_invalid is not None:
         _need(n_invalid, torch.int32, "n_invalid", 1)
     _check("mq_repack_act", load().mq_repack_act(M, K, _ptr(Xq_c), Xq_c.stride(0), _ptr(Xq),
@@ -484,7 +496,7 @@ def unpack_act(Xq, stream=None):
     M, K = Xq.shape[0], Xq.shape[1] * 4 // 3
     if Xq.shape[1] != act_bytes(K) or K % 128:
         raise ValueError("Xq is not in the operand layout of a K divisible by 128")
-    Xq_c = torch.empty((M, K // 2), dtype=torch.uint8, device=Xq.device)
+    Xq_c = _empty((M, K // 2), torch.uint8, Xq.device, stream)
     _check("mq_unpack_act", load().mq_unpack_act(M, K, _ptr(Xq), _ptr(Xq_c), K // 2, _stream(stream)))
     return Xq_c
 
@@ -495,9 +507,9 @@ def quantize_weight(W, with_score: bool = True, stream=None):
     torch = _torch()
     _need(W, torch.float32, "W", 2)
     N, K = W.shape
-    Wq = torch.empty((N, K // 2), dtype=torch.uint8, device=W.device)
-    s_w = torch.empty((N, K // BLOCK), dtype=torch.float16, device=W.device)
-    score = torch.empty((N // BLOCK, K // BLOCK), dtype=torch.float64, device=W.device) if with_score else None
+    Wq = _empty((N, K // 2), torch.uint8, W.device, stream)
+    s_w = _empty((N, K // BLOCK), torch.float16, W.device, stream)
+    score = _empty((N // BLOCK, K // BLOCK), torch.float64, W.device, stream) if with_score else None
     _check("mq_quantize_weight", load().mq_quantize_weight(
         _ptr(W), N, K, W.stride(0), _ptr(Wq), _ptr(s_w), _ptr(score), _stream(stream)))
     return Wq, s_w, score
@@ -507,7 +519,7 @@ def hessian_diag(X, stream=None):
     torch = _torch()
     _need(X, torch.float16, "X", 2)
     T, K = X.shape
-    h = torch.empty((K,), dtype=torch.float64, device=X.device)
+    h = _empty((K,), torch.float64, X.device, stream)
     _check("mq_hessian_diag", load().mq_hessian_diag(_ptr(X), T, K, X.stride(0), _ptr(h),
                                                      _stream(stream)))
     return h
@@ -517,7 +529,7 @@ def block_scores_dhessian(W, Wq, s_w, h, stream=None):
     torch = _torch()
     _need(W, torch.float32, "W", 2)
     N, K = W.shape
-    score = torch.empty((N // BLOCK, K // BLOCK), dtype=torch.float64, device=W.device)
+    score = _empty((N // BLOCK, K // BLOCK), torch.float64, W.device, stream)
     _check("mq_block_scores_dhessian", load().mq_block_scores_dhessian(
         _ptr(W), N, K, W.stride(0), _ptr(Wq), _ptr(s_w), _ptr(h), _ptr(score), _stream(stream)))
     return score
@@ -528,8 +540,8 @@ def select_blocks(score, nnzb: int, stream=None):
     torch = _torch()
     _need(score, torch.float64, "score", 2)
     NB, KB = score.shape
-    rowptr = torch.empty((NB + 1,), dtype=torch.int32, device=score.device)
-    kb = torch.empty((max(nnzb, 1),), dtype=torch.int32, device=score.device)
+    rowptr = _empty((NB + 1,), torch.int32, score.device, stream)
+    kb = _empty((max(nnzb, 1),), torch.int32, score.device, stream)
     _check("mq_select_blocks", load().mq_select_blocks(_ptr(score), NB, KB, nnzb, _ptr(rowptr),
                                                        _ptr(kb), _stream(stream)))
     return rowptr, kb[:nnzb]
@@ -540,8 +552,8 @@ def quantize_residual(W, Wq, s_w, rowptr, kb, stream=None):
     _need(W, torch.float32, "W", 2)
     N, K = W.shape
     nnzb = int(kb.numel())
-    Rq = torch.empty((max(nnzb, 1), BLOCK, BLOCK // 2), dtype=torch.uint8, device=W.device)
-    s_r = torch.empty((max(nnzb, 1), BLOCK), dtype=torch.float16, device=W.device)
+    Rq = _empty((max(nnzb, 1), BLOCK, BLOCK // 2), torch.uint8, W.device, stream)
+    s_r = _empty((max(nnzb, 1), BLOCK), torch.float16, W.device, stream)
     _check("mq_quantize_residual", load().mq_quantize_residual(
         _ptr(W), N, K, W.stride(0), _ptr(Wq), _ptr(s_w), _ptr(rowptr),
         _ptr(kb) if nnzb else None, nnzb, _ptr(Rq), _ptr(s_r), _stream(stream)))

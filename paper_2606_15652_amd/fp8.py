@@ -12,8 +12,8 @@ import math
 from contextlib import nullcontext
 from dataclasses import dataclass, field
 
-from . import _check, _need, _need_out, _ptr, _scratch, _stream, _torch, load
-from .serving import _INT_MAX, _dtype_code, _empty, _need_heads, _need_max_q, _need_rows, _same_device
+from . import _check, _empty, _need, _need_out, _ptr, _scratch, _stream, _torch, load
+from .serving import _INT_MAX, _dtype_code, _need_heads, _need_max_q, _need_rows, _same_device
 
 _no_guard = nullcontext()
 

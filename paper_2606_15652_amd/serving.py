@@ -10,7 +10,7 @@ import ctypes as C
 import math
 from dataclasses import dataclass, field
 
-from . import _check, _need, _need_out, _ptr, _scratch, _stream, _torch, load
+from . import _check, _empty, _need, _need_out, _ptr, _scratch, _stream, _torch, load
 
 LAYOUTS = {"rows": 0, "a8": 1}
 
@@ -31,16 +31,6 @@ def _dtype_code(dtype, name, fp32=False):
     if code is None or (code == 2 and not fp32):
         raise TypeError(f"{name} must be fp16{', bf16 or fp32' if fp32 else ' or bf16'}, got {dtype}")
     return code
-
-
-def _empty(shape, dtype, device, stream):
-    """A result that a launch on ``stream`` writes: tied to it when that is not torch's current stream, so
-    that its memory is not handed out again while the launch still writes it."""
-    torch = _torch()
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and stream != torch.cuda.current_stream(device):
-        t.record_stream(stream)
-    return t
 
 
 def _need_rows(t, name, cols=None):
