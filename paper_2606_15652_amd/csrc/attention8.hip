@@ -22,8 +22,8 @@
 // Two kernels: for few columns, whose waves share out the tokens and load codes straight
 // to registers, memory bounds it (two contexts of up to 131072 tokens 86 us, 5.5 TB/s; 64 of up
 // to 8191 107 us, 5.2; with the join 90 and 115); for many, whose waves share the tokens' codes in
-// LDS, the vector unit (8192 queries over 8192 tokens 590 us, 930 TFLOP/s; four ragged prompts
-// of up to 2047 queries 212 us with the order of their work).
+// LDS, the vector unit (8192 queries over 8192 tokens 575 to 590 us as the card's clock goes, 930 to
+// 955 TFLOP/s; four ragged prompts of up to 2047 queries 210 to 222 us with the order of their work).
 #include "kv8.h"
 
 #include <float.h>

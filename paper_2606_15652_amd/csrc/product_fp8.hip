@@ -18,8 +18,8 @@
 //
 // Two kernels, as there:
 //  * tiled: output tiles through LDS slots of one group, filled by the LDS DMA, scales of X among them.  The matrix
-//    unit, LDS and four fmas a product bound it together: 8192 rows of 8192 codes by 28672 channels 1690 us, 2.3 PFLOP/s;
-//    4096 -> 4096 at 4096 rows 64 us;
+//    unit, LDS and four fmas a product bound it together: 8192 rows of 8192 codes by 28672 channels 1610 to 1800 us
+//    as the card's clock goes, 2.1 to 2.4 PFLOP/s; 4096 -> 4096 at 4096 rows 64 to 70 us;
 //  * streaming (few rows): weights straight to registers, once; the eight waves of a workgroup share out the groups,
 //    and their sums are added in LDS in the order of the waves.  Reading the weight bounds it: 4096 -> 14336 at one row
 //    9.6 us, 6.1 TB/s.
@@ -124,7 +124,7 @@ __device__ __forceinline__ void store_block_f8(const ProductF8Args& a, int m0, i
 // on go into its slot.  Loads past the last stage read nothing: they keep the number
 // in flight the same throughout.  X is read two rows ahead, and a row's sums are put to
 // the rest after the next row's products have been issued (8192 x 8192 -> 28672 1754 us
-// without both, 1690).
+// without both, 1690 on the same card).
 // SPLIT: workgroup y takes the groups [y, y + 1) per_split and writes its sums to part[y][M][N].
 template <typename T, int WM, int WN, int MI, int SLOTS, bool SPLIT>
 __device__ __forceinline__ void product_tiled(ProductF8Args a, int per_split, float* __restrict__ part) {
